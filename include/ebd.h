@@ -57,6 +57,9 @@ typedef enum ebd_status {
                                   params.max_capacity: nothing was sampled or written for it
                                   and count[u] = 0.  ebd_attend_certify: the unit holds more
                                   rows than params.max_rows; those past it were not seen */
+#define EBD_ST_BAD_PAGE 32u    /* paged cache: a row lies on no page of the pool (its page number is
+                                  outside [0, num_pages), or its index outside the page table):
+                                  it is not written, not seen, or read out as zeros */
 
 /*
  * Sampler parameters (Sec. 3.3, eq. (2) and the certainty set).
@@ -334,16 +337,185 @@ typedef struct ebd_cert_params {
 ebd_status ebd_certificate_step(const ebd_cert_params *p, const float *radius, float *cert,
                                 float *mean_out, void *stream);
 
+/*
+ * Rotary positions.  A head's first rot_dim elements form rot_dim / 2 pairs (x1, x2); pair i of a row at
+ * position pos is turned by the angle pos * freq[i] and scaled by the amplitude:
+ *     y1 = amplitude (x1 cos - x2 sin),   y2 = amplitude (x2 cos + x1 sin)
+ * and the elements past rot_dim are copied.
+ *   freq      [rot_dim / 2] device double, radians per position (scaled for long contexts by the caller).
+ *             Angles are reduced to a turn in 64 bits, so far positions lose nothing.
+ *   rot_dim   even, 2 .. 128.
+ *   layout    EBD_ROPE_HALF (0): pair i is elements (i, i + rot_dim / 2);
+ *             EBD_ROPE_PAIRS (1): elements (2i, 2i + 1).
+ *   amplitude scales cos and sin (0 means 1).
+ *   flags     0, or EBD_ROPE_INVERSE: turned by the negative angle (with the same amplitude this is also
+ *             the gradient of the rotation).
+ */
+#define EBD_ROPE_HALF 0
+#define EBD_ROPE_PAIRS 1
+#define EBD_ROPE_INVERSE 1u
+
+typedef struct ebd_rotary {
+    const double *freq;
+    int32_t rot_dim;
+    int32_t layout;
+    float amplitude;
+    uint32_t flags;
+} ebd_rotary;
+
+/* A set of rows [tokens, heads, 128] bf16: element strides between tokens and between heads, each a
+   non-negative multiple of 8 below 2^40 (the 128 elements of a row are contiguous, its address a multiple
+   of 16 bytes). */
+typedef struct ebd_rows {
+    int64_t token_stride;
+    int64_t head_stride;
+} ebd_rows;
+
+/*
+ * ebd_rope -- rotary positions of num_tokens x num_heads rows, y = rotated x.
+ *   pos [num_tokens] device int32 (any sign).  y may be x itself (same address and strides); they may not
+ *   overlap otherwise.
+ */
+typedef struct ebd_rope_params {
+    int32_t num_tokens;
+    int32_t num_heads;
+    int32_t head_dim;
+    int32_t reserved; /* 0 */
+    ebd_rows x, y;
+    const int32_t *pos;
+    ebd_rotary rot;
+} ebd_rope_params;
+
+ebd_status ebd_rope(const ebd_rope_params *p, const uint16_t *x, uint16_t *y, void *stream);
+
+/*
+ * A paged cache: the rows of the sequences before eviction.  K and V are pools of num_pages pages of
+ * page_size rows for each KV head; row r of sequence s and head h is
+ *     page page_table[s * max_pages + r / page_size], slot r % page_size:
+ *     K + page * page_stride + h * head_stride + slot * row_stride   (elements; V alike)
+ * so that pools [pages, heads, rows, 128] and [pages, rows, heads, 128], and pools inside a larger
+ * allocation, are all described by their strides.
+ *   page_size   a power of two, 16 .. 65536.
+ *   page_table  [num_seqs, max_pages] device int32; entries past a sequence's rows are not used.
+ *   strides     positive multiples of 8; row_stride below 2^26, the others below 2^40.
+ * Limits of the calls on it (beyond them, and for other page sizes, EBD_ERR_UNSUPPORTED): fewer than 2^24 new
+ * tokens, 65536 heads, max_rows up to 2^30, and fewer than 2^24 work-groups in a launch.
+ */
+typedef struct ebd_pages {
+    int32_t num_seqs;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t page_size;
+    int32_t num_pages;
+    int32_t max_pages;
+    const int32_t *page_table;
+    int64_t page_stride;
+    int64_t head_stride;
+    int64_t row_stride;
+} ebd_pages;
+
+/*
+ * ebd_append_paged -- write new tokens' keys and values into their sequences' pages, the keys rotated on
+ * the way, and (optionally) rotate the same tokens' queries.
+ *   num_tokens  new tokens in k_new, v_new (and q, q_out).
+ *   new_off     [num_seqs + 1] device int64, non-decreasing: sequence s owns new tokens
+ *               new_off[s] .. new_off[s+1]-1; tokens before new_off[0] or from new_off[num_seqs] on are
+ *               padding: nothing is read from or written for them.
+ *   len         [num_seqs] device int32: the rows sequence s holds with its new tokens, which are its last
+ *               ones: token new_off[s] + j becomes row len[s] - (new_off[s+1] - new_off[s]) + j.
+ *   pos         [num_tokens] device int32 rotary positions, or NULL: a token's row index.
+ *   rot         rot.freq NULL: keys and queries are copied unrotated (amplitude unused).
+ *   k_new, v_new [tokens, kv_heads, 128] by k_rows, v_rows; q, q_out [tokens, q_heads, 128] by q_rows,
+ *               q_out_rows, q_heads = 0 for none (then NULL).  q_out may be q (same strides).
+ *   status      [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a new row has no page (that row is
+ *               not written; its query is rotated all the same).
+ * The caller sees to it that no two new rows share a slot.
+ */
+typedef struct ebd_append_paged_params {
+    ebd_pages pages;
+    int64_t num_tokens;
+    const int64_t *new_off;
+    const int32_t *len;
+    const int32_t *pos;
+    ebd_rotary rot;
+    int32_t q_heads;
+    int32_t reserved; /* 0 */
+    ebd_rows k_rows, v_rows, q_rows, q_out_rows;
+} ebd_append_paged_params;
+
+ebd_status ebd_append_paged(const ebd_append_paged_params *p, const uint16_t *k_new,
+                            const uint16_t *v_new, uint16_t *K, uint16_t *V, const uint16_t *q,
+                            uint16_t *q_out, uint32_t *status, void *stream);
+
+/*
+ * ebd_attend_paged -- attention of a chunk of new tokens over the paged cache (one new token per sequence:
+ * a decode step), before any eviction: no offsets, no certificate.
+ *   Token j of sequence s (index t = new_off[s] + j) sees rows lo .. hi of the sequence, with
+ *     hi = min(len[s] - 1, qpos[t]),  or len[s] - (new_off[s+1] - new_off[s]) + j when qpos is NULL,
+ *     lo = max(0, hi - window + 1),   or 0 when window is 0
+ *   and for each of its q_heads = kv_heads * group query heads (head hq reads KV head hq / group)
+ *     y = sum_{r = lo..hi} softmax_r(scale q.k_r) v_r       [tokens, q_heads, 128] bf16
+ *     lse = ln sum_{r = lo..hi} exp(scale q.k_r)            [tokens, q_heads] fp32, or NULL
+ *   A token that sees no row (hi < 0, every row on a bad page) gets y = 0 and lse = -inf.  A row that a
+ *   token does not see has no effect on it, whatever its key and value hold, infinities and NaN included.
+ *   new_off, len as for ebd_append_paged; num_tokens: tokens in q and y.  y and lse of padding tokens
+ *   (before new_off[0], from new_off[num_seqs] on) are left as they were.
+ *   max_new, max_rows: host bounds on the new tokens and on the rows of a sequence (they size the grid).  Of
+ *   a sequence with more, new tokens past max_new get no output and rows past max_rows are not seen, and
+ *   EBD_ST_BAD_LAYOUT is set.
+ *   scale: logit scale (0 means 1/sqrt(head_dim)).
+ *   status [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a row that some token sees has no page
+ *   (it is not seen), EBD_ST_BAD_LAYOUT as above.
+ *   Logits, softmax statistics and the sums over v are fp32.  workspace: at least
+ *   ebd_workspace_size(EBD_WS_ATTEND_PAGED, p) bytes, 256-byte aligned; nothing in it is kept from one
+ *   call to the next.
+ */
+typedef struct ebd_attend_paged_params {
+    ebd_pages pages;
+    int32_t group;
+    int32_t max_new;
+    int64_t num_tokens;
+    int64_t max_rows;
+    const int64_t *new_off;
+    const int32_t *len;
+    const int32_t *qpos;
+    int32_t window;
+    float scale;
+    ebd_rows q_rows, y_rows;
+} ebd_attend_paged_params;
+
+ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q, const uint16_t *K,
+                            const uint16_t *V, uint16_t *y, float *lse, uint32_t *status,
+                            void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * ebd_gather_paged -- read the paged cache out as units: unit u = s * kv_heads + h receives rows
+ * 0 .. seq_off[u+1]-seq_off[u]-1 of sequence s and head h, contiguous, as ebd_scores and ebd_evict take them.
+ *   seq_off [num_seqs * kv_heads + 1] device int64, non-decreasing; max_rows >= the longest unit (sizes the
+ *   grid; rows of a longer unit past it are not written, and flagged EBD_ST_BAD_LAYOUT).
+ *   Ku, Vu [rows, 128] bf16.  status [units] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a row has no page
+ *   (it is written as zeros).
+ */
+typedef struct ebd_gather_paged_params {
+    ebd_pages pages;
+    int64_t max_rows;
+    const int64_t *seq_off;
+} ebd_gather_paged_params;
+
+ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K, const uint16_t *V,
+                            uint16_t *Ku, uint16_t *Vu, uint32_t *status, void *stream);
+
 /* which-values for ebd_workspace_size */
 #define EBD_WS_EVICT 0
 #define EBD_WS_ATTEND 1
 #define EBD_WS_SCORES 2
+#define EBD_WS_ATTEND_PAGED 3
 
 /*
  * Workspace bytes needed by ebd_evict (which = EBD_WS_EVICT, params = ebd_evict_params*),
- * ebd_attend_certify (EBD_WS_ATTEND, ebd_attend_params*) or ebd_scores (EBD_WS_SCORES,
- * ebd_scores_params*).  Depends only on the host fields of the params.  Returns 0 on
- * invalid arguments.
+ * ebd_attend_certify (EBD_WS_ATTEND, ebd_attend_params*), ebd_scores (EBD_WS_SCORES,
+ * ebd_scores_params*) or ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*).
+ * Depends only on the host fields of the params.  Returns 0 on invalid arguments.
  */
 size_t ebd_workspace_size(int32_t which, const void *params);
 
@@ -358,10 +530,11 @@ const char *ebd_version(void);
  * launch of the library is bracketed by HIP events recorded on its own launch stream.
  * ebd_timing_read() waits for the recorded events, and adds the elapsed times of kernel `name`
  * ("evict_select", "evict_copy", "attend_split", "attend_finalize", "append_certain",
- * "scores_stats", "scores_accum", "block_contrib", "cert_step") to *total_ms and its launch
- * count to *launches; it then clears that kernel's record.  The switch is an atomic flag and the
- * records are guarded by a lock, so both calls may come from any host thread; while timing is
- * off no event is created and launches take no lock.
+ * "scores_stats", "scores_accum", "block_contrib", "cert_step", "rope", "append_paged",
+ * "attend_paged", "attend_paged_join", "gather_paged") to *total_ms and its launch count to
+ * *launches; it then clears that kernel's record.  The switch is an atomic flag and the records
+ * are guarded by a lock, so both calls may come from any host thread; while timing is off no
+ * event is created and launches take no lock.
  */
 ebd_status ebd_timing_enable(int32_t enable);
 ebd_status ebd_timing_read(const char *name, double *total_ms, int64_t *launches);

@@ -38,6 +38,7 @@ EBD_ST_BUDGET_FLOOR = 2
 EBD_ST_NO_EVICTION = 4
 EBD_ST_BAD_SCORE = 8
 EBD_ST_BAD_LAYOUT = 16
+EBD_ST_BAD_PAGE = 32
 
 EBD_DESIGN_POISSON = 0
 EBD_DESIGN_SYSTEMATIC = 1
@@ -49,6 +50,7 @@ EBD_F_NO_OFFSET = 1
 EBD_WS_EVICT = 0
 EBD_WS_ATTEND = 1
 EBD_WS_SCORES = 2
+EBD_WS_ATTEND_PAGED = 3
 EBD_SCORES_ACCUMULATE = 1
 EBD_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -253,7 +255,8 @@ def scores_params(num_units, num_queries, max_rows, seq_off, qpos=None, split_ro
 
 def ebd_workspace_size(which: int, params) -> int:
     n = _lib.ebd_workspace_size(int(which), ctypes.byref(params))
-    if n == 0 and params.num_units > 0:
+    units = params.pages.num_seqs if which == EBD_WS_ATTEND_PAGED else params.num_units
+    if n == 0 and units > 0:
         raise EbdError("ebd_workspace_size", EBD_ERR_INVALID_ARG)
     return int(n)
 
@@ -372,3 +375,8 @@ def ebd_timing_read(name: str):
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
     """A caller-owned workspace buffer (256-byte aligned by the caching allocator)."""
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+from .paged import (EBD_ROPE_HALF, EBD_ROPE_INVERSE, EBD_ROPE_PAIRS, append_paged_params,  # noqa: E402
+                    attend_paged_params, ebd_append_paged, ebd_attend_paged, ebd_gather_paged, ebd_pages, ebd_rope,
+                    ebd_rotary, gather_paged_params, pages, rope_params, rotary)

@@ -1,0 +1,494 @@
+// attend_paged.hip -- attention of a chunk of new tokens over a paged cache on gfx950.
+//
+// Query rows: token j and query head g of the heads that share a KV head make row j group + g, so that one
+// pass over the KV head's keys serves all of them.  Per row, over the rows lo .. hi it sees, in base-2
+// logits l = scale log2e q.k:
+//   m = max l,  w = 2^(l - m),  y = sum w v / sum w,  lse = m ln 2 + ln sum w
+// in one pass, m running (what was summed is scaled down when it grows).
+//
+// attend_rows (few query rows): one work-group per (sequence, KV head, block of 16 or 32 query rows, split of
+//   the rows they see), four waves that take its tiles of 32 keys in turn, each on its own.  A wave keeps the
+//   next tile's keys and values on their way into its share of LDS (loads that write LDS directly, 16 bytes a
+//   lane) while it computes the present one; nothing in the loop waits for another wave.
+//   Scores are formed transposed, S^T = K Q^T (MFMA 16x16x32 bf16: exact products, fp32 sums): lane (g, c) then
+//   holds keys 4g .. 4g+3 of query row c, so a row's maximum is a maximum over registers and two lane swaps,
+//   and its weights are, as they stand, the B operand of O^T = V^T W^T with the keys of the k slots in the order
+//   4g .. 4g+3, 16+4g .. 16+4g+3.  V^T comes from the row-major tile by transposing LDS reads.
+//   The 16-byte chunks of a tile's row r are stored at chunk ^ (r mod 16): without that, the rows a
+//   read gathers from would all lie in the same banks.
+//   Weights enter as a bf16 head and a bf16 tail (16 bits of each): the memory bounds these launches, and
+//   the second product costs nothing beside it.
+// attend_join: the splits of each row, combined in order.
+#include "ebd.h"
+#include "ebd_internal.hpp"
+#include "paged_device.hpp"
+
+namespace ebd {
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(4))) int32_t const_i32;  // read through the scalar cache
+
+constexpr int kTileKeys = 32;
+constexpr int kTileBytes = kTileKeys * 2 * kHeadDim;  // of K, or of V
+constexpr int kRowsStages = 2;
+constexpr int kRowsWaveLds = kRowsStages * 2 * kTileBytes;
+constexpr int kRowBytes = 2 * kHeadDim;
+
+__device__ __forceinline__ uint32_t lds_at(const void *p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8 *)(uint8_t *)p);
+}
+
+// 16 bytes per lane from base + off straight into LDS at `to` + 16 lane.  Written as assembly because the
+// compiler would wait for all of them before any read of LDS; it holds no result register, and the
+// waits below order it.
+__device__ __forceinline__ void load_lds16(uint32_t to, const uint8_t *base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ bf16x8 join8(s16x4 lo, s16x4 hi) {
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ s16x4 read_transposed(const uint8_t *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_u8 *)p);
+}
+
+__device__ __forceinline__ float max_xor16_32(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// A sequence's part of a launch.
+struct Seq {
+  int64_t t0;       // its first new token
+  int tokens;       // new tokens that get an output
+  int64_t first;    // row of its first new token
+  int64_t len;      // rows it holds
+  int64_t seen;     // ... of which the launch can see
+  uint32_t status;
+};
+__device__ __forceinline__ Seq sequence(const ebd_attend_paged_params &p, int s) {
+  Seq q;
+  q.t0 = p.new_off[s];
+  const int64_t n = p.new_off[s + 1] - q.t0;
+  q.len = p.len[s];
+  q.first = q.len - n;
+  q.status = (n > p.max_new || q.len > p.max_rows) ? EBD_ST_BAD_LAYOUT : 0u;
+  q.seen = min(q.len, p.max_rows);
+  const int64_t room = (int64_t)p.pages.max_pages * p.pages.page_size;
+  if (q.seen > room) {
+    q.status |= EBD_ST_BAD_PAGE;
+    q.seen = room;
+  }
+  q.tokens = (int)max((int64_t)0, min(min(n, (int64_t)p.max_new), p.num_tokens - q.t0));
+  if (q.t0 < 0) q.tokens = 0;
+  return q;
+}
+
+// The rows lo .. hi - 1 that query row `row` sees (lo >= hi: none).
+struct Span {
+  int lo, hi;
+};
+__device__ __forceinline__ Span span_of(const ebd_attend_paged_params &p, const Seq &q, int row) {
+  const int j = row / p.group;
+  if (j >= q.tokens) return {0, 0};
+  int64_t last = q.first + j;
+  if (p.qpos) last = min((int64_t)p.qpos[q.t0 + j], q.len - 1);
+  const int64_t lo = p.window > 0 ? max((int64_t)0, last - p.window + 1) : 0;
+  const int64_t hi = min(last + 1, q.seen);
+  return lo < hi ? Span{(int)lo, (int)hi} : Span{0, 0};
+}
+
+// The range a block of query rows sees (the same in every lane of a wave that holds them all), and
+// whether a tile needs masks: inside [every_lo, every_hi) every row that sees anything sees all.
+struct Range {
+  int lo, hi, every_lo, every_hi;
+};
+template <int N>
+__device__ __forceinline__ Range range_of(const Span (&s)[N]) {
+  int lo = INT32_MAX, hi = 0, elo = 0, ehi = INT32_MAX;
+#pragma unroll
+  for (int b = 0; b < N; ++b) {
+    if (s[b].lo >= s[b].hi) continue;
+    lo = min(lo, s[b].lo), hi = max(hi, s[b].hi);
+    elo = max(elo, s[b].lo), ehi = min(ehi, s[b].hi);
+  }
+  return {wave_min(lo), -wave_min(-hi), -wave_min(-elo), wave_min(ehi)};
+}
+
+// Elements e .. e+7 of a finished row: token t, query head hq, sums o over weights that total Z with the
+// maximum M (-inf: the row saw nothing).
+__device__ __forceinline__ void store_row(const AttendPagedLaunch &L, int64_t t, int hq, int e, float M, float Z,
+                                          const float (&o)[8]) {
+  const bool any = M != -INFINITY;
+  const float a = any ? 1.0f / Z : 0.0f;
+  uint4 v;
+  v.x = any ? pack_bf16(o[0] * a, o[1] * a) : 0u;
+  v.y = any ? pack_bf16(o[2] * a, o[3] * a) : 0u;
+  v.z = any ? pack_bf16(o[4] * a, o[5] * a) : 0u;
+  v.w = any ? pack_bf16(o[6] * a, o[7] * a) : 0u;
+  *reinterpret_cast<uint4 *>(L.y + t * L.p.y_rows.token_stride + hq * L.p.y_rows.head_stride + e) = v;
+  if (e == 0 && L.lse)
+    L.lse[t * ((int64_t)L.p.pages.kv_heads * L.p.group) + hq] = any ? (M + fast_log2(Z)) * kLn2 : -INFINITY;
+}
+
+}  // namespace
+
+template <int NQ>
+__global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L) {
+  __shared__ __align__(1024) uint8_t lds[kRowsWaves * kRowsWaveLds];
+  const ebd_attend_paged_params &p = L.p;
+  constexpr int kRows = 16 * NQ;
+  const int H = p.pages.kv_heads, G = p.group;
+  int bid = blockIdx.x;
+  const int sp = bid % L.nsplit;
+  bid /= L.nsplit;
+  const int rb = bid % L.blocks;
+  bid /= L.blocks;
+  const int h = bid % H, s = bid / H;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  const Seq sq = sequence(p, s);
+  const int row0 = rb * kRows, nrow = min(kRows, sq.tokens * G - row0);
+  if (threadIdx.x == 0 && rb == 0 && sp == 0 && h == 0 && L.status && sq.status) atomicOr(&L.status[s], sq.status);
+  if (nrow <= 0) return;
+
+  Span span[NQ];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) span[b] = span_of(p, sq, row0 + 16 * b + c);
+  const Range R = range_of<NQ>(span);
+  // this split's keys
+  const int64_t start = (R.lo & -kTileKeys) + (int64_t)sp * L.split_rows;
+  const int k_end = start < R.hi ? (int)min((int64_t)R.hi, start + L.split_rows) : 0;
+  const int k_beg = start < R.hi ? (int)start : 0;  // rows stay below 2^30: no sum below overflows
+
+  bf16x8 Q[NQ][4];  // B operand: column c of block b is query row 16 b + c
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    const int row = row0 + 16 * b + c;
+    const bool ok = span[b].lo < span[b].hi;
+    const int j = ok ? row / G : 0, hq = h * G + (ok ? row % G : 0);
+    const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+      Q[b][kb] = __builtin_bit_cast(bf16x8, ok ? reinterpret_cast<const uint4 *>(q)[4 * kb + g] : make_uint4(0u, 0u, 0u, 0u));
+  }
+
+  // the queries are here before any tile is asked for: a wait for them in the loop would be one for all loads
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) asm volatile("" : "+v"(Q[b][kb]));
+  }
+
+  f32x4 O[NQ][8];
+  float m[NQ], z[NQ];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    m[b] = -INFINITY;
+    z[b] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) O[b][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  // lane offsets (bytes) of rows 4i + g of a 16-row slab, chunks permuted
+  uint8_t *my = lds + wave * kRowsWaveLds;
+  const uint32_t rs = (uint32_t)p.pages.row_stride * 2u;
+  uint32_t off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) off[i] = (uint32_t)g * rs + (uint32_t)(c ^ (4 * i + g)) * 16u;
+  const int64_t head = (int64_t)h * p.pages.head_stride;
+  const const_i32 *table = (const const_i32 *)(p.pages.page_table + (int64_t)s * p.pages.max_pages);
+  const int slots = p.pages.page_size - 1;
+
+  // page numbers of the two slabs of the tile at key k (uniform); -1: none
+  auto page_of = [&](int k) -> int {
+    if (k >= k_end) return 0;  // past the range: never loaded, or masked
+    return table[k >> L.shift];
+  };
+  uint32_t bad_any = 0;
+  auto issue = [&](int k, int pg0, int pg1, int stage) -> uint32_t {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      int pg = b ? pg1 : pg0;
+      if ((uint32_t)pg >= (uint32_t)p.pages.num_pages) {
+        pg = 0;
+        bad |= 1u << b;
+      }
+      const int slot = (k + 16 * b) & slots;
+      const int64_t at = 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)slot * rs;
+      const uint8_t *pk = reinterpret_cast<const uint8_t *>(L.K) + at;
+      const uint8_t *pv = reinterpret_cast<const uint8_t *>(L.V) + at;
+      const uint32_t to = lds_at(my + stage * 2 * kTileBytes + b * 16 * kRowBytes);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        load_lds16(to + i * 4 * kRowBytes, pk + (int64_t)(4 * i) * rs, off[i]);
+        load_lds16(to + kTileBytes + i * 4 * kRowBytes, pv + (int64_t)(4 * i) * rs, off[i]);
+      }
+    }
+    return bad;
+  };
+
+  const float sc2 = L.scale * kLog2e;
+  const int stride = kRowsWaves * kTileKeys;
+  int k = k_beg + wave * kTileKeys, stage = 0;
+  uint32_t bad = 0;
+  int pg0 = 0, pg1 = 0;
+  if (k < k_end) {
+    bad = issue(k, page_of(k), page_of(k + 16), 0);
+    pg0 = page_of(k + stride), pg1 = page_of(k + stride + 16);
+  }
+  for (; k < k_end; k += stride, stage ^= 1) {
+    uint32_t next_bad = 0;
+    if (k + stride < k_end) {
+      wait_lds();
+      next_bad = issue(k + stride, pg0, pg1, stage ^ 1);
+      pg0 = page_of(k + 2 * stride), pg1 = page_of(k + 2 * stride + 16);
+      wait_loads<16>();
+    } else {
+      wait_loads<0>();
+    }
+    uint8_t *Kt = my + stage * 2 * kTileBytes, *Vt = Kt + kTileBytes;
+    // values of rows that no query row may see must not reach a product: 0 x NaN
+    if (k + kTileKeys > k_end || bad) {
+      const int keep = k_end - k;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + g;
+        if (r >= keep || ((bad >> (i / 4)) & 1u))
+          *reinterpret_cast<uint4 *>(Vt + r * kRowBytes + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
+    const bool mixed = bad || k < R.every_lo || k + kTileKeys > min(R.every_hi, k_end);
+
+    f32x4 S[NQ][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) S[b][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        const bf16x8 A = *reinterpret_cast<const bf16x8 *>(Kt + (16 * t + c) * kRowBytes + ((4 * kb + g) ^ c) * 16);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) S[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Q[b][kb], S[b][t], 0, 0, 0);
+      }
+    }
+    float w[NQ][8];
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[b][i] = S[b][i / 4][i % 4] * sc2;
+      if (mixed) {
+        const int hi = min(span[b].hi, k_end);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = k + 16 * (i / 4) + 4 * g + i % 4;
+          const bool ok = (key >= span[b].lo) & (key < hi) & !((bad >> (i / 4)) & 1u);
+          w[b][i] = ok ? w[b][i] : -INFINITY;
+        }
+      }
+      float t = fmaxf(fmaxf(fmaxf(w[b][0], w[b][1]), fmaxf(w[b][2], w[b][3])),
+                      fmaxf(fmaxf(w[b][4], w[b][5]), fmaxf(w[b][6], w[b][7])));
+      t = max_xor16_32(t);
+      if (__any(t > m[b])) {
+        const float mn = fmaxf(m[b], t);
+        const float a = mn == -INFINITY ? 1.0f : fast_exp2(m[b] - mn);
+        m[b] = mn;
+        z[b] *= a;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) O[b][d] *= a;
+      }
+      const float mu = m[b] == -INFINITY ? 0.0f : m[b];  // nothing seen yet: every l is -inf
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[b][i] = fast_exp2(w[b][i] - mu);
+        z[b] += w[b][i];
+      }
+    }
+    bf16x8 hi[NQ], lo[NQ];
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        hi[b][i] = (__bf16)w[b][i];
+        lo[b][i] = (__bf16)(w[b][i] - (float)hi[b][i]);
+      }
+    }
+    // V^T operand of dims 16 d .. + 15
+    auto values = [&](int d) {
+      const int r = 4 * g + (c >> 2);
+      const uint8_t *a = Vt + r * kRowBytes + (((2 * d + ((c & 3) >> 1)) ^ r) * 16) + 8 * (c & 1);
+      return join8(read_transposed(a), read_transposed(a + 16 * kRowBytes));
+    };
+    bool special = false;
+    if (mixed) {
+      // some row may not see a key that another sees: an infinity or NaN there must not reach it
+      uint32_t top = 0;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const u32x4 v = __builtin_bit_cast(u32x4, values(d));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          top |= (v[i] & 0x7f80u) == 0x7f80u;
+          top |= (v[i] & 0x7f800000u) == 0x7f800000u;
+        }
+      }
+      special = __any(top);
+    }
+    if (!special) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const bf16x8 A = values(d);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) {
+          O[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, lo[b], O[b][d], 0, 0, 0);
+          O[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, hi[b], O[b][d], 0, 0, 0);
+        }
+      }
+    } else {
+      // the same sums key by key, those that a row does not see left out; the weights go through the K
+      // tile's place, which has been read
+      float *W = reinterpret_cast<float *>(Kt);  // [kTileKeys][kRows]
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 16 * (i / 4) + 4 * g + i % 4, key = k + r;
+          const bool ok = (key >= span[b].lo) & (key < min(span[b].hi, k_end)) & !((bad >> (i / 4)) & 1u);
+          W[r * kRows + 16 * b + c] = ok ? w[b][i] : -1.0f;
+        }
+      }
+      wave_sync();
+#pragma unroll 1
+      for (int r = 0; r < kTileKeys; ++r) {
+        float wk[NQ];
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) wk[b] = W[r * kRows + 16 * b + c];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const u32x2 v = *reinterpret_cast<const u32x2 *>(
+              Vt + r * kRowBytes + (((2 * d + (g >> 1)) ^ (r & 15)) * 16) + 8 * (g & 1));
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) {
+            const bool ok = !(wk[b] < 0.0f);  // a NaN weight counts
+            O[b][d][0] += ok ? wk[b] * bf16_lo(v[0]) : 0.0f;
+            O[b][d][1] += ok ? wk[b] * bf16_hi(v[0]) : 0.0f;
+            O[b][d][2] += ok ? wk[b] * bf16_lo(v[1]) : 0.0f;
+            O[b][d][3] += ok ? wk[b] * bf16_hi(v[1]) : 0.0f;
+          }
+        }
+      }
+      wave_sync();
+    }
+    bad_any |= bad;
+    bad = next_bad;
+  }
+  if (bad_any && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+
+  // The waves' sums, combined in order; a row that sees nothing keeps none.
+  __syncthreads();
+  float *Ow = reinterpret_cast<float *>(my);            // [kRows][132]
+  float2 *mz = reinterpret_cast<float2 *>(Ow + kRows * 132);  // [kRows]
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    z[b] = add_xor32(add_xor16(z[b]));
+    if (g == 0) mz[16 * b + c] = span[b].lo < span[b].hi ? make_float2(m[b], z[b]) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4 *>(Ow + (16 * b + c) * 132 + 16 * d + 4 * g) = O[b][d];
+  }
+  __syncthreads();
+  const int64_t slot = blockIdx.x;
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    const int r = 16 * b + (threadIdx.x >> 4), e = (threadIdx.x & 15) * 8;
+    float M = -INFINITY, Z = 0.0f, o[8] = {};
+#pragma unroll
+    for (int v = 0; v < kRowsWaves; ++v)
+      M = fmaxf(M, reinterpret_cast<const float2 *>(lds + v * kRowsWaveLds + kRows * 528)[r].x);
+#pragma unroll
+    for (int v = 0; v < kRowsWaves; ++v) {
+      const float *Ov = reinterpret_cast<const float *>(lds + v * kRowsWaveLds);
+      const float2 t = reinterpret_cast<const float2 *>(Ov + kRows * 132)[r];
+      if (t.x == -INFINITY) continue;  // this wave saw nothing of the row
+      const float a = fast_exp2(t.x - M);
+      Z += a * t.y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] += a * Ov[r * 132 + e + i];
+    }
+    if (r >= nrow) continue;
+    if (L.nsplit > 1) {
+      float *part = L.part + (slot * kRows + r) * kHeadDim + e;
+      if (e == 0) L.stats[slot * kRows + r] = make_float2(M, Z);
+      if (M == -INFINITY) continue;
+      *reinterpret_cast<f32x4 *>(part) = f32x4{o[0], o[1], o[2], o[3]};
+      *reinterpret_cast<f32x4 *>(part + 4) = f32x4{o[4], o[5], o[6], o[7]};
+    } else {
+      store_row(L, sq.t0 + (row0 + r) / G, h * G + (row0 + r) % G, e, M, Z, o);
+    }
+  }
+}
+
+// Work-group per (sequence, KV head, block of query rows): 16 lanes a row, eight elements each.
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
+  const ebd_attend_paged_params &p = L.p;
+  const int H = p.pages.kv_heads, G = p.group;
+  int bid = blockIdx.x;
+  const int sub = bid % (L.rows / 16);
+  bid /= L.rows / 16;
+  const int64_t slot0 = (int64_t)bid * L.nsplit;
+  const int rb = bid % L.blocks;
+  bid /= L.blocks;
+  const int h = bid % H, s = bid / H;
+  const Seq sq = sequence(p, s);
+  const int r = 16 * sub + (threadIdx.x >> 4), e = (threadIdx.x & 15) * 8;
+  const int row = rb * L.rows + r;
+  if (row >= sq.tokens * G) return;
+  float M = -INFINITY, Z = 0.0f, o[8] = {};
+  for (int v = 0; v < L.nsplit; ++v) M = fmaxf(M, L.stats[(slot0 + v) * L.rows + r].x);
+  for (int v = 0; v < L.nsplit; ++v) {
+    const float2 t = L.stats[(slot0 + v) * L.rows + r];
+    if (t.x == -INFINITY) continue;
+    const float a = fast_exp2(t.x - M);
+    const float *part = L.part + ((slot0 + v) * L.rows + r) * kHeadDim + e;
+    Z += a * t.y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] += a * part[i];
+  }
+  store_row(L, sq.t0 + row / G, h * G + row % G, e, M, Z, o);
+}
+
+size_t attend_paged_part_bytes(const AttendPagedLaunch &L) {
+  return L.nsplit > 1 ? (size_t)attend_paged_groups(L) * L.rows * (kHeadDim * sizeof(float) + sizeof(float2)) : 0;
+}
+
+int64_t attend_paged_groups(const AttendPagedLaunch &L) {
+  return (int64_t)L.p.pages.num_seqs * L.p.pages.kv_heads * L.blocks * L.nsplit;
+}
+
+hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
+  const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
+  if (L.rows == 16) hipLaunchKernelGGL(attend_rows_kernel<1>, grid, block, 0, s, L);
+  else hipLaunchKernelGGL(attend_rows_kernel<2>, grid, block, 0, s, L);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_paged_join(const AttendPagedLaunch &L, hipStream_t s) {
+  const int64_t groups = attend_paged_groups(L) / L.nsplit * (L.rows / 16);
+  hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)groups), dim3(256), 0, s, L);
+  return hipGetLastError();
+}
+
+}  // namespace ebd

@@ -325,6 +325,10 @@ namespace ebd {
 
 ebd_status device_ok() { return check_device(); }
 
+hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch) {
+  return timed(name, s, launch);
+}
+
 ebd_status attend_check(const ebd_attend_params *p, const uint16_t *q, const uint16_t *Kc,
                         const uint16_t *Vc, const float *pic, const int32_t *count, const float *y,
                         const float *vhat, const float *lse, size_t *need) {
@@ -432,6 +436,8 @@ size_t ebd_workspace_size(int32_t which, const void *params) {
     const int32_t sr = scores_split_rows(p);
     return scores_workspace_bytes(p->num_units, scores_nsplit(p, sr), p->num_queries);
   }
+  if (which == EBD_WS_ATTEND_PAGED)
+    return attend_paged_workspace(static_cast<const ebd_attend_paged_params *>(params));
   return 0;
 }
 

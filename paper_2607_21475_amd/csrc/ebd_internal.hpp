@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <functional>
+
 #include "ebd.h"
 
 namespace ebd {
@@ -161,6 +163,49 @@ struct CertLaunch {
   float *cert, *mean_out;
 };
 
+struct RopeLaunch {
+  ebd_rope_params p;  // amplitude resolved
+  const uint16_t *x;
+  uint16_t *y;
+  int32_t tpb;  // tokens per work-group
+};
+
+struct AppendPagedLaunch {
+  ebd_append_paged_params p;
+  const uint16_t *k_new, *v_new, *q;
+  uint16_t *K, *V, *q_out;
+  uint32_t *status;
+  int32_t shift;  // log2 page_size
+  int32_t tpb;
+};
+
+struct GatherPagedLaunch {
+  ebd_gather_paged_params p;
+  const uint16_t *K, *V;
+  uint16_t *Ku, *Vu;
+  uint32_t *status;
+  int32_t shift;
+  int32_t chunks;  // work-groups per unit
+};
+
+struct AttendPagedLaunch {
+  ebd_attend_paged_params p;
+  const uint16_t *q, *K, *V;
+  uint16_t *y;
+  float *lse;
+  uint32_t *status;
+  float scale;
+  int32_t shift;
+  int32_t rows;        // query rows per block
+  int32_t blocks;      // ... blocks per sequence and KV head
+  int32_t nsplit;      // splits of the rows a block sees
+  int32_t split_rows;  // ... rows each
+  float *part;         // [groups, rows, 128] sums of the splits, then
+  float2 *stats;       // [groups, rows] their maximum and total weight
+};
+
+constexpr int kRowsWaves = 4;  // waves of an attend_rows work-group
+
 constexpr int64_t kMaxBlocks = 8192;  // blocks per unit of ebd_block_contributions (LDS bins)
 constexpr int kBlockWaves = 8;        // most waves of its work-groups
 
@@ -181,6 +226,19 @@ ebd_status attend_launch(const ebd_attend_params *p, const uint16_t *q, const ui
                          const uint16_t *Vc, const float *pic, const int32_t *count, float *y,
                          float *vhat, float *lse, float *brange, float *radius, uint32_t *status,
                          void *workspace, void *stream, bool timing);
+
+// Launches through the optional timing record (ebd_api.cpp).
+hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch);
+
+hipError_t launch_rope(RopeLaunch L, hipStream_t s);
+hipError_t launch_append_paged(AppendPagedLaunch L, hipStream_t s);
+int64_t gather_paged_groups(const ebd_gather_paged_params &p);
+hipError_t launch_gather_paged(GatherPagedLaunch L, hipStream_t s);
+int64_t attend_paged_groups(const AttendPagedLaunch &L);
+size_t attend_paged_part_bytes(const AttendPagedLaunch &L);
+size_t attend_paged_workspace(const ebd_attend_paged_params *p);  // 0: invalid parameters
+hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s);
+hipError_t launch_attend_paged_join(const AttendPagedLaunch &L, hipStream_t s);
 
 hipError_t launch_evict_select(const EvictLaunch &L, hipStream_t s);
 hipError_t launch_evict_copy(const EvictLaunch &L, hipStream_t s);

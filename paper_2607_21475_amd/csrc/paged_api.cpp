@@ -1,0 +1,207 @@
+// paged_api.cpp -- the C ABI of the paged cache: argument validation and launch planning.
+#include "ebd.h"
+
+#include <hip/hip_runtime_api.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "ebd_internal.hpp"
+
+namespace {
+
+using namespace ebd;
+
+constexpr int64_t kStrideMax = (int64_t)1 << 40;
+constexpr int64_t kRowStrideMax = (int64_t)1 << 26;  // a lane's offset inside 16 rows stays below 32 bits
+constexpr int64_t kGridMax = ((int64_t)1 << 24) - 1;  // work-groups of 256 threads in a launch
+constexpr int64_t kRowsMax = (int64_t)1 << 30;         // rows of a sequence
+constexpr int32_t kHeadsMax = 65536;
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+bool valid_rows(const ebd_rows &r) {
+  return r.token_stride >= 0 && r.head_stride >= 0 && r.token_stride % 8 == 0 && r.head_stride % 8 == 0 &&
+         r.token_stride < kStrideMax && r.head_stride < kStrideMax;
+}
+
+bool valid_pages(const ebd_pages &P) {
+  if (P.num_seqs < 0 || P.kv_heads < 1 || P.num_pages < 1 || P.max_pages < 1 || P.page_size < 1) return false;
+  if (P.num_seqs > 0 && !P.page_table) return false;
+  if (P.page_stride < 8 || P.head_stride < 8 || P.row_stride < 8) return false;
+  if (P.page_stride % 8 || P.head_stride % 8 || P.row_stride % 8) return false;
+  return true;
+}
+
+bool supported_pages(const ebd_pages &P) {
+  return P.head_dim == kHeadDim && P.kv_heads <= kHeadsMax && P.page_size >= 16 && P.page_size <= 65536 &&
+         (P.page_size & (P.page_size - 1)) == 0 && P.page_stride < kStrideMax && P.head_stride < kStrideMax &&
+         P.row_stride < kRowStrideMax;
+}
+
+int32_t log2_of(int32_t n) {
+  int32_t s = 0;
+  while ((1 << s) < n) ++s;
+  return s;
+}
+
+bool valid_rotary(const ebd_rotary &R) {
+  if (R.rot_dim < 2 || R.rot_dim > kHeadDim || R.rot_dim % 2) return false;
+  if (R.layout != EBD_ROPE_HALF && R.layout != EBD_ROPE_PAIRS) return false;
+  if ((R.flags & ~EBD_ROPE_INVERSE) != 0u || !std::isfinite(R.amplitude)) return false;
+  return ((uintptr_t)R.freq & 7) == 0;
+}
+
+float amplitude_of(const ebd_rotary &R) { return R.amplitude != 0.0f ? R.amplitude : 1.0f; }
+
+bool valid_attend_paged(const ebd_attend_paged_params *p) {
+  if (!p || !valid_pages(p->pages)) return false;
+  if (p->group < 1 || p->max_new < 0 || p->num_tokens < 0 || p->max_rows < 0) return false;
+  if (p->window < 0 || p->scale < 0.0f || !std::isfinite(p->scale)) return false;
+  return valid_rows(p->q_rows) && valid_rows(p->y_rows);
+}
+
+bool supported_attend_paged(const ebd_attend_paged_params *p) {
+  return supported_pages(p->pages) && (int64_t)p->group * p->pages.kv_heads <= kHeadsMax &&
+         p->num_tokens <= kGridMax && p->max_rows <= kRowsMax && (int64_t)p->max_new * p->group <= INT32_MAX / 2;
+}
+
+// How a launch is cut.  Units (sequence, KV head, block of query rows) are split until there are
+// kRowsGroups work-groups; a split holds at least a tile for each wave.
+constexpr int64_t kRowsGroups = 256;
+constexpr int64_t kRowsLeast = 128;
+AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
+  AttendPagedLaunch L{};
+  L.p = *p;
+  const int64_t rows = (int64_t)p->max_new * p->group;
+  L.rows = rows <= 16 ? 16 : 32;
+  L.blocks = (int32_t)std::max<int64_t>(1, (rows + L.rows - 1) / L.rows);
+  // the most rows a block of query rows sees, from a tile's border on
+  int64_t span = p->max_rows;
+  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows + 32);
+  span = std::max<int64_t>(span, 1) + 31;
+  const int64_t units = std::max<int64_t>(1, (int64_t)p->pages.num_seqs * p->pages.kv_heads * L.blocks);
+  int64_t ns = std::max<int64_t>(1, kRowsGroups / units);
+  ns = std::min<int64_t>(ns, std::max<int64_t>(1, span / kRowsLeast));
+  L.split_rows = (int32_t)std::min<int64_t>(((span + ns - 1) / ns + 127) / 128 * 128, (INT32_MAX / 128) * 128);
+  L.nsplit = (int32_t)((span + L.split_rows - 1) / L.split_rows);
+  L.shift = log2_of(p->pages.page_size);
+  L.scale = p->scale > 0.0f ? p->scale : 1.0f / std::sqrt((float)kHeadDim);
+  return L;
+}
+
+}  // namespace
+
+namespace ebd {
+
+size_t attend_paged_workspace(const ebd_attend_paged_params *p) {
+  if (!valid_attend_paged(p) || !supported_attend_paged(p)) return 0;
+  return (attend_paged_part_bytes(attend_paged_plan(p)) + 256) / 256 * 256;
+}
+
+}  // namespace ebd
+
+extern "C" {
+
+ebd_status ebd_rope(const ebd_rope_params *p, const uint16_t *x, uint16_t *y, void *stream) {
+  if (!p || p->num_tokens < 0 || p->num_heads < 0 || p->reserved != 0) return EBD_ERR_INVALID_ARG;
+  if (!valid_rotary(p->rot) || !valid_rows(p->x) || !valid_rows(p->y)) return EBD_ERR_INVALID_ARG;
+  if (p->head_dim != kHeadDim || p->num_tokens > kGridMax || p->num_heads > kHeadsMax) return EBD_ERR_UNSUPPORTED;
+  if (p->num_tokens == 0 || p->num_heads == 0) return EBD_OK;
+  if (!x || !y || !p->pos || !p->rot.freq || !aligned16(x) || !aligned16(y)) return EBD_ERR_INVALID_ARG;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  RopeLaunch L{};
+  L.p = *p;
+  L.p.rot.amplitude = amplitude_of(p->rot);
+  L.x = x;
+  L.y = y;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("rope", s, [&] { return launch_rope(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
+}
+
+ebd_status ebd_append_paged(const ebd_append_paged_params *p, const uint16_t *k_new,
+                            const uint16_t *v_new, uint16_t *K, uint16_t *V, const uint16_t *q,
+                            uint16_t *q_out, uint32_t *status, void *stream) {
+  if (!p || !valid_pages(p->pages) || p->num_tokens < 0 || p->q_heads < 0 || p->reserved != 0)
+    return EBD_ERR_INVALID_ARG;
+  if (p->rot.freq && !valid_rotary(p->rot)) return EBD_ERR_INVALID_ARG;
+  if (!valid_rows(p->k_rows) || !valid_rows(p->v_rows) || !valid_rows(p->q_rows) || !valid_rows(p->q_out_rows))
+    return EBD_ERR_INVALID_ARG;
+  if (!supported_pages(p->pages) || p->num_tokens > kGridMax || p->q_heads > kHeadsMax) return EBD_ERR_UNSUPPORTED;
+  if (p->num_tokens == 0 || p->pages.num_seqs == 0) return EBD_OK;
+  if (!k_new || !v_new || !K || !V || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(K) || !aligned16(V)) return EBD_ERR_INVALID_ARG;
+  if ((p->q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr)) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(q_out)) return EBD_ERR_INVALID_ARG;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  AppendPagedLaunch L{};
+  L.p = *p;
+  L.p.rot.amplitude = amplitude_of(p->rot);
+  L.k_new = k_new;
+  L.v_new = v_new;
+  L.q = q;
+  L.K = K;
+  L.V = V;
+  L.q_out = q_out;
+  L.status = status;
+  L.shift = log2_of(p->pages.page_size);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("append_paged", s, [&] { return launch_append_paged(L, s); }) == hipSuccess ? EBD_OK
+                                                                                                   : EBD_ERR_HIP;
+}
+
+ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q, const uint16_t *K,
+                            const uint16_t *V, uint16_t *y, float *lse, uint32_t *status,
+                            void *workspace, size_t ws_bytes, void *stream) {
+  if (!valid_attend_paged(p)) return EBD_ERR_INVALID_ARG;
+  if (!supported_attend_paged(p)) return EBD_ERR_UNSUPPORTED;
+  if (p->num_tokens == 0 || p->pages.num_seqs == 0) return EBD_OK;
+  if (!q || !K || !V || !y || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(y) || ((uintptr_t)lse & 3))
+    return EBD_ERR_INVALID_ARG;
+  AttendPagedLaunch L = attend_paged_plan(p);
+  if (attend_paged_groups(L) > kGridMax) return EBD_ERR_UNSUPPORTED;
+  if (!workspace || ws_bytes < attend_paged_workspace(p) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  L.q = q;
+  L.K = K;
+  L.V = V;
+  L.y = y;
+  L.lse = lse;
+  L.status = status;
+  L.part = static_cast<float *>(workspace);
+  L.stats = reinterpret_cast<float2 *>(L.part + attend_paged_groups(L) * L.rows * kHeadDim);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (timed_launch("attend_paged", s, [&] { return launch_attend_paged(L, s); }) != hipSuccess) return EBD_ERR_HIP;
+  if (L.nsplit > 1 &&
+      timed_launch("attend_paged_join", s, [&] { return launch_attend_paged_join(L, s); }) != hipSuccess)
+    return EBD_ERR_HIP;
+  return EBD_OK;
+}
+
+ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K, const uint16_t *V,
+                            uint16_t *Ku, uint16_t *Vu, uint32_t *status, void *stream) {
+  if (!p || !valid_pages(p->pages) || p->max_rows < 0) return EBD_ERR_INVALID_ARG;
+  if (!supported_pages(p->pages) || p->max_rows > kRowsMax || gather_paged_groups(*p) > kGridMax) return EBD_ERR_UNSUPPORTED;
+  if (p->pages.num_seqs == 0 || p->max_rows == 0) return EBD_OK;
+  if (!K || !V || !Ku || !Vu || !p->seq_off) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(Ku) || !aligned16(Vu)) return EBD_ERR_INVALID_ARG;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  GatherPagedLaunch L{};
+  L.p = *p;
+  L.K = K;
+  L.V = V;
+  L.Ku = Ku;
+  L.Vu = Vu;
+  L.status = status;
+  L.shift = log2_of(p->pages.page_size);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("gather_paged", s, [&] { return launch_gather_paged(L, s); }) == hipSuccess ? EBD_OK
+                                                                                                   : EBD_ERR_HIP;
+}
+
+}  // extern "C"

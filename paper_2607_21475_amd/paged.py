@@ -1,0 +1,372 @@
+"""The paged cache in front of the eviction: binding and helpers (no method arithmetic).
+
+    ebd_rope            rotary positions of query or key rows
+    ebd_append_paged    new tokens into their sequences' pages, keys rotated on the way, queries too
+    ebd_attend_paged    attention of a chunk of new tokens, or of a decode step, over the pages
+    ebd_gather_paged    the pages read out as units, which ebd_scores and ebd_evict take
+
+Each call takes a parameter struct (`rope_params`, `append_paged_params`, ...) that a program makes once
+per plan and keeps: it holds the tables' addresses and the rows' strides.  A struct keeps the tensors
+whose addresses it holds alive, and the tensors of a call must have the shapes and strides it was made for.
+`PagedCache` allocates a pool and makes the structs of each call.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from dataclasses import dataclass
+from typing import Optional
+
+import torch
+
+from . import (EBD_ERR_INVALID_ARG, EBD_WS_ATTEND_PAGED, HEAD_DIM, EbdError, _check, _lib, _ptr, _stream,
+               ebd_workspace_size, workspace)
+
+EBD_ROPE_HALF = 0
+EBD_ROPE_PAIRS = 1
+EBD_ROPE_INVERSE = 1
+
+_P = ctypes.c_void_p
+_BF = torch.bfloat16
+
+
+class ebd_rotary(ctypes.Structure):
+    _fields_ = [
+        ("freq", ctypes.c_void_p),
+        ("rot_dim", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("amplitude", ctypes.c_float),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class ebd_rows(ctypes.Structure):
+    _fields_ = [("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class ebd_rope_params(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("x", ebd_rows),
+        ("y", ebd_rows),
+        ("pos", ctypes.c_void_p),
+        ("rot", ebd_rotary),
+    ]
+
+
+class ebd_pages(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("page_table", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+    ]
+
+
+class ebd_append_paged_params(ctypes.Structure):
+    _fields_ = [
+        ("pages", ebd_pages),
+        ("num_tokens", ctypes.c_int64),
+        ("new_off", ctypes.c_void_p),
+        ("len", ctypes.c_void_p),
+        ("pos", ctypes.c_void_p),
+        ("rot", ebd_rotary),
+        ("q_heads", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("k_rows", ebd_rows),
+        ("v_rows", ebd_rows),
+        ("q_rows", ebd_rows),
+        ("q_out_rows", ebd_rows),
+    ]
+
+
+class ebd_attend_paged_params(ctypes.Structure):
+    _fields_ = [
+        ("pages", ebd_pages),
+        ("group", ctypes.c_int32),
+        ("max_new", ctypes.c_int32),
+        ("num_tokens", ctypes.c_int64),
+        ("max_rows", ctypes.c_int64),
+        ("new_off", ctypes.c_void_p),
+        ("len", ctypes.c_void_p),
+        ("qpos", ctypes.c_void_p),
+        ("window", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("q_rows", ebd_rows),
+        ("y_rows", ebd_rows),
+    ]
+
+
+class ebd_gather_paged_params(ctypes.Structure):
+    _fields_ = [
+        ("pages", ebd_pages),
+        ("max_rows", ctypes.c_int64),
+        ("seq_off", ctypes.c_void_p),
+    ]
+
+
+_lib.ebd_rope.argtypes = [_P] * 4
+_lib.ebd_rope.restype = ctypes.c_int
+_lib.ebd_append_paged.argtypes = [_P] * 9
+_lib.ebd_append_paged.restype = ctypes.c_int
+_lib.ebd_attend_paged.argtypes = [_P] * 8 + [ctypes.c_size_t, _P]
+_lib.ebd_attend_paged.restype = ctypes.c_int
+_lib.ebd_gather_paged.argtypes = [_P] * 7
+_lib.ebd_gather_paged.restype = ctypes.c_int
+
+
+# ---- tensors -> parameters ---------------------------------------------------------------------
+
+def _table(t, dtype, shape, name):
+    """Device pointer of a contiguous tensor of this type and shape."""
+    p = _ptr(t, dtype, name)
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return p
+
+
+def _here(*tensors):
+    """The GPU that holds all of these tensors."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("tensors of one call must be on one device: got %s and %s" % (dev, t.device))
+    return dev
+
+
+def _layout(t, name, heads=None, tokens=None):
+    """(shape, strides) of rows [tokens, heads, 128] bf16, checked."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype != _BF:
+        raise TypeError("%s must be %s, got %s" % (name, _BF, t.dtype))
+    if t.dim() != 3 or t.shape[2] != HEAD_DIM or (t.numel() and t.stride(2) != 1):
+        raise ValueError("%s must be [tokens, heads, %d] with contiguous rows" % (name, HEAD_DIM))
+    if heads is not None and t.shape[1] != heads:
+        raise ValueError("%s must have %d heads, got %d" % (name, heads, t.shape[1]))
+    if tokens is not None and t.shape[0] != tokens:
+        raise ValueError("%s must have %d tokens, got %d" % (name, tokens, t.shape[0]))
+    return tuple(t.shape), t.stride()
+
+
+def _rows_of(t):
+    # a stride over one element is never used, and may be anything
+    return ebd_rows(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _distinct(t, name):
+    """Refuse outputs whose rows share memory (expanded tensors)."""
+    if t.numel() and any(n > 1 and s < HEAD_DIM for n, s in zip(t.shape[:-1], t.stride()[:-1])):
+        raise ValueError("the rows of %s must not share memory" % name)
+
+
+def _plan(p, device, keep, **tensors):
+    """Note what the calls on `p` must pass, and keep what its addresses point to."""
+    p.device, p.keep = device, keep
+    p.expect = {n: None if t is None else (t.shape, t.stride()) for n, t in tensors.items()}
+    return p
+
+
+def _arg(p, name, t):
+    """Address of a call's bf16 tensor, of the shape and strides the parameters were made for."""
+    want = p.expect[name]
+    if t is None and want is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if want is None:
+        raise ValueError("%s: the parameters were made without it" % name)
+    if t.dtype != _BF:
+        raise TypeError("%s must be %s, got %s" % (name, _BF, t.dtype))
+    if t.device != p.device:
+        raise ValueError("%s must be on %s, got %s" % (name, p.device, t.device))
+    if (t.shape, t.stride()) != want:
+        raise ValueError("%s must have the shape and strides that the parameters were made for" % name)
+    return t.data_ptr()
+
+
+def _status(p, t, n):
+    if t is None:
+        return None
+    if t.device != p.device:
+        raise ValueError("status must be on %s, got %s" % (p.device, t.device))
+    return _table(t, torch.int32, (n,), "status")
+
+
+def _launch_stream(p, stream):
+    if p.device.index != torch.cuda.current_device():
+        raise ValueError("the tensors are on %s, which is not the current device" % p.device)
+    return _stream(stream)
+
+
+def rotary(freq: Optional[torch.Tensor], layout: int = EBD_ROPE_HALF, amplitude: float = 1.0,
+           inverse: bool = False) -> ebd_rotary:
+    """Rotary positions by the frequencies `freq` [rot_dim / 2] (float64 radians per position)."""
+    r = ebd_rotary()
+    r.layout, r.amplitude = int(layout), float(amplitude)
+    r.flags = EBD_ROPE_INVERSE if inverse else 0
+    if freq is not None:
+        if freq.dim() != 1 or not 1 <= freq.numel() <= HEAD_DIM // 2:
+            raise ValueError("freq must be [rot_dim / 2], 1 to %d of them" % (HEAD_DIM // 2))
+        r.freq = _ptr(freq, torch.float64, "freq")
+        r.rot_dim = 2 * freq.numel()
+    r.keep = freq
+    return r
+
+
+def rope_params(x, y, pos, rot: ebd_rotary) -> ebd_rope_params:
+    """Rows x [tokens, heads, 128] -> y (may be x), pos [tokens] int32."""
+    (tokens, heads, _), _ = _layout(x, "x")
+    _layout(y, "y", heads, tokens)
+    _distinct(y, "y")
+    if rot.keep is None:
+        raise ValueError("rope needs frequencies")
+    p = ebd_rope_params()
+    p.num_tokens, p.num_heads, p.head_dim = tokens, heads, HEAD_DIM
+    p.x, p.y = _rows_of(x), _rows_of(y)
+    p.pos = _table(pos, torch.int32, (tokens,), "pos")
+    p.rot = rot
+    return _plan(p, _here(x, y, pos, rot.keep), (pos, rot.keep), x=x, y=y)
+
+
+def pages(K, V, page_table) -> ebd_pages:
+    """The pools K and V [pages, KV heads, rows per page, 128] (any strides over the first three, the same
+    for both) and page_table [sequences, pages per sequence] int32."""
+    for t, name in ((K, "K"), (V, "V")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if t.dtype != _BF:
+            raise TypeError("%s must be %s, got %s" % (name, _BF, t.dtype))
+        if t.dim() != 4 or t.shape[3] != HEAD_DIM or t.stride(3) != 1:
+            raise ValueError("%s must be [pages, KV heads, rows, %d] with contiguous rows" % (name, HEAD_DIM))
+    if K.shape != V.shape or K.stride() != V.stride():
+        raise ValueError("K and V must have the same shape and strides")
+    _distinct(K, "K")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [sequences, pages per sequence]")
+    P = ebd_pages()
+    P.num_pages, P.kv_heads, P.page_size, P.head_dim = *K.shape[:3], HEAD_DIM
+    P.num_seqs, P.max_pages = page_table.shape
+    P.page_table = _ptr(page_table, torch.int32, "page_table")
+    # strides over one page, head or row are never used, and may be anything
+    P.page_stride, P.head_stride, P.row_stride = (s if n > 1 else HEAD_DIM
+                                                  for n, s in zip(K.shape[:3], K.stride()[:3]))
+    P.pools, P.keep = (K, V), page_table
+    return P
+
+
+def append_paged_params(pgs: ebd_pages, k_new, v_new, new_off, len, rot: Optional[ebd_rotary] = None,
+                        pos=None, q=None, q_out=None) -> ebd_append_paged_params:
+    """New tokens k_new, v_new [tokens, KV heads, 128] (and q -> q_out [tokens, query heads, 128]) of the
+    sequences new_off [sequences + 1] int64, which hold len [sequences] int32 rows with them.  rot None:
+    nothing is rotated; pos [tokens] int32 None: a token's position is its row."""
+    (tokens, _, _), _ = _layout(k_new, "k_new", pgs.kv_heads)
+    _layout(v_new, "v_new", pgs.kv_heads, tokens)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    p = ebd_append_paged_params()
+    p.pages, p.num_tokens = pgs, tokens
+    p.new_off = _table(new_off, torch.int64, (pgs.num_seqs + 1,), "new_off")
+    p.len = _table(len, torch.int32, (pgs.num_seqs,), "len")
+    p.pos = _table(pos, torch.int32, (tokens,), "pos")
+    freq = None
+    if rot is not None:
+        p.rot, freq = rot, rot.keep
+    p.k_rows, p.v_rows = _rows_of(k_new), _rows_of(v_new)
+    if q is not None:
+        (_, heads, _), _ = _layout(q, "q", None, tokens)
+        _layout(q_out, "q_out", heads, tokens)
+        _distinct(q_out, "q_out")
+        p.q_heads, p.q_rows, p.q_out_rows = heads, _rows_of(q), _rows_of(q_out)
+    K, V = pgs.pools
+    dev = _here(K, V, pgs.keep, k_new, v_new, new_off, len, pos, freq, q, q_out)
+    return _plan(p, dev, (pgs.keep, new_off, len, pos, freq), K=K, V=V, k_new=k_new, v_new=v_new, q=q, q_out=q_out)
+
+
+def attend_paged_params(pgs: ebd_pages, q, y, new_off, len, max_new: int, max_rows: int, qpos=None,
+                        window: int = 0, scale: float = 0.0) -> ebd_attend_paged_params:
+    """Queries q -> y [tokens, query heads, 128] of the sequences new_off [sequences + 1] int64 (at most
+    max_new tokens each), which hold len [sequences] int32 rows (at most max_rows)."""
+    (tokens, heads, _), _ = _layout(q, "q")
+    _layout(y, "y", heads, tokens)
+    _distinct(y, "y")
+    if heads < 1 or heads % pgs.kv_heads:
+        raise ValueError("query heads (%d) must be a multiple of the KV heads (%d)" % (heads, pgs.kv_heads))
+    p = ebd_attend_paged_params()
+    p.pages, p.num_tokens, p.group = pgs, tokens, heads // pgs.kv_heads
+    p.max_new, p.max_rows = int(max_new), int(max_rows)
+    p.new_off = _table(new_off, torch.int64, (pgs.num_seqs + 1,), "new_off")
+    p.len = _table(len, torch.int32, (pgs.num_seqs,), "len")
+    p.qpos = _table(qpos, torch.int32, (tokens,), "qpos")
+    p.window, p.scale = int(window), float(scale)
+    p.q_rows, p.y_rows = _rows_of(q), _rows_of(y)
+    K, V = pgs.pools
+    return _plan(p, _here(K, V, pgs.keep, q, y, new_off, len, qpos), (pgs.keep, new_off, len, qpos),
+                 K=K, V=V, q=q, y=y)
+
+
+def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_paged_params:
+    """Units seq_off [sequences * KV heads + 1] int64, the longest at most max_rows."""
+    p = ebd_gather_paged_params()
+    p.pages, p.max_rows = pgs, int(max_rows)
+    p.seq_off = _table(seq_off, torch.int64, (pgs.num_seqs * pgs.kv_heads + 1,), "seq_off")
+    K, V = pgs.pools
+    return _plan(p, _here(K, V, pgs.keep, seq_off), (pgs.keep, seq_off), K=K, V=V)
+
+
+# ---- the calls ---------------------------------------------------------------------------------
+
+def ebd_rope(params: ebd_rope_params, x, y, stream=None) -> None:
+    """Rotate rows x into y (asynchronous on the current stream)."""
+    code = _lib.ebd_rope(ctypes.byref(params), _arg(params, "x", x), _arg(params, "y", y),
+                         _launch_stream(params, stream))
+    _check("ebd_rope", code)
+
+
+def ebd_append_paged(params: ebd_append_paged_params, k_new, v_new, K, V, q=None, q_out=None, status=None,
+                     stream=None) -> None:
+    """Write new tokens into their pages, and rotate their queries (asynchronous)."""
+    code = _lib.ebd_append_paged(ctypes.byref(params), _arg(params, "k_new", k_new), _arg(params, "v_new", v_new),
+                                 _arg(params, "K", K), _arg(params, "V", V), _arg(params, "q", q),
+                                 _arg(params, "q_out", q_out), _status(params, status, params.pages.num_seqs),
+                                 _launch_stream(params, stream))
+    _check("ebd_append_paged", code)
+
+
+def ebd_attend_paged(params: ebd_attend_paged_params, q, K, V, y, workspace, lse=None, status=None,
+                     stream=None) -> None:
+    """Attention of the new tokens over the paged cache (asynchronous)."""
+    if lse is not None:
+        heads = params.pages.kv_heads * params.group
+        lse_p = _table(lse, torch.float32, (params.num_tokens, heads), "lse")
+    if workspace.device != params.device or (lse is not None and lse.device != params.device):
+        raise ValueError("workspace and lse must be on %s" % params.device)
+    code = _lib.ebd_attend_paged(ctypes.byref(params), _arg(params, "q", q), _arg(params, "K", K),
+                                 _arg(params, "V", V), _arg(params, "y", y), lse_p if lse is not None else None,
+                                 _status(params, status, params.pages.num_seqs), _ptr(workspace, None, "workspace"),
+                                 workspace.numel() * workspace.element_size(), _launch_stream(params, stream))
+    _check("ebd_attend_paged", code)
+
+
+def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None, stream=None) -> None:
+    """Read the pages out as units Ku, Vu [rows, 128] (asynchronous)."""
+    units = params.pages.num_seqs * params.pages.kv_heads
+    if Ku.device != params.device or Vu.device != params.device:
+        raise ValueError("Ku and Vu must be on %s" % params.device)
+    code = _lib.ebd_gather_paged(ctypes.byref(params), _arg(params, "K", K), _arg(params, "V", V),
+                                 _ptr(Ku, _BF, "Ku"), _ptr(Vu, _BF, "Vu"), _status(params, status, units),
+                                 _launch_stream(params, stream))
+    _check("ebd_gather_paged", code)

@@ -1,0 +1,510 @@
+"""The paged-cache operators on the GPU, against their plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import paged_ref as ref
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+INF = float("inf")
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _freq(rot, base=5e5):
+    i = torch.arange(rot // 2, dtype=torch.float64, device="cuda")
+    return base ** (-2.0 * i / rot)
+
+
+def _say(*a):
+    print(*a, flush=True)
+
+
+# ---- rope --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens,heads,rot,layout,fused", [
+    (1, 1, 128, 0, False), (1, 32, 128, 1, True), (7, 3, 64, 0, True), (130, 33, 96, 0, False),
+    (5, 8, 2, 0, False), (5, 9, 2, 1, False), (64, 16, 34, 0, True), (33, 17, 34, 1, True),
+    (9, 28, 126, 0, False), (3, 70, 112, 1, True), (0, 4, 128, 0, False), (1025, 5, 128, 0, False),
+])
+def test_rope(tokens, heads, rot, layout, fused):
+    import paper_2607_21475_amd as ebd
+
+    _say("rope", tokens, heads, rot, layout, fused)
+    g = _gen(tokens + heads + rot)
+    x = ref.spaced((tokens, heads, 128), g, fused)
+    pos = torch.randint(-1000, 1 << 20, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    if tokens > 2:
+        pos[0], pos[1] = 0, 2 ** 31 - 1
+    f = _freq(rot)
+    for amp, inverse in ((1.0, False), (1.3, True)):
+        r = ebd.rotary(f, layout, amp, inverse)
+        want = ref.rotate(x, pos, f, amp, layout, inverse)
+        tol = ref.rotate_tolerance(x, want, f, amp, layout)
+        y = ref.spaced((tokens, heads, 128), g, not fused)
+        ebd.ebd_rope(ebd.rope_params(x, y, pos, r), x, y)
+        ref.check(y, want, tol, "rope")
+        z = x.clone() if not fused else torch.cat([x, x, x], 1)[:, heads:2 * heads]
+        ebd.ebd_rope(ebd.rope_params(z, z, pos, r), z, z)  # in place
+        assert torch.equal(z, y)
+
+
+def test_rope_inverse_is_the_gradient():
+    """The rotation is linear: its transpose, which the backward pass applies, is the inverse rotation."""
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(3)
+    x, dy = ref.spaced((5, 4, 128), g, False), ref.spaced((5, 4, 128), g, False)
+    pos = torch.arange(5, device="cuda", dtype=torch.int32) * 977
+    f = _freq(96)
+    leaf = x.double().requires_grad_()
+    (ref.rotate(leaf, pos, f, 0.7, 1) * dy.double()).sum().backward()
+    dx = torch.empty_like(x)
+    ebd.ebd_rope(ebd.rope_params(dy, dx, pos, ebd.rotary(f, 1, 0.7, inverse=True)), dy, dx)
+    ref.check(dx, leaf.grad, ref.rotate_tolerance(dy, leaf.grad, f, 0.7, 1), "gradient")
+
+
+def test_rope_leaves_the_rows_around_it():
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(4)
+    x = ref.spaced((6, 4, 128), g, True)
+    whole = torch.full((6, 12, 128), 7.0, dtype=BF, device="cuda")
+    y = whole[:, 4:8]
+    pos = torch.arange(6, device="cuda", dtype=torch.int32)
+    ebd.ebd_rope(ebd.rope_params(x, y, pos, ebd.rotary(_freq(128))), x, y)
+    assert bool((whole[:, :4] == 7).all()) and bool((whole[:, 8:] == 7).all())
+
+
+# ---- append ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens,news,kv,heads,page,order,rot,layout,fused,given", [
+    ([1], [1], 8, 32, 16, "heads", 128, 0, True, False),
+    ([40, 7, 300, 16], [40, 0, 33, 16], 4, 28, 32, "tokens", 128, 0, True, False),
+    ([5, 1000, 64], [1, 1, 1], 1, 1, 16, "heads", 64, 1, False, True),
+    ([130, 129], [130, 65], 2, 6, 64, "tokens", 34, 0, False, True),
+    ([33, 0, 12], [33, 0, 3], 3, 0, 256, "heads", 128, 1, True, False),
+    ([70, 2], [9, 2], 5, 7, 16, "heads", 0, 0, False, False),
+] + [([17 + s % 5 for s in range(150)], [s % 4 for s in range(150)], 2, 4, 16, "heads", 128, 0, False, False)])
+def test_append(lens, news, kv, heads, page, order, rot, layout, fused, given):
+    import paper_2607_21475_amd as ebd
+
+    _say("append", lens[:4], news[:4], kv, heads, page, order, rot, layout)
+    g = _gen(sum(lens) + page)
+    c = ref.Cache(lens, kv, page, g, order)
+    pad = 3  # tokens behind the last sequence
+    T = sum(news) + pad
+    k, v = ref.spaced((T, kv, 128), g, fused), ref.spaced((T, kv, 128), g, fused)
+    q = ref.spaced((T, heads, 128), g, fused) if heads else None
+    out = torch.full((T, heads, 128), 7.0, dtype=BF, device="cuda") if heads else None
+    off = torch.tensor([0] + [sum(news[:i + 1]) for i in range(len(news))], device="cuda")
+    row = torch.tensor([n - m + j for n, m in zip(lens, news) for j in range(m)] + [0] * pad, device="cuda")
+    pos = (row * 3 + 100000).to(torch.int32) if given else None
+    f = _freq(rot) if rot else None
+    r = ebd.rotary(f, layout, 1.25) if rot else None
+    K0, V0 = c.K.clone(), c.V.clone()
+    st = torch.zeros(len(lens), dtype=torch.int32, device="cuda")
+    p = ebd.append_paged_params(ebd.pages(c.K, c.V, c.table), k, v, off, c.len, r, pos=pos, q=q, q_out=out)
+    ebd.ebd_append_paged(p, k, v, c.K, c.V, q, out, status=st)
+    assert not bool(st.any())
+    at = pos if given else row
+    turn = (lambda x: ref.rotate(x, at, f, 1.25, layout)) if rot else (lambda x: x.double())
+    tol = (lambda x, y: ref.rotate_tolerance(x, y, f, 1.25, layout)) if rot else (lambda x, y: torch.zeros_like(y))
+    K1, V1, kr = K0.double(), V0.clone(), turn(k)
+    tk, kt = torch.zeros_like(K1), tol(k, turn(k))
+    t = 0
+    for s, (n, m) in enumerate(zip(lens, news)):
+        for i in range(n - m, n):
+            pg = int(c.table[s, i // page])
+            K1[pg, :, i % page], tk[pg, :, i % page], V1[pg, :, i % page] = kr[t], kt[t], v[t]
+            t += 1
+    ref.check(c.K, K1, tk, "K")
+    assert torch.equal(c.V, V1)
+    if heads:
+        want = turn(q)
+        ref.check(out[:t], want[:t], tol(q, want)[:t], "q")
+        assert bool((out[t:] == 7).all())
+
+
+def test_append_rows_without_a_page():
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(9)
+    c = ref.Cache([40, 40, 40, 40], 2, 16, g)
+    c.table[0, 2] = -1
+    c.table[1, 2] = c.K.shape[0]
+    c.len[2] = 16 * c.table.shape[1] + 2  # two rows past the table
+    c.len[3] = 2                          # fewer rows than new tokens
+    off = torch.tensor([0, 4, 8, 12, 16], device="cuda")
+    k, v = ref.spaced((16, 2, 128), g, False), ref.spaced((16, 2, 128), g, False)
+    st = torch.full((4,), 64, dtype=torch.int32, device="cuda")
+    K0, V0 = c.K.clone(), c.V.clone()
+    q, out = ref.spaced((16, 3, 128), g, False), torch.zeros((16, 3, 128), dtype=BF, device="cuda")
+    c.table[2, 3] = 0
+    p = ebd.append_paged_params(ebd.pages(c.K, c.V, c.table), k, v, off, c.len, None, q=q, q_out=out)
+    ebd.ebd_append_paged(p, k, v, c.K, c.V, q, out, status=st)
+    assert st.tolist() == [96, 96, 96, 96]
+    # rows 62, 63 of sequence 2 and 0, 1 of sequence 3 have pages
+    for x, new in ((K0, k), (V0, v)):
+        x[0, :, 14], x[0, :, 15] = new[8], new[9]
+        pg = int(c.table[3, 0])
+        x[pg, :, 0], x[pg, :, 1] = new[14], new[15]
+    assert torch.equal(c.K, K0) and torch.equal(c.V, V0) and torch.equal(out, q)
+
+
+# ---- gather ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens,kv,page,order", [
+    ([1], 8, 16, "heads"), ([100, 0, 65, 64], 3, 32, "tokens"), ([4097, 3], 2, 64, "heads"),
+    ([300], 1, 1024, "tokens"),
+])
+def test_gather(lens, kv, page, order):
+    import paper_2607_21475_amd as ebd
+
+    _say("gather", lens, kv, page, order)
+    c = ref.Cache(lens, kv, page, _gen(5), order, fill=math.nan)
+    off = [0]
+    for n in lens:
+        off += [off[-1] + n * (i + 1) for i in range(kv)]
+    so = torch.tensor(off, device="cuda")
+    Ku = torch.full((off[-1] + 2, 128), 7.0, dtype=BF, device="cuda")
+    Vu = Ku.clone()
+    st = torch.zeros(len(lens) * kv, dtype=torch.int32, device="cuda")
+    p = ebd.gather_paged_params(ebd.pages(c.K, c.V, c.table), so, max(lens))
+    ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu, status=st)
+    assert not bool(st.any())
+    for out, pool in ((Ku, c.K), (Vu, c.V)):
+        want = torch.cat([c.rows(pool, s, h) for s in range(len(lens)) for h in range(kv)])
+        assert torch.equal(out[:-2], want) and bool((out[-2:] == 7).all())
+
+
+def test_gather_bad_pages_and_long_units():
+    import paper_2607_21475_amd as ebd
+
+    c = ref.Cache([100, 50], 2, 16, _gen(6))
+    c.table[0, 3] = 1 << 20
+    so = torch.tensor([0, 100, 200, 250, 300], device="cuda")
+    Ku = torch.full((300, 128), 7.0, dtype=BF, device="cuda")
+    Vu = Ku.clone()
+    st = torch.zeros(4, dtype=torch.int32, device="cuda")
+    p = ebd.gather_paged_params(ebd.pages(c.K, c.V, c.table), so, 70)
+    ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu, status=st)
+    both = ebd.EBD_ST_BAD_PAGE | ebd.EBD_ST_BAD_LAYOUT
+    assert st.tolist() == [both, both, 0, 0]
+    for h in range(2):
+        u = Ku[100 * h:100 * h + 100]
+        c.table[0, 3] = 0
+        want = c.rows(c.K, 0, h).clone()
+        want[48:64] = 0
+        assert torch.equal(u[:70], want[:70]) and bool((u[70:] == 7).all())
+        assert torch.equal(Vu[200 + 50 * h:250 + 50 * h], c.rows(c.V, 1, h))
+
+
+# ---- attend ------------------------------------------------------------------------------------
+
+def _attend(c, news, G, q=None, seed=0, fused=False, hi=None, window=0, scale=0.0, max_new=None, max_rows=None,
+            pad=0, lens=None, want_lse=True):
+    import paper_2607_21475_amd as ebd
+
+    T = sum(news) + pad
+    if q is None:
+        q = ref.spaced((T, c.kv * G, 128), _gen(seed + 1), fused)
+    y = torch.full((T, c.kv * G, 128), 7.0, dtype=BF, device="cuda")
+    lse = torch.full((T, c.kv * G), 7.0, dtype=torch.float32, device="cuda")
+    off = torch.tensor([0] + [sum(news[:i + 1]) for i in range(len(news))], device="cuda")
+    st = torch.zeros(len(news), dtype=torch.int32, device="cuda")
+    p = ebd.attend_paged_params(ebd.pages(c.K, c.V, c.table), q, y, off, c.len,
+                                max(news) if max_new is None else max_new,
+                                max(c.lens) if max_rows is None else max_rows, qpos=hi, window=window, scale=scale)
+    ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, p))
+    ws.fill_(255)
+    ebd.ebd_attend_paged(p, q, c.K, c.V, y, ws, lse=lse if want_lse else None, status=st)
+    return q, y, lse, st
+
+
+# weights are stored with at least this many bits (half a step of bf16 relative: 2^-8)
+BITS = 8
+
+
+@pytest.mark.parametrize("lens,news,kv,G,page,order,window", [
+    ([1], [1], 1, 1, 16, "heads", 0),
+    ([1, 31, 32, 33], [1, 1, 1, 1], 8, 4, 16, "heads", 0),
+    ([4096], [1], 8, 1, 16, "heads", 0),
+    ([5000, 17, 1], [1, 1, 1], 2, 7, 64, "tokens", 0),
+    ([700, 20, 64, 9], [8, 3, 1, 0], 4, 7, 32, "tokens", 0),
+    ([130, 64], [130, 7], 2, 3, 16, "heads", 0),
+    ([257], [257], 1, 8, 128, "heads", 0),
+    ([600, 511, 90], [300, 1, 90], 2, 4, 64, "tokens", 100),
+    ([1000, 40], [1, 1], 2, 16, 256, "heads", 33),
+    ([300], [64], 1, 17, 16, "heads", 1),
+    ([2049, 33], [513, 33], 1, 2, 64, "heads", 700),
+    ([64, 0, 5], [64, 0, 5], 2, 1, 16, "heads", 0),
+])
+def test_attend(lens, news, kv, G, page, order, window):
+    _say("attend", lens, news, kv, G, page, order, window)
+    c = ref.Cache(lens, kv, page, _gen(sum(lens)), order, fill=math.nan)
+    q, y, lse, st = _attend(c, news, G, fused=len(lens) % 2 == 1, window=window, pad=2)
+    assert not bool(st.any())
+    ry, rl, ty, tl = ref.attend(c, q[:-2], news, window=window, weights_bits=BITS)
+    ref.check(y[:-2], ry, ty, "y")
+    ref.check(lse[:-2], rl, tl, "lse")
+    assert bool((y[-2:] == 7).all()) and bool((lse[-2:] == 7).all())
+
+
+@pytest.mark.parametrize("news", [[1, 1, 1], [8, 2, 7], [70, 33, 129]])
+def test_attend_query_positions(news):
+    """Positions in any order, padding that sees nothing, positions past the cache; no lse asked for."""
+    _say("attend qpos", news)
+    lens = [200, 33, 129]
+    c = ref.Cache(lens, 2, 16, _gen(8), fill=INF)
+    T = sum(news)
+    hi = torch.randint(-30, 260, (T,), generator=_gen(4), device="cuda", dtype=torch.int32)
+    hi[0], hi[T - 1] = -1, -(1 << 31)
+    for window in (0, 20):
+        q, y, lse, st = _attend(c, news, 4, hi=hi, window=window)
+        ry, rl, ty, tl = ref.attend(c, q, news, hi=hi, window=window, weights_bits=BITS)
+        assert bool((rl == -INF).any())
+        ref.check(y, ry, ty, "y")
+        ref.check(lse, rl, tl, "lse")
+    assert torch.equal(_attend(c, news, 4, hi=hi, window=window, want_lse=False)[1], y)
+    hi.fill_(-1)
+    _, y, lse, _ = _attend(c, news, 4, hi=hi)
+    assert not bool(y.any()) and bool((lse == -INF).all())
+
+
+@pytest.mark.parametrize("what", [math.nan, INF, -INF])
+@pytest.mark.parametrize("news,G", [([4], 2), ([16], 1), ([100], 4), ([300], 1)])
+def test_attend_unseen_rows_have_no_effect(news, G, what):
+    """Keys and values of rows that some query rows see and others do not hold infinities and NaN."""
+    _say("attend unseen", news, G, what)
+    n, m = 400, news[0]
+    c = ref.Cache([n], 2, 16, _gen(8))
+    at = n - m + m // 2
+    pg, slot = int(c.table[0, at // 16]), at % 16
+    clean = _attend(c, news, G)
+    for pools in ((c.V,), (c.K, c.V)):
+        K0, V0 = c.K.clone(), c.V.clone()
+        for x in pools:
+            x[pg, :, slot, ::3] = what
+        q, y, lse, _ = _attend(c, news, G)
+        c.K.copy_(K0), c.V.copy_(V0)
+        # tokens before it: nothing changed (their sums may be taken in another way: compare with the formula)
+        ry, rl, ty, tl = ref.attend(c, q, news, weights_bits=BITS)
+        j = m // 2
+        ref.check(y[:j], ry[:j], ty[:j], "y")
+        assert torch.equal(lse[:j], clean[2][:j])
+        assert not bool(torch.isfinite(y[j:].float()).all(-1).any())
+
+
+def test_attend_rows_without_a_page():
+    for m in (1, 60):
+        c = ref.Cache([200, 90], 2, 32, _gen(8), fill=math.nan)
+        c.table[0, 2], c.table[0, 5] = -1, 10 ** 6
+        gone = torch.zeros(200, dtype=torch.bool, device="cuda")
+        gone[64:96] = gone[160:192] = True
+        q, y, lse, st = _attend(c, [m, m], 3)
+        c.table[0, 2] = c.table[0, 5] = 0
+        import paper_2607_21475_amd as ebd
+        assert st.tolist() == [ebd.EBD_ST_BAD_PAGE, 0]
+        ry, rl, ty, tl = ref.attend(c, q, [m, m], weights_bits=BITS,
+                                    seen=lambda s: ~gone if s == 0 else torch.ones(90, dtype=torch.bool, device="cuda"))
+        ref.check(y, ry, ty, "y")
+        ref.check(lse, rl, tl, "lse")
+    c.table[0] = -1
+    _, y, lse, st = _attend(c, [m, m], 3)
+    assert not bool(y[:m].any()) and bool((lse[:m] == -INF).all())
+    # a sequence longer than its table: its rows there are seen
+    c = ref.Cache([64], 1, 16, _gen(8))
+    c.len[0] = 16 * c.table.shape[1] + 5
+    c.table[0, -1] = 0
+    _, _, _, st = _attend(c, [1], 1, max_rows=1000)
+    assert st.tolist() == [ebd.EBD_ST_BAD_PAGE]
+
+
+@pytest.mark.parametrize("news", [[3, 5], [60, 90]])
+def test_attend_beyond_the_bounds(news):
+    """Sequences with more rows or new tokens than the host said: flagged, the rest as asked."""
+    import paper_2607_21475_amd as ebd
+
+    c = ref.Cache([300, 100], 2, 16, _gen(8))
+    q, y, lse, st = _attend(c, news, 2, max_new=news[0], max_rows=150)
+    assert st.tolist() == [ebd.EBD_ST_BAD_LAYOUT] * 2
+    t = news[0]
+    assert bool((y[2 * t:] == 7).all()) and bool((lse[2 * t:] == 7).all())
+    full = [torch.ones(300, dtype=torch.bool, device="cuda"), torch.ones(100, dtype=torch.bool, device="cuda")]
+    full[0][150:] = False
+    ry, rl, ty, tl = ref.attend(c, q, news, weights_bits=BITS, seen=lambda s: full[s])
+    ref.check(y[:2 * t], ry[:2 * t], ty[:2 * t], "y")
+    ref.check(lse[:2 * t], rl[:2 * t], tl[:2 * t], "lse")
+
+
+@pytest.mark.parametrize("news", [[1], [2], [40], [200]])
+def test_attend_sharp_and_flat_rows(news):
+    """Logits of hundreds (one row takes all), a scale that makes them all alike, rows growing along the cache."""
+    g = _gen(8)
+    c = ref.Cache([900], 1, 64, g)
+    q = ref.spaced((news[0], 4, 128), g, False, scale=8.0)
+    for scale in (0.0, 1e-6, 2.0):
+        _, y, lse, _ = _attend(c, news, 4, q=q, scale=scale)
+        ry, rl, ty, tl = ref.attend(c, q, news, scale=scale or None, weights_bits=BITS)
+        ref.check(y, ry, ty, "y")
+        ref.check(lse, rl, tl, "lse")
+    for r in range(900):
+        c.K[int(c.table[0, r // 64]), 0, r % 64] = (q[0, 0].float() * (r / 900)).to(BF)
+    _, y, lse, _ = _attend(c, news, 4, q=q)
+    ry, rl, ty, tl = ref.attend(c, q, news, weights_bits=BITS)
+    ref.check(y, ry, ty, "y")
+    ref.check(lse, rl, tl, "lse")
+
+
+def test_offsets_past_32_bits():
+    """A pool whose pages lie more than 2^32 elements apart, rows of 5 GB in all."""
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(1)
+    big = torch.empty(5 * (1 << 30), dtype=BF, device="cuda")
+    stride = (1 << 30) + 8
+    small = ref.Cache([70, 50], 2, 16, g, spare=0)  # 9 pages
+    shape, st = small.K.shape, small.K.stride()
+    half = 4096 * 16
+    K = torch.as_strided(big, (5, *shape[1:]), (stride, *st[1:]))
+    V = torch.as_strided(big[half:], (5, *shape[1:]), (stride, *st[1:]))
+    table = torch.tensor([[4, 3, 2, 1, 0]], dtype=torch.int32, device="cuda")
+    k, v = ref.spaced((80, 2, 128), g, False), ref.spaced((80, 2, 128), g, False)
+    off, ln = torch.tensor([0, 80], device="cuda"), torch.tensor([80], dtype=torch.int32, device="cuda")
+    P = ebd.pages(K, V, table)
+    ebd.ebd_append_paged(ebd.append_paged_params(P, k, v, off, ln), k, v, K, V)
+    for i in range(5):
+        assert torch.equal(K[4 - i], k[16 * i:16 * i + 16].transpose(0, 1))
+        assert torch.equal(V[4 - i], v[16 * i:16 * i + 16].transpose(0, 1))
+    so = torch.tensor([0, 80, 160], device="cuda")
+    Ku, Vu = torch.empty((160, 128), dtype=BF, device="cuda"), torch.empty((160, 128), dtype=BF, device="cuda")
+    ebd.ebd_gather_paged(ebd.gather_paged_params(P, so, 80), K, V, Ku, Vu)
+    assert torch.equal(Ku.view(2, 80, 128), k.transpose(0, 1)) and torch.equal(Vu.view(2, 80, 128), v.transpose(0, 1))
+    c = ref.Cache([80], 2, 16, g, spare=0)
+    c.K, c.V, c.table, c.len = K, V, torch.cat([table, table[:, :1]], 1), ln
+    for m in (1, 80):
+        q, y, lse, _ = _attend(c, [m], 4)
+        ry, rl, ty, tl = ref.attend(c, q, [m], weights_bits=BITS)
+        ref.check(y, ry, ty, "y")
+
+
+def test_two_streams_and_a_graph():
+    """Calls on two side streams at once, and a captured step replayed with the program's own work between."""
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(2)
+    lens, news, G = [900, 333], [1, 1], 4
+    c = ref.Cache(lens, 2, 16, g)
+    off = torch.tensor([0, 1, 2], device="cuda")
+    P = ebd.pages(c.K, c.V, c.table)
+    k, v, q = (ref.spaced((2, h, 128), g, False) for h in (2, 2, 8))
+    qr, y = torch.empty_like(q), torch.empty_like(q)
+    lse = torch.empty((2, 8), device="cuda")
+    ap = ebd.append_paged_params(P, k, v, off, c.len, ebd.rotary(_freq(128)), q=q, q_out=qr)
+    at = ebd.attend_paged_params(P, qr, y, off, c.len, 1, 1024)
+    ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, at))
+
+    def step():
+        ebd.ebd_append_paged(ap, k, v, c.K, c.V, q, qr)
+        ebd.ebd_attend_paged(at, qr, c.K, c.V, y, ws, lse=lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        for x in (k, v, q):
+            x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+        c.len += 1
+        y.fill_(7)
+        ws.fill_(255)
+        graph.replay()
+        got = y.clone(), lse.clone(), c.K.clone()
+        torch.cuda.synchronize()
+        y.fill_(7)
+        step()
+        assert torch.equal(got[0], y) and torch.equal(got[1], lse) and torch.equal(got[2], c.K)
+        c.lens = c.len.tolist()
+        # the last step's second sequence has outgrown its pages: that row is nowhere
+        held = lambda s: c.table[s].repeat_interleave(c.page)[:c.lens[s]] >= 0  # noqa: E731
+        ry, rl, ty, tl = ref.attend(c, qr, news, weights_bits=BITS, seen=held)
+        ref.check(y, ry, ty, "y")
+    # two streams, each with outputs and a workspace of its own
+    outs = [(torch.empty_like(y), ebd.workspace(ws.numel()), torch.cuda.Stream()) for _ in range(2)]
+    torch.cuda.synchronize()
+    for o, w, s in outs * 5:
+        with torch.cuda.stream(s):
+            ebd.ebd_attend_paged(at, qr, c.K, c.V, o, w)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, y) for o, _, _ in outs)
+
+
+def test_the_path_from_a_prompt_to_certified_decoding():
+    """Chunks appended and attended, the pages read out, scored and evicted, then a certified step over the
+    retained rows: what the same rows give without pages."""
+    import paper_2607_21475_amd as ebd
+    from paper_2607_21475_amd import cache as ec
+
+    g = _gen(7)
+    lens, kv, G, page = [700, 411], 2, 4, 16
+    c = ref.Cache(lens, kv, page, g, fill=math.nan)
+    f = _freq(128)
+    rot = ebd.rotary(f)
+    P = ebd.pages(c.K, c.V, c.table)
+    ks = [ref.spaced((n, kv, 128), g, False) for n in lens]
+    vs = [ref.spaced((n, kv, 128), g, False) for n in lens]
+    qs = [ref.spaced((n, kv * G, 128), g, False) for n in lens]
+    done = [0, 0]
+    while done != lens:
+        new = [min(256, n - d) for n, d in zip(lens, done)]
+        cut = lambda xs: torch.cat([x[d:d + m] for x, d, m in zip(xs, done, new)])  # noqa: E731,B023
+        k, v, q = cut(ks), cut(vs), cut(qs)
+        done = [d + m for d, m in zip(done, new)]
+        c.len.copy_(torch.tensor(done))
+        c.lens = done
+        off = torch.tensor([0, new[0], sum(new)], device="cuda")
+        qr = torch.empty_like(q)
+        ebd.ebd_append_paged(ebd.append_paged_params(P, k, v, off, c.len, rot, q=q, q_out=qr), k, v, c.K, c.V, q, qr)
+        y = torch.empty_like(q)
+        at = ebd.attend_paged_params(P, qr, y, off, c.len, max(new), max(done))
+        ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, at))
+        ebd.ebd_attend_paged(at, qr, c.K, c.V, y, ws)
+        ry, rl, ty, tl = ref.attend(c, qr, new, weights_bits=BITS)
+        ref.check(y, ry, ty, "y")
+    sizes = [n for n in lens for _ in range(kv)]
+    so = torch.tensor([0, 700, 1400, 1811, 2222], device="cuda")
+    Ku, Vu = torch.empty((2222, 128), dtype=BF, device="cuda"), torch.empty((2222, 128), dtype=BF, device="cuda")
+    ebd.ebd_gather_paged(ebd.gather_paged_params(P, so, 700), c.K, c.V, Ku, Vu)
+    turned = torch.cat([ref.rotate(k, torch.arange(n, device="cuda"), f)[:, h] for k, n in zip(ks, lens) for h in range(kv)])
+    ref.check(Ku, turned, ref.rotate_tolerance(torch.cat([k[:, h] for k in ks for h in range(kv)])[:, None],
+                                               turned[:, None], f)[:, 0], "K")
+    # the certified step over everything retained is the paged decode step
+    qd = ref.spaced((2, kv * G, 128), g, False)
+    so_q = qd.view(2 * kv, G, 128)
+    sc, _ = ec.importance_scores(Ku, so, so_q, 700)
+    out = ec.evict(Ku, Vu, sc, so, sizes, budget_frac=1.0, n_sink=4, n_recent=64)
+    res = ec.attend_certify(out, so_q)
+    assert out.count.tolist() == sizes
+    y = torch.empty_like(qd)
+    lse = torch.empty((2, kv * G), device="cuda")
+    off = torch.tensor([0, 1, 2], device="cuda")
+    at = ebd.attend_paged_params(P, qd, y, off, c.len, 1, 700)
+    ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, at))
+    ebd.ebd_attend_paged(at, qd, c.K, c.V, y, ws, lse=lse)
+    ry, rl, ty, tl = ref.attend(c, qd, [1, 1], weights_bits=BITS)
+    ref.check(y, ry, ty, "y")
+    ref.check(lse, rl, tl, "lse")
+    ref.check(res["y"].view(2, kv * G, 128).to(BF), ry, 2 * ty, "certified y")
+    ref.check(res["lse"].view(2, kv * G), rl, 2 * tl, "certified lse")
