@@ -21,7 +21,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libebd.so")
 
 SOURCES = ["evict.hip", "evict_long.hip", "attend.hip", "append.hip", "scores.hip", "finegrain.hip", "noalloc.hip",
-           "rope.hip", "gather_paged.hip", "attend_paged.hip", "ebd_api.cpp", "paged_api.cpp"]
+           "rope.hip", "gather_paged.hip", "attend_paged.hip",
+           "attend_paged_tiles.hip", "ebd_api.cpp", "paged_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 # Packed fp32 ops are disabled in every kernel (some of their forms have been unreliable).

@@ -1,0 +1,116 @@
+// attend_paged.hpp -- what the kernels of the paged attention share: a launch's sequences and the rows their
+// queries see, loads that write LDS directly, transposing LDS reads, and the finished rows' store.
+#pragma once
+
+#include "ebd.h"
+#include "ebd_internal.hpp"
+#include "paged_device.hpp"
+
+namespace ebd {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(4))) int32_t const_i32;  // read through the scalar cache
+
+constexpr int kRowBytes = 2 * kHeadDim;
+
+__device__ __forceinline__ uint32_t lds_at(const void *p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8 *)(uint8_t *)p);
+}
+
+// 16 bytes per lane from base + off straight into LDS at `to` + 16 lane.  Written as assembly because the
+// compiler would wait for all of them before any read of LDS; it holds no result register, and the
+// waits below order it.
+__device__ __forceinline__ void load_lds16(uint32_t to, const uint8_t *base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ bf16x8 join8(s16x4 lo, s16x4 hi) {
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ s16x4 read_transposed(const uint8_t *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds_u8 *)p);
+}
+
+// A sequence's part of a launch.
+struct Seq {
+  int64_t t0;       // its first new token
+  int tokens;       // new tokens that get an output
+  int64_t first;    // row of its first new token
+  int64_t len;      // rows it holds
+  int64_t seen;     // ... of which the launch can see
+  uint32_t status;
+};
+__device__ __forceinline__ Seq sequence(const ebd_attend_paged_params &p, int s) {
+  Seq q;
+  q.t0 = p.new_off[s];
+  const int64_t n = p.new_off[s + 1] - q.t0;
+  q.len = p.len[s];
+  q.first = q.len - n;
+  q.status = (n > p.max_new || q.len > p.max_rows) ? EBD_ST_BAD_LAYOUT : 0u;
+  q.seen = min(q.len, p.max_rows);
+  const int64_t room = (int64_t)p.pages.max_pages * p.pages.page_size;
+  if (q.seen > room) {
+    q.status |= EBD_ST_BAD_PAGE;
+    q.seen = room;
+  }
+  q.tokens = (int)max((int64_t)0, min(min(n, (int64_t)p.max_new), p.num_tokens - q.t0));
+  if (q.t0 < 0) q.tokens = 0;
+  return q;
+}
+
+// The rows lo .. hi - 1 that query row `row` sees (lo >= hi: none).
+struct Span {
+  int lo, hi;
+};
+__device__ __forceinline__ Span span_of(const ebd_attend_paged_params &p, const Seq &q, int row) {
+  const int j = row / p.group;
+  if (j >= q.tokens) return {0, 0};
+  int64_t last = q.first + j;
+  if (p.qpos) last = min((int64_t)p.qpos[q.t0 + j], q.len - 1);
+  const int64_t lo = p.window > 0 ? max((int64_t)0, last - p.window + 1) : 0;
+  const int64_t hi = min(last + 1, q.seen);
+  return lo < hi ? Span{(int)lo, (int)hi} : Span{0, 0};
+}
+
+// The range a block of query rows sees (the same in every lane of a wave that holds them all), and
+// whether a tile needs masks: inside [every_lo, every_hi) every row that sees anything sees all.
+struct Range {
+  int lo, hi, every_lo, every_hi;
+};
+template <int N>
+__device__ __forceinline__ Range range_of(const Span (&s)[N]) {
+  int lo = INT32_MAX, hi = 0, elo = 0, ehi = INT32_MAX;
+#pragma unroll
+  for (int b = 0; b < N; ++b) {
+    if (s[b].lo >= s[b].hi) continue;
+    lo = min(lo, s[b].lo), hi = max(hi, s[b].hi);
+    elo = max(elo, s[b].lo), ehi = min(ehi, s[b].hi);
+  }
+  return {wave_min(lo), -wave_min(-hi), -wave_min(-elo), wave_min(ehi)};
+}
+
+// Elements e .. e+7 of a finished row: token t, query head hq, sums o over weights that total Z with the
+// maximum M (-inf: the row saw nothing).
+__device__ __forceinline__ void store_row(const AttendPagedLaunch &L, int64_t t, int hq, int e, float M, float Z,
+                                          const float (&o)[8]) {
+  const bool any = M != -INFINITY;
+  const float a = any ? 1.0f / Z : 0.0f;
+  uint4 v;
+  v.x = any ? pack_bf16(o[0] * a, o[1] * a) : 0u;
+  v.y = any ? pack_bf16(o[2] * a, o[3] * a) : 0u;
+  v.z = any ? pack_bf16(o[4] * a, o[5] * a) : 0u;
+  v.w = any ? pack_bf16(o[6] * a, o[7] * a) : 0u;
+  *reinterpret_cast<uint4 *>(L.y + t * L.p.y_rows.token_stride + hq * L.p.y_rows.head_stride + e) = v;
+  if (e == 0 && L.lse)
+    L.lse[t * ((int64_t)L.p.pages.kv_heads * L.p.group) + hq] = any ? (M + fast_log2(Z)) * kLn2 : -INFINITY;
+}
+
+}  // namespace ebd

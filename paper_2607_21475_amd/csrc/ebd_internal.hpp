@@ -204,7 +204,9 @@ struct AttendPagedLaunch {
   float2 *stats;       // [groups, rows] their maximum and total weight
 };
 
-constexpr int kRowsWaves = 4;  // waves of an attend_rows work-group
+constexpr int kRowsWaves = 4;      // waves of an attend_rows work-group
+constexpr int kRowsKernelMax = 64;  // query rows of a KV head up to which a launch takes attend_rows
+constexpr int kTileRows = 256;     // query rows of an attend_tiles work-group
 
 constexpr int64_t kMaxBlocks = 8192;  // blocks per unit of ebd_block_contributions (LDS bins)
 constexpr int kBlockWaves = 8;        // most waves of its work-groups
@@ -238,6 +240,7 @@ int64_t attend_paged_groups(const AttendPagedLaunch &L);
 size_t attend_paged_part_bytes(const AttendPagedLaunch &L);
 size_t attend_paged_workspace(const ebd_attend_paged_params *p);  // 0: invalid parameters
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s);
+hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s);
 hipError_t launch_attend_paged_join(const AttendPagedLaunch &L, hipStream_t s);
 
 hipError_t launch_evict_select(const EvictLaunch &L, hipStream_t s);

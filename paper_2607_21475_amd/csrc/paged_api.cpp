@@ -67,23 +67,25 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
 }
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split until there are
-// kRowsGroups work-groups; a split holds at least a tile for each wave.
-constexpr int64_t kRowsGroups = 256;
+// 256 work-groups, one a CU; a split holds at least a tile for each wave (attend_rows) or eight tiles.
+constexpr int64_t kGroups = 256;
 constexpr int64_t kRowsLeast = 128;
+constexpr int64_t kTilesLeast = 512;
 AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   AttendPagedLaunch L{};
   L.p = *p;
   const int64_t rows = (int64_t)p->max_new * p->group;
-  L.rows = rows <= 16 ? 16 : 32;
+  L.rows = rows <= 16 ? 16 : (rows <= kRowsKernelMax ? 32 : kTileRows);
+  const bool tiles = L.rows == kTileRows;
   L.blocks = (int32_t)std::max<int64_t>(1, (rows + L.rows - 1) / L.rows);
   // the most rows a block of query rows sees, from a tile's border on
   int64_t span = p->max_rows;
-  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows + 32);
-  span = std::max<int64_t>(span, 1) + 31;
+  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows / p->group + 1);
+  span = std::max<int64_t>(span, 1) + 63;
   const int64_t units = std::max<int64_t>(1, (int64_t)p->pages.num_seqs * p->pages.kv_heads * L.blocks);
-  int64_t ns = std::max<int64_t>(1, kRowsGroups / units);
-  ns = std::min<int64_t>(ns, std::max<int64_t>(1, span / kRowsLeast));
-  L.split_rows = (int32_t)std::min<int64_t>(((span + ns - 1) / ns + 127) / 128 * 128, (INT32_MAX / 128) * 128);
+  int64_t ns = std::max<int64_t>(1, kGroups / units);
+  ns = std::min<int64_t>(ns, std::max<int64_t>(1, span / (tiles ? kTilesLeast : kRowsLeast)));
+  L.split_rows = (int32_t)(((span + ns - 1) / ns + 127) / 128 * 128);
   L.nsplit = (int32_t)((span + L.split_rows - 1) / L.split_rows);
   L.shift = log2_of(p->pages.page_size);
   L.scale = p->scale > 0.0f ? p->scale : 1.0f / std::sqrt((float)kHeadDim);
