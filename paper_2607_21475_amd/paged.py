@@ -13,14 +13,11 @@ whose addresses it holds alive, and the tensors of a call must have the shapes a
 from __future__ import annotations
 
 import ctypes
-import math
-from dataclasses import dataclass
 from typing import Optional
 
 import torch
 
-from . import (EBD_ERR_INVALID_ARG, EBD_WS_ATTEND_PAGED, HEAD_DIM, EbdError, _check, _lib, _ptr, _stream,
-               ebd_workspace_size, workspace)
+from . import HEAD_DIM, _check, _lib, _ptr
 
 EBD_ROPE_HALF = 0
 EBD_ROPE_PAIRS = 1
@@ -28,6 +25,7 @@ EBD_ROPE_INVERSE = 1
 
 _P = ctypes.c_void_p
 _BF = torch.bfloat16
+_I32 = torch.int32
 
 
 class ebd_rotary(ctypes.Structure):
@@ -175,10 +173,16 @@ def _distinct(t, name):
 
 def _plan(p, device, keep, **tensors):
     """Note what the calls on `p` must pass, and keep what its addresses point to."""
-    p.device, p.keep = device, keep
+    if device.type != "cuda":
+        raise ValueError("the tensors must be on the GPU")
+    p.device, p.index, p.keep = device, device.index, keep
     p.expect = {n: None if t is None else (t.shape, t.stride()) for n, t in tensors.items()}
+    p.at = ctypes.addressof(p)
     return p
 
+
+# A call's checks cost as much host time as a small kernel runs, so that they read no more of a tensor than
+# its type, device, shape and strides.
 
 def _arg(p, name, t):
     """Address of a call's bf16 tensor, of the shape and strides the parameters were made for."""
@@ -189,27 +193,34 @@ def _arg(p, name, t):
         raise TypeError("%s must be a torch.Tensor" % name)
     if want is None:
         raise ValueError("%s: the parameters were made without it" % name)
-    if t.dtype != _BF:
+    if t.dtype is not _BF:
         raise TypeError("%s must be %s, got %s" % (name, _BF, t.dtype))
-    if t.device != p.device:
+    if t.get_device() != p.index:
         raise ValueError("%s must be on %s, got %s" % (name, p.device, t.device))
-    if (t.shape, t.stride()) != want:
+    if t.shape != want[0] or t.stride() != want[1]:
         raise ValueError("%s must have the shape and strides that the parameters were made for" % name)
     return t.data_ptr()
 
 
-def _status(p, t, n):
+def _out(p, name, t, dtype, shape):
+    """Address of an optional contiguous output of a call."""
     if t is None:
         return None
-    if t.device != p.device:
-        raise ValueError("status must be on %s, got %s" % (p.device, t.device))
-    return _table(t, torch.int32, (n,), "status")
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != p.index:
+        raise ValueError("%s must be on %s, got %s" % (name, p.device, t.device))
+    if (shape is not None and t.shape != shape) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous%s" % (name, "" if shape is None else " and %s" % (tuple(shape),)))
+    return t.data_ptr()
 
 
-def _launch_stream(p, stream):
-    if p.device.index != torch.cuda.current_device():
+def _on_stream(p, stream):
+    if p.index != torch._C._cuda_getDevice():
         raise ValueError("the tensors are on %s, which is not the current device" % p.device)
-    return _stream(stream)
+    return torch._C._cuda_getCurrentRawStream(p.index) if stream is None else stream.cuda_stream
 
 
 def rotary(freq: Optional[torch.Tensor], layout: int = EBD_ROPE_HALF, amplitude: float = 1.0,
@@ -292,6 +303,7 @@ def append_paged_params(pgs: ebd_pages, k_new, v_new, new_off, len, rot: Optiona
         _distinct(q_out, "q_out")
         p.q_heads, p.q_rows, p.q_out_rows = heads, _rows_of(q), _rows_of(q_out)
     K, V = pgs.pools
+    p.seqs = (pgs.num_seqs,)
     dev = _here(K, V, pgs.keep, k_new, v_new, new_off, len, pos, freq, q, q_out)
     return _plan(p, dev, (pgs.keep, new_off, len, pos, freq), K=K, V=V, k_new=k_new, v_new=v_new, q=q, q_out=q_out)
 
@@ -313,6 +325,7 @@ def attend_paged_params(pgs: ebd_pages, q, y, new_off, len, max_new: int, max_ro
     p.qpos = _table(qpos, torch.int32, (tokens,), "qpos")
     p.window, p.scale = int(window), float(scale)
     p.q_rows, p.y_rows = _rows_of(q), _rows_of(y)
+    p.seqs, p.heads = (pgs.num_seqs,), (tokens, heads)
     K, V = pgs.pools
     return _plan(p, _here(K, V, pgs.keep, q, y, new_off, len, qpos), (pgs.keep, new_off, len, qpos),
                  K=K, V=V, q=q, y=y)
@@ -323,6 +336,7 @@ def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_pa
     p = ebd_gather_paged_params()
     p.pages, p.max_rows = pgs, int(max_rows)
     p.seq_off = _table(seq_off, torch.int64, (pgs.num_seqs * pgs.kv_heads + 1,), "seq_off")
+    p.units = (pgs.num_seqs * pgs.kv_heads,)
     K, V = pgs.pools
     return _plan(p, _here(K, V, pgs.keep, seq_off), (pgs.keep, seq_off), K=K, V=V)
 
@@ -331,42 +345,34 @@ def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_pa
 
 def ebd_rope(params: ebd_rope_params, x, y, stream=None) -> None:
     """Rotate rows x into y (asynchronous on the current stream)."""
-    code = _lib.ebd_rope(ctypes.byref(params), _arg(params, "x", x), _arg(params, "y", y),
-                         _launch_stream(params, stream))
+    code = _lib.ebd_rope(params.at, _arg(params, "x", x), _arg(params, "y", y), _on_stream(params, stream))
     _check("ebd_rope", code)
 
 
 def ebd_append_paged(params: ebd_append_paged_params, k_new, v_new, K, V, q=None, q_out=None, status=None,
                      stream=None) -> None:
     """Write new tokens into their pages, and rotate their queries (asynchronous)."""
-    code = _lib.ebd_append_paged(ctypes.byref(params), _arg(params, "k_new", k_new), _arg(params, "v_new", v_new),
+    code = _lib.ebd_append_paged(params.at, _arg(params, "k_new", k_new), _arg(params, "v_new", v_new),
                                  _arg(params, "K", K), _arg(params, "V", V), _arg(params, "q", q),
-                                 _arg(params, "q_out", q_out), _status(params, status, params.pages.num_seqs),
-                                 _launch_stream(params, stream))
+                                 _arg(params, "q_out", q_out), _out(params, "status", status, _I32, params.seqs),
+                                 _on_stream(params, stream))
     _check("ebd_append_paged", code)
 
 
 def ebd_attend_paged(params: ebd_attend_paged_params, q, K, V, y, workspace, lse=None, status=None,
                      stream=None) -> None:
     """Attention of the new tokens over the paged cache (asynchronous)."""
-    if lse is not None:
-        heads = params.pages.kv_heads * params.group
-        lse_p = _table(lse, torch.float32, (params.num_tokens, heads), "lse")
-    if workspace.device != params.device or (lse is not None and lse.device != params.device):
-        raise ValueError("workspace and lse must be on %s" % params.device)
-    code = _lib.ebd_attend_paged(ctypes.byref(params), _arg(params, "q", q), _arg(params, "K", K),
-                                 _arg(params, "V", V), _arg(params, "y", y), lse_p if lse is not None else None,
-                                 _status(params, status, params.pages.num_seqs), _ptr(workspace, None, "workspace"),
-                                 workspace.numel() * workspace.element_size(), _launch_stream(params, stream))
+    code = _lib.ebd_attend_paged(params.at, _arg(params, "q", q), _arg(params, "K", K), _arg(params, "V", V),
+                                 _arg(params, "y", y), _out(params, "lse", lse, torch.float32, params.heads),
+                                 _out(params, "status", status, _I32, params.seqs),
+                                 _out(params, "workspace", workspace, workspace.dtype, None), workspace.nbytes,
+                                 _on_stream(params, stream))
     _check("ebd_attend_paged", code)
 
 
 def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None, stream=None) -> None:
     """Read the pages out as units Ku, Vu [rows, 128] (asynchronous)."""
-    units = params.pages.num_seqs * params.pages.kv_heads
-    if Ku.device != params.device or Vu.device != params.device:
-        raise ValueError("Ku and Vu must be on %s" % params.device)
-    code = _lib.ebd_gather_paged(ctypes.byref(params), _arg(params, "K", K), _arg(params, "V", V),
-                                 _ptr(Ku, _BF, "Ku"), _ptr(Vu, _BF, "Vu"), _status(params, status, units),
-                                 _launch_stream(params, stream))
+    code = _lib.ebd_gather_paged(params.at, _arg(params, "K", K), _arg(params, "V", V),
+                                 _out(params, "Ku", Ku, _BF, None), _out(params, "Vu", Vu, _BF, None),
+                                 _out(params, "status", status, _I32, params.units), _on_stream(params, stream))
     _check("ebd_gather_paged", code)
