@@ -28,7 +28,7 @@ namespace {
 constexpr int kTileKeys = 32;
 constexpr int kTileBytes = kTileKeys * 2 * kHeadDim;  // of K, or of V
 constexpr int kRowsStages = 2;
-constexpr int kRowsWaveLds = kRowsStages * 2 * kTileBytes;
+constexpr int kMergeRow = 132;  // floats of a row's sums in LDS, padded
 
 __device__ __forceinline__ float max_xor16_32(float x) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -37,13 +37,27 @@ __device__ __forceinline__ float max_xor16_32(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// A bf16 value in a word's upper half: whether it is an infinity or NaN, and its note (bit 0: +inf, bit 1:
+// -inf, both: NaN); what a note adds to a sum.
+__device__ __forceinline__ bool not_finite(uint32_t v) { return (v & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t poison_of(uint32_t v) {
+  return !not_finite(v) ? 0u : (v & 0x007f0000u) ? 3u : (v >> 31) ? 2u : 1u;
+}
+__device__ __forceinline__ float poison_value(uint32_t note) {
+  return note == 0u ? 0.0f : note == 1u ? INFINITY : note == 2u ? -INFINITY : NAN;
+}
+
 }  // namespace
 
 template <int NQ>
 __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L) {
-  __shared__ __align__(1024) uint8_t lds[kRowsWaves * kRowsWaveLds];
-  const ebd_attend_paged_params &p = L.p;
   constexpr int kRows = 16 * NQ;
+  constexpr int kMerge = kRows * (kMergeRow * 4 + 8);  // a wave's sums and statistics, when the waves combine
+  constexpr int kPoison = kRowsStages * 2 * kTileBytes;  // (read before the waves combine)
+  constexpr int kWaveLds = kPoison + kRows * kHeadDim > kMerge ? kPoison + kRows * kHeadDim : kMerge;
+  constexpr int kPair = NQ < 2 ? 1 : 2;
+  __shared__ __align__(1024) uint8_t lds[kRowsWaves * kWaveLds];
+  const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
   int bid = blockIdx.x;
   const int sp = bid % L.nsplit;
@@ -98,7 +112,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   }
 
   // lane offsets (bytes) of rows 4i + g of a 16-row slab, chunks permuted
-  uint8_t *my = lds + wave * kRowsWaveLds;
+  uint8_t *my = lds + wave * kWaveLds;
   const uint32_t rs = (uint32_t)p.pages.row_stride * 2u;
   uint32_t off[4];
 #pragma unroll
@@ -136,6 +150,10 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     return bad;
   };
 
+  // what a row got from values that are not finite, a byte per element (1: +inf, 2: -inf, 3: NaN)
+  uint8_t *poison = my + kPoison;
+  bool poisoned = false;
+
   const float sc2 = L.scale * kLog2e;
   const int stride = kRowsWaves * kTileKeys;
   int k = k_beg + wave * kTileKeys, stage = 0;
@@ -168,140 +186,139 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     }
     const bool mixed = bad || k < R.every_lo || k + kTileKeys > min(R.every_hi, k_end);
 
-    f32x4 S[NQ][2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) S[b][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        const bf16x8 A = *reinterpret_cast<const bf16x8 *>(Kt + (16 * t + c) * kRowBytes + ((4 * kb + g) ^ c) * 16);
-#pragma unroll
-        for (int b = 0; b < NQ; ++b) S[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Q[b][kb], S[b][t], 0, 0, 0);
-      }
-    }
-    float w[NQ][8];
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[b][i] = S[b][i / 4][i % 4] * sc2;
-      if (mixed) {
-        const int hi = min(span[b].hi, k_end);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = k + 16 * (i / 4) + 4 * g + i % 4;
-          const bool ok = (key >= span[b].lo) & (key < hi) & !((bad >> (i / 4)) & 1u);
-          w[b][i] = ok ? w[b][i] : -INFINITY;
-        }
-      }
-      float t = fmaxf(fmaxf(fmaxf(w[b][0], w[b][1]), fmaxf(w[b][2], w[b][3])),
-                      fmaxf(fmaxf(w[b][4], w[b][5]), fmaxf(w[b][6], w[b][7])));
-      t = max_xor16_32(t);
-      if (__any(t > m[b])) {
-        const float mn = fmaxf(m[b], t);
-        const float a = mn == -INFINITY ? 1.0f : fast_exp2(m[b] - mn);
-        m[b] = mn;
-        z[b] *= a;
-#pragma unroll
-        for (int d = 0; d < 8; ++d) O[b][d] *= a;
-      }
-      const float mu = m[b] == -INFINITY ? 0.0f : m[b];  // nothing seen yet: every l is -inf
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[b][i] = fast_exp2(w[b][i] - mu);
-        z[b] += w[b][i];
-      }
-    }
-    bf16x8 hi[NQ], lo[NQ];
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        hi[b][i] = (__bf16)w[b][i];
-        lo[b][i] = (__bf16)(w[b][i] - (float)hi[b][i]);
-      }
-    }
     // V^T operand of dims 16 d .. + 15
     auto values = [&](int d) {
       const int r = 4 * g + (c >> 2);
       const uint8_t *a = Vt + r * kRowBytes + (((2 * d + ((c & 3) >> 1)) ^ r) * 16) + 8 * (c & 1);
       return join8(read_transposed(a), read_transposed(a + 16 * kRowBytes));
     };
-    bool special = false;
     if (mixed) {
       // some row may not see a key that another sees: an infinity or NaN there must not reach it
-      uint32_t top = 0;
+      bool top = false;
 #pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        const u32x4 v = __builtin_bit_cast(u32x4, values(d));
+      for (int i = 0; i < 8; ++i) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(Vt + lane * 16 + i * 1024);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          top |= (v[i] & 0x7f80u) == 0x7f80u;
-          top |= (v[i] & 0x7f800000u) == 0x7f800000u;
+        for (int e = 0; e < 4; ++e) top |= not_finite(v[e]) | not_finite(v[e] << 16);
+      }
+      if (__any(top)) {
+        if (!poisoned) {
+#pragma unroll 1
+          for (int i = lane; i < kRows * kHeadDim / 4; i += 64) reinterpret_cast<uint32_t *>(poison)[i] = 0u;
+          poisoned = true;
+        }
+        wave_sync();
+#pragma unroll 1
+        for (int r = 0; r < kTileKeys; ++r) {
+          // dims 2 x .. 2 x + 1 of key r: the rows that see it note what they get, and it counts as zero
+          const int x = lane, key = k + r;
+          uint32_t *at = reinterpret_cast<uint32_t *>(Vt + r * kRowBytes + (((x >> 2) ^ (r & 15)) * 16) + 4 * (x & 3));
+          const uint32_t v = *at, v0 = v << 16, v1 = v & 0xffff0000u;
+          if (!__any(not_finite(v0) | not_finite(v1))) continue;
+          const uint32_t note = poison_of(v0) | poison_of(v1) << 8;
+#pragma unroll
+          for (int b = 0; b < NQ; ++b) {
+#pragma unroll 1
+            for (int j = 0; j < 16; ++j) {
+              const bool sees = (key >= __shfl(span[b].lo, j)) & (key < __shfl(span[b].hi, j));
+              if (sees & !((bad >> (r / 16)) & 1u)) reinterpret_cast<uint16_t *>(poison)[(16 * b + j) * 64 + x] |= (uint16_t)note;
+            }
+          }
+          *at = (not_finite(v0) ? 0u : v0 >> 16) | (not_finite(v1) ? 0u : v1);
+        }
+        wave_sync();
+      }
+    }
+    // two blocks of query rows at a time: more would not fit the registers, and the tile's second reads from
+    // LDS cost nothing beside the memory's
+#pragma unroll
+    for (int b0 = 0; b0 < NQ; b0 += kPair) {
+      if (b0) asm volatile("" ::: "memory");
+      f32x4 S[kPair][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int b = 0; b < kPair; ++b) S[b][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+          const bf16x8 A = *reinterpret_cast<const bf16x8 *>(Kt + (16 * t + c) * kRowBytes + ((4 * kb + g) ^ c) * 16);
+#pragma unroll
+          for (int b = 0; b < kPair; ++b)
+            S[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Q[b0 + b][kb], S[b][t], 0, 0, 0);
         }
       }
-      special = __any(top);
-    }
-    if (!special) {
+      float w[kPair][8];
+      bf16x8 hi[kPair], lo[kPair];
+#pragma unroll
+      for (int b = 0; b < kPair; ++b) {
+        const int B = b0 + b, own_hi = min(span[B].hi, k_end);
+        auto visible = [&](int i) {
+          const int key = k + 16 * (i / 4) + 4 * g + i % 4;
+          return (key >= span[B].lo) & (key < own_hi) & !((bad >> (i / 4)) & 1u);
+        };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[b][i] = S[b][i / 4][i % 4] * sc2;
+        if (mixed) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[b][i] = visible(i) ? w[b][i] : -INFINITY;
+        }
+        float t = fmaxf(fmaxf(fmaxf(w[b][0], w[b][1]), fmaxf(w[b][2], w[b][3])),
+                        fmaxf(fmaxf(w[b][4], w[b][5]), fmaxf(w[b][6], w[b][7])));
+        t = max_xor16_32(t);
+        if (__any(t > m[B])) {
+          const float mn = fmaxf(m[B], t);
+          const float a = mn == -INFINITY ? 1.0f : fast_exp2(m[B] - mn);
+          m[B] = mn;
+          z[B] *= a;
+#pragma unroll
+          for (int d = 0; d < 8; ++d) O[B][d] *= a;
+        }
+        const float mu = m[B] == -INFINITY ? 0.0f : m[B];  // nothing seen yet: every l is -inf
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          w[b][i] = fast_exp2(w[b][i] - mu);
+          z[B] += w[b][i];
+          hi[b][i] = (__bf16)w[b][i];
+          lo[b][i] = (__bf16)(w[b][i] - (float)hi[b][i]);
+        }
+      }
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
         const bf16x8 A = values(d);
 #pragma unroll
-        for (int b = 0; b < NQ; ++b) {
-          O[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, lo[b], O[b][d], 0, 0, 0);
-          O[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, hi[b], O[b][d], 0, 0, 0);
+        for (int b = 0; b < kPair; ++b) {
+          f32x4 &o = O[b0 + b][d];
+          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, lo[b], o, 0, 0, 0);
+          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, hi[b], o, 0, 0, 0);
         }
       }
-    } else {
-      // the same sums key by key, those that a row does not see left out; the weights go through the K
-      // tile's place, which has been read
-      float *W = reinterpret_cast<float *>(Kt);  // [kTileKeys][kRows]
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = 16 * (i / 4) + 4 * g + i % 4, key = k + r;
-          const bool ok = (key >= span[b].lo) & (key < min(span[b].hi, k_end)) & !((bad >> (i / 4)) & 1u);
-          W[r * kRows + 16 * b + c] = ok ? w[b][i] : -1.0f;
-        }
-      }
-      wave_sync();
-#pragma unroll 1
-      for (int r = 0; r < kTileKeys; ++r) {
-        float wk[NQ];
-#pragma unroll
-        for (int b = 0; b < NQ; ++b) wk[b] = W[r * kRows + 16 * b + c];
-#pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          const u32x2 v = *reinterpret_cast<const u32x2 *>(
-              Vt + r * kRowBytes + (((2 * d + (g >> 1)) ^ (r & 15)) * 16) + 8 * (g & 1));
-#pragma unroll
-          for (int b = 0; b < NQ; ++b) {
-            const bool ok = !(wk[b] < 0.0f);  // a NaN weight counts
-            O[b][d][0] += ok ? wk[b] * bf16_lo(v[0]) : 0.0f;
-            O[b][d][1] += ok ? wk[b] * bf16_hi(v[0]) : 0.0f;
-            O[b][d][2] += ok ? wk[b] * bf16_lo(v[1]) : 0.0f;
-            O[b][d][3] += ok ? wk[b] * bf16_hi(v[1]) : 0.0f;
-          }
-        }
-      }
-      wave_sync();
     }
     bad_any |= bad;
     bad = next_bad;
   }
   if (bad_any && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  if (poisoned) {
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const uint32_t note = *reinterpret_cast<const uint32_t *>(poison + (16 * b + c) * kHeadDim + 16 * d + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) O[b][d][i] += poison_value((note >> (8 * i)) & 3u);
+      }
+    }
+  }
 
   // The waves' sums, combined in order; a row that sees nothing keeps none.
   __syncthreads();
-  float *Ow = reinterpret_cast<float *>(my);            // [kRows][132]
-  float2 *mz = reinterpret_cast<float2 *>(Ow + kRows * 132);  // [kRows]
+  float *Ow = reinterpret_cast<float *>(my);            // [kRows][kMergeRow]
+  float2 *mz = reinterpret_cast<float2 *>(Ow + kRows * kMergeRow);  // [kRows]
 #pragma unroll
   for (int b = 0; b < NQ; ++b) {
     z[b] = add_xor32(add_xor16(z[b]));
     if (g == 0) mz[16 * b + c] = span[b].lo < span[b].hi ? make_float2(m[b], z[b]) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-    for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4 *>(Ow + (16 * b + c) * 132 + 16 * d + 4 * g) = O[b][d];
+    for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4 *>(Ow + (16 * b + c) * kMergeRow + 16 * d + 4 * g) = O[b][d];
   }
   __syncthreads();
   const int64_t slot = blockIdx.x;
@@ -311,16 +328,16 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     float M = -INFINITY, Z = 0.0f, o[8] = {};
 #pragma unroll
     for (int v = 0; v < kRowsWaves; ++v)
-      M = fmaxf(M, reinterpret_cast<const float2 *>(lds + v * kRowsWaveLds + kRows * 528)[r].x);
+      M = fmaxf(M, reinterpret_cast<const float2 *>(lds + v * kWaveLds + kRows * kMergeRow * 4)[r].x);
 #pragma unroll
     for (int v = 0; v < kRowsWaves; ++v) {
-      const float *Ov = reinterpret_cast<const float *>(lds + v * kRowsWaveLds);
-      const float2 t = reinterpret_cast<const float2 *>(Ov + kRows * 132)[r];
+      const float *Ov = reinterpret_cast<const float *>(lds + v * kWaveLds);
+      const float2 t = reinterpret_cast<const float2 *>(Ov + kRows * kMergeRow)[r];
       if (t.x == -INFINITY) continue;  // this wave saw nothing of the row
       const float a = fast_exp2(t.x - M);
       Z += a * t.y;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] += a * Ov[r * 132 + e + i];
+      for (int i = 0; i < 8; ++i) o[i] += a * Ov[r * kMergeRow + e + i];
     }
     if (r >= nrow) continue;
     if (L.nsplit > 1) {
@@ -335,33 +352,61 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   }
 }
 
-// Work-group per (sequence, KV head, block of query rows): 16 lanes a row, eight elements each.
+// A wave per query row: each quarter of it takes every fourth split, eight elements a lane, four splits' loads
+// in flight.  Short: what it takes is the latency of one load after another, so the splits' statistics,
+// their sums and the weights are asked for together.
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
   int bid = blockIdx.x;
-  const int sub = bid % (L.rows / 16);
-  bid /= L.rows / 16;
+  const int sub = bid % (L.rows / 4);
+  bid /= L.rows / 4;
   const int64_t slot0 = (int64_t)bid * L.nsplit;
   const int rb = bid % L.blocks;
   bid /= L.blocks;
   const int h = bid % H, s = bid / H;
-  const Seq sq = sequence(p, s);
-  const int r = 16 * sub + (threadIdx.x >> 4), e = (threadIdx.x & 15) * 8;
+  const int r = 4 * sub + (threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, e = (lane & 15) * 8;
   const int row = rb * L.rows + r;
+  const float2 *stats = L.stats + slot0 * L.rows + r;
+  const float *part = L.part + (slot0 * L.rows + r) * kHeadDim + e;
+  const int64_t step = (int64_t)L.rows * kHeadDim;
+  const Seq sq = sequence(p, s);
   if (row >= sq.tokens * G) return;
   float M = -INFINITY, Z = 0.0f, o[8] = {};
-  for (int v = 0; v < L.nsplit; ++v) M = fmaxf(M, L.stats[(slot0 + v) * L.rows + r].x);
-  for (int v = 0; v < L.nsplit; ++v) {
-    const float2 t = L.stats[(slot0 + v) * L.rows + r];
-    if (t.x == -INFINITY) continue;
-    const float a = fast_exp2(t.x - M);
-    const float *part = L.part + ((slot0 + v) * L.rows + r) * kHeadDim + e;
-    Z += a * t.y;
+  for (int v0 = 0; v0 < L.nsplit; v0 += 16) {
+    float2 t[4];
+    f32x4 x[4][2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] += a * part[i];
+    for (int i = 0; i < 4; ++i) {
+      const int v = v0 + 4 * i + g;
+      t[i] = make_float2(-INFINITY, 0.0f);
+      if (v >= L.nsplit) continue;
+      t[i] = stats[(int64_t)v * L.rows];
+      x[i][0] = *reinterpret_cast<const f32x4 *>(part + v * step);
+      x[i][1] = *reinterpret_cast<const f32x4 *>(part + v * step + 4);
+    }
+    const float mn = fmaxf(fmaxf(M, fmaxf(t[0].x, t[1].x)), fmaxf(t[2].x, t[3].x));
+    const float a = M == -INFINITY ? 0.0f : fast_exp2(M - mn);
+    Z *= a;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] *= a;
+    M = mn;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (t[i].x == -INFINITY) continue;  // nothing seen: its sums were not written
+      const float w = fast_exp2(t[i].x - M);
+      Z += w * t[i].y;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] += w * x[i][j / 4][j % 4];
+    }
   }
-  store_row(L, sq.t0 + row / G, h * G + row % G, e, M, Z, o);
+  // the quarters, in a fixed order
+  const float all = max_xor16_32(M);
+  const float a = M == -INFINITY ? 0.0f : fast_exp2(M - all);
+  Z = add_xor32(add_xor16(Z * a));
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o[j] = add_xor32(add_xor16(a == 0.0f ? 0.0f : o[j] * a));
+  if (g == 0) store_row(L, sq.t0 + row / G, h * G + row % G, e, all, Z, o);
 }
 
 size_t attend_paged_part_bytes(const AttendPagedLaunch &L) {
@@ -376,12 +421,13 @@ hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
   if (L.rows == kTileRows) return launch_attend_tiles(L, s);
   const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
   if (L.rows == 16) hipLaunchKernelGGL(attend_rows_kernel<1>, grid, block, 0, s, L);
-  else hipLaunchKernelGGL(attend_rows_kernel<2>, grid, block, 0, s, L);
+  else if (L.rows == 32) hipLaunchKernelGGL(attend_rows_kernel<2>, grid, block, 0, s, L);
+  else hipLaunchKernelGGL(attend_rows_kernel<4>, grid, block, 0, s, L);
   return hipGetLastError();
 }
 
 hipError_t launch_attend_paged_join(const AttendPagedLaunch &L, hipStream_t s) {
-  const int64_t groups = attend_paged_groups(L) / L.nsplit * (L.rows / 16);
+  const int64_t groups = attend_paged_groups(L) / L.nsplit * (L.rows / 4);
   hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)groups), dim3(256), 0, s, L);
   return hipGetLastError();
 }

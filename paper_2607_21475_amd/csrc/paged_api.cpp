@@ -75,7 +75,7 @@ AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   AttendPagedLaunch L{};
   L.p = *p;
   const int64_t rows = (int64_t)p->max_new * p->group;
-  L.rows = rows <= 16 ? 16 : (rows <= kRowsKernelMax ? 32 : kTileRows);
+  L.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= kRowsKernelMax ? 64 : kTileRows;
   const bool tiles = L.rows == kTileRows;
   L.blocks = (int32_t)std::max<int64_t>(1, (rows + L.rows - 1) / L.rows);
   // the most rows a block of query rows sees, from a tile's border on
