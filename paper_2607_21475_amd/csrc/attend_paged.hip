@@ -37,16 +37,6 @@ __device__ __forceinline__ float max_xor16_32(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// A bf16 value in a word's upper half: whether it is an infinity or NaN, and its note (bit 0: +inf, bit 1:
-// -inf, both: NaN); what a note adds to a sum.
-__device__ __forceinline__ bool not_finite(uint32_t v) { return (v & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ uint32_t poison_of(uint32_t v) {
-  return !not_finite(v) ? 0u : (v & 0x007f0000u) ? 3u : (v >> 31) ? 2u : 1u;
-}
-__device__ __forceinline__ float poison_value(uint32_t note) {
-  return note == 0u ? 0.0f : note == 1u ? INFINITY : note == 2u ? -INFINITY : NAN;
-}
-
 }  // namespace
 
 template <int NQ>

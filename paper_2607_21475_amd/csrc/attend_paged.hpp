@@ -97,6 +97,16 @@ __device__ __forceinline__ Range range_of(const Span (&s)[N]) {
   return {wave_min(lo), -wave_min(-hi), -wave_min(-elo), wave_min(ehi)};
 }
 
+// A bf16 value in a word's upper half: whether it is an infinity or NaN, and its note (bit 0: +inf, bit 1:
+// -inf, both: NaN); what a note adds to a sum.
+__device__ __forceinline__ bool not_finite(uint32_t v) { return (v & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t poison_of(uint32_t v) {
+  return !not_finite(v) ? 0u : (v & 0x007f0000u) ? 3u : (v >> 31) ? 2u : 1u;
+}
+__device__ __forceinline__ float poison_value(uint32_t note) {
+  return note == 0u ? 0.0f : note == 1u ? INFINITY : note == 2u ? -INFINITY : NAN;
+}
+
 // Elements e .. e+7 of a finished row: token t, query head hq, sums o over weights that total Z with the
 // maximum M (-inf: the row saw nothing).
 __device__ __forceinline__ void store_row(const AttendPagedLaunch &L, int64_t t, int hq, int e, float M, float Z,

@@ -21,13 +21,46 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kKeys = 64;                    // keys per tile
-constexpr int kTile = kKeys * kRowBytes;     // bytes of its K, or of its V
+constexpr int kKeys = 64;                 // keys per tile
+constexpr int kTile = kKeys * kRowBytes;  // bytes of its K, or of its V
 constexpr int kStage = 2 * kTile;
+constexpr int kStages = 3;
 constexpr int kWaves = 8;
 constexpr float kLazy = 8.0f;
 
+// The order of 16 products and their reads of LDS (READS a product): `ahead` products' operands are on their way,
+// no more, so that the registers suffice.
+template <int AHEAD, int READS>
+__device__ __forceinline__ void feed() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+  for (int i = 0; i < 16 - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
+template <class T>
+__device__ __forceinline__ T lds_read(uint32_t at) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) T *>(at);
+}
+template <class T>
+__device__ __forceinline__ void lds_write(uint32_t at, const T &v) {
+  *reinterpret_cast<__attribute__((address_space(3))) T *>(at) = v;
+}
+__device__ __forceinline__ s16x4 lds_read_transposed(uint32_t at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(at));
+}
+
 __device__ __forceinline__ int chunk_turn(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+
+// Written out: from fmaxf the compiler makes three instructions, two of them to quiet NaN.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 __device__ __forceinline__ float max_halves(float x) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -37,8 +70,10 @@ __device__ __forceinline__ float max_halves(float x) {
 }  // namespace
 
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
-  __shared__ __align__(1024) uint8_t tiles[2 * kStage];
-  __shared__ float weights[kWaves][kKeys][32];  // of a tile that is summed key by key (below)
+  __shared__ __align__(1024) uint8_t tiles[kStages * kStage];
+  __shared__ uint32_t poisons[kWaves][32][8];     // of each query row, two bits an element
+  __shared__ uint16_t notes[kStages][kKeys][16];  // of a tile's values, 16 bits a chunk
+  __shared__ int noted[kStages][kWaves];          // ... whether a wave noted any
   __shared__ Range ranges[kWaves];
   __shared__ int bad_pages;
   const ebd_attend_paged_params &p = L.p;
@@ -67,15 +102,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   if (threadIdx.x == 0) bad_pages = 0;
   if (lane == 0) ranges[wave] = R;
   __syncthreads();
-  int lo = INT32_MAX, hi = 0;
+  int lo = INT32_MAX, hi = 0, every_lo = 0, every_hi = INT32_MAX;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    lo = min(lo, ranges[w].lo);
-    hi = max(hi, ranges[w].hi);
+    lo = min(lo, ranges[w].lo), hi = max(hi, ranges[w].hi);
+    every_lo = max(every_lo, ranges[w].every_lo), every_hi = min(every_hi, ranges[w].every_hi);
   }
+  lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+  every_lo = __builtin_amdgcn_readfirstlane(every_lo);
   const int64_t start = (lo & -kKeys) + (int64_t)sp * L.split_rows;
   const int k_end = start < hi ? (int)min((int64_t)hi, start + L.split_rows) : 0;
   const int k_beg = start < hi ? (int)start : 0;
+  every_hi = min(__builtin_amdgcn_readfirstlane(every_hi), k_end);
 
   const const_i32 *table = (const const_i32 *)(p.pages.page_table + (int64_t)s * p.pages.max_pages);
   const int slots = p.pages.page_size - 1;
@@ -111,31 +149,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   }
   const int64_t head = (int64_t)h * p.pages.head_stride;
   auto page_of = [&](int k) -> int { return k < k_end ? table[k >> L.shift] : 0; };
-  auto issue = [&](int k, int pg, int stage) {
+  // Step t reads V of tile t and K of tile t + 1: they travel together, in stage (t + 1) % kStages, K first.
+  const uint32_t part = 8 * wave * kRowBytes;
+  auto address = [&](int k, int pg) {
     if ((uint32_t)pg >= (uint32_t)p.pages.num_pages) pg = 0;  // its rows are masked
-    const int slot = (k + 8 * wave) & slots;
-    const int64_t at = 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)slot * rs;
-    const uint8_t *pk = reinterpret_cast<const uint8_t *>(L.K) + at, *pv = reinterpret_cast<const uint8_t *>(L.V) + at;
-    const uint32_t to = lds_at(tiles + stage * kStage + 8 * wave * kRowBytes);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      load_lds16(to + i * 4 * kRowBytes, pk + (int64_t)(4 * i) * rs, off[i]);
-      load_lds16(to + kTile + i * 4 * kRowBytes, pv + (int64_t)(4 * i) * rs, off[i]);
-    }
+    return 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)((k + 8 * wave) & slots) * rs;
   };
+  auto load_tile = [&](const uint16_t *pool, int64_t at, uint32_t to) {
+    const uint8_t *x = reinterpret_cast<const uint8_t *>(pool) + at;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_lds16(to + i * 4 * kRowBytes, x + (int64_t)(4 * i) * rs, off[i]);
+  };
+  // (what lies past the range comes from page 0 and is not used: each step loads the same number of times)
 
-  // LDS offsets: K operand rows c, dims 16 kb + 8 half; V operand rows 4 half + c16 / 4 (+ 8)
-  uint32_t ka[8], va[4][2];
-#pragma unroll
-  for (int kb = 0; kb < 8; ++kb) ka[kb] = c * kRowBytes + ((2 * kb + half) ^ chunk_turn(c)) * 16;
+  // LDS addresses within a tile: K operand row c, dims 16 kb + 8 half at ka ^ 32 kb; V operand rows
+  // 4 half + c16 / 4 (+ 8), dims 32 d + .. at va ^ 64 d (tiles are aligned to 1024 bytes)
   const int c16 = lane & 15, q16 = (lane >> 4) & 1;
+  const uint32_t ka = c * kRowBytes + (half ^ chunk_turn(c)) * 16;
+  uint32_t va[2];
 #pragma unroll
-  for (int d = 0; d < 4; ++d) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = 4 * half + (c16 >> 2) + 8 * u;
-      va[d][u] = kTile + r * kRowBytes + ((4 * d + 2 * q16 + ((c16 & 3) >> 1)) ^ chunk_turn(r)) * 16 + 8 * (c16 & 1);
-    }
+  for (int u = 0; u < 2; ++u) {
+    const int r = 4 * half + (c16 >> 2) + 8 * u;
+    va[u] = r * kRowBytes + ((2 * q16 + ((c16 & 3) >> 1)) ^ chunk_turn(r)) * 16 + 8 * (c16 & 1);
   }
 
   f32x16 O[4];
@@ -144,32 +179,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   float m = -INFINITY, z = 0.0f;
   const float sc2 = L.scale * kLog2e;
 
-  auto step = [&](int k, const uint8_t *T, uint32_t bad) {
-    const bool mixed = bad || k < R.every_lo || k + kKeys > min(R.every_hi, k_end);
-    f32x16 S[2];
+  const uint32_t tiles_at = lds_at(tiles);
+  auto stage_of = [&](int i) { return tiles_at + i * kStage; };
+  const int own_hi = min(span[0].hi, k_end);
+  uint32_t(*poison)[8] = poisons[wave];
+  bool poisoned = false;
+  f32x16 S[2];
+  bf16x8 W[4];
+
+  auto scores = [&](uint32_t Kt) {
+    const uint32_t at = Kt + ka;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       S[b] = f32x16{};
 #pragma unroll
       for (int kb = 0; kb < 8; ++kb)
-        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(T + ka[kb] + b * 32 * kRowBytes), Q[kb], S[b], 0, 0, 0);
+        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read<bf16x8>((at ^ (32 * kb)) + b * 32 * kRowBytes), Q[kb], S[b], 0, 0, 0);
     }
-    const int own_hi = min(span[0].hi, k_end);
-    auto visible = [&](int b, int i) {
-      const int key = k + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
-      return (key >= span[0].lo) & (key < own_hi) & !((bad >> (2 * b + i / 8)) & 1u);
-    };
-    if (mixed) {
+    feed<4, 1>();
+  };
+  auto mixed = [&](int k, uint32_t bad) { return bad || k < R.every_lo || k + kKeys > min(R.every_hi, k_end); };
+  auto softmax = [&](int k, uint32_t bad) {
+    if (mixed(k, bad)) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[b][i] = visible(b, i) ? S[b][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int key = k + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+          const bool ok = (key >= span[0].lo) & (key < own_hi) & !((bad >> (2 * b + i / 8)) & 1u);
+          S[b][i] = ok ? S[b][i] : -INFINITY;
+        }
       }
     }
-    float t = fmaxf(S[0][0], S[1][0]);
+    // (the first maxima read both accumulators' last products, which the compiler waits for, and the rest
+    // depend on them)
+    float t0 = fmaxf(S[0][0], S[1][0]), t1 = fmaxf(S[0][1], S[1][1]);
+    t1 = fmaxf(t1, t0);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) t = fmaxf(t, fmaxf(S[0][i], S[1][i]));
-    t = max_halves(t) * sc2;
+    for (int i = 2; i < 16; i += 2) {
+      t0 = max3(t0, S[0][i], S[0][i + 1]);
+      t1 = max3(t1, S[1][i], S[1][i + 1]);
+    }
+    const float t = max_halves(fmaxf(t0, t1)) * sc2;
     if (__any(t > m + kLazy)) {
       const float mn = fmaxf(m, t);
       const float a = mn == -INFINITY ? 1.0f : fast_exp2(m - mn);
@@ -179,97 +230,164 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
       for (int d = 0; d < 4; ++d) O[d] *= a;
     }
     const float mu = m == -INFINITY ? 0.0f : m;  // nothing seen yet: every score is -inf
-    bf16x8 W[4];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        S[b][i] = fast_exp2(__builtin_fmaf(S[b][i], sc2, -mu));
-        z += S[b][i];
-        W[2 * b + i / 8][i % 8] = (__bf16)S[b][i];
+        const float w = fast_exp2(__builtin_fmaf(S[b][i], sc2, -mu));
+        z += w;
+        W[2 * b + i / 8][i % 8] = (__bf16)w;
       }
-    }
-    auto values = [&](int d, int ks) {
-      return join8(read_transposed(T + va[d][0] + ks * 16 * kRowBytes), read_transposed(T + va[d][1] + ks * 16 * kRowBytes));
-    };
-    bool special = false;
-    if (mixed) {
-      // some row may not see a key that another sees: an infinity or NaN there must not reach it
-      bool top = false;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(T + kTile + lane * 16 + i * 1024);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f80u) == 0x7f80u) | ((v[e] & 0x7f800000u) == 0x7f800000u);
-      }
-      special = __any(top);
-    }
-    if (!special) {
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-#pragma unroll
-        for (int d = 0; d < 4; ++d) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, ks), W[ks], O[d], 0, 0, 0);
-      }
-    } else {
-      // the same sums key by key, those that a row does not see left out
-      float(*w)[32] = weights[wave];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[32 * b + 8 * (i / 4) + 4 * half + i % 4][c] = visible(b, i) ? S[b][i] : -1.0f;
-      }
-      wave_sync();
-#pragma unroll 1
-      for (int r = 0; r < kKeys; ++r) {
-        const float wk = w[r][c];
-        const bool ok = !(wk < 0.0f);  // a NaN weight counts
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const u32x2 v = *reinterpret_cast<const u32x2 *>(T + kTile + r * kRowBytes + ((4 * d + j) ^ chunk_turn(r)) * 16 + 8 * half);
-            O[d][4 * j + 0] += ok ? wk * bf16_lo(v[0]) : 0.0f;
-            O[d][4 * j + 1] += ok ? wk * bf16_hi(v[0]) : 0.0f;
-            O[d][4 * j + 2] += ok ? wk * bf16_lo(v[1]) : 0.0f;
-            O[d][4 * j + 3] += ok ? wk * bf16_hi(v[1]) : 0.0f;
-          }
-        }
-      }
-      wave_sync();
     }
   };
-
-  int k = k_beg, stage = 0, pg = 0;
-  if (k < k_end) {
-    issue(k, page_of(k + 8 * wave), 0);
-    pg = page_of(k + kKeys + 8 * wave);
-  }
-  for (; k < k_end; k += kKeys, stage ^= 1) {
-    wait_loads<0>();
-    __syncthreads();  // the tile is here, and the other one has been read
-    if (k + kKeys < k_end) {
-      issue(k + kKeys, pg, stage ^ 1);
-      pg = page_of(k + 2 * kKeys + 8 * wave);
+  auto sums = [&](uint32_t Vt) {
+    const uint32_t at0 = Vt + va[0], at1 = Vt + va[1];
+    auto values = [&](int d, int ks) {
+      return join8(lds_read_transposed((at0 ^ (64 * d)) + ks * 16 * kRowBytes),
+                   lds_read_transposed((at1 ^ (64 * d)) + ks * 16 * kRowBytes));
+    };
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, ks), W[ks], O[d], 0, 0, 0);
     }
+    feed<4, 2>();
+  };
+  auto bad_of = [&](int k) {
     uint32_t bad = 0;
     if (any_bad) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
-        bad |= (uint32_t)((uint32_t)page_of(k + 16 * b) >= (uint32_t)p.pages.num_pages) << b;
+      for (int b = 0; b < 4; ++b) bad |= (uint32_t)((uint32_t)page_of(k + 16 * b) >= (uint32_t)p.pages.num_pages) << b;
     }
-    uint8_t *T = tiles + stage * kStage;
-    if (k + kKeys > k_end || bad) {
-      // values of rows that no query row may see must not reach a product: 0 x NaN
-      const int r = 8 * wave + (lane >> 4);
+    return bad;
+  };
+  // Infinities and NaN must not reach the sums of query rows that do not see them (0 x NaN).  In tiles that some
+  // query row sees in part, each wave looks through the values that it loaded: rows that none may see become
+  // zeros, and elsewhere what is not finite becomes zero and is noted, two bits an element; then
+  // the waves whose query rows see such a key keep the notes (poison), and add them to their sums at the end.
+  auto partial = [&](int k, uint32_t bad) { return bad || k < every_lo || k + kKeys > every_hi; };
+  auto inspect = [&](int stage, int k) {
+    const uint32_t bad = bad_of(k);
+    if (!partial(k, bad)) return;
+    bool any = false;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int rr = r + 4 * i;
-        if (k + rr >= k_end || ((bad >> (rr / 16)) & 1u))
-          *reinterpret_cast<uint4 *>(T + kTile + rr * kRowBytes + (lane & 15) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < 2; ++i) {
+      const int r = 8 * wave + (lane >> 4) + 4 * i;
+      const uint32_t at = stage_of(stage) + kTile + r * kRowBytes + (lane & 15) * 16;
+      u32x4 v = lds_read<u32x4>(at);
+      uint32_t note = 0;
+      if (k + r >= k_end || ((bad >> (r / 16)) & 1u)) {
+        v = u32x4{0u, 0u, 0u, 0u};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t n0 = poison_of(v[e] << 16), n1 = poison_of(v[e] & 0xffff0000u);
+          v[e] &= (n0 ? 0u : 0xffffu) | (n1 ? 0u : 0xffff0000u);
+          note |= (n0 | n1 << 2) << (4 * e);
+        }
       }
-      __syncthreads();
+      notes[stage][r][(lane & 15) ^ chunk_turn(r)] = (uint16_t)note;
+      lds_write(at, v);
+      any |= note != 0u;
     }
-    if (k < R.hi && k + kKeys > R.lo) step(k, T, bad);
+    any = __any(any);
+    if (lane == 0) noted[stage][wave] = any;
+  };
+  auto keep_notes = [&](int stage, int k, uint32_t bad) {
+    if (!partial(k, bad) || !__any(lane < kWaves && noted[stage][lane & (kWaves - 1)])) return;
+    if (!poisoned) {
+      for (int i = lane; i < 256; i += 64) poison[0][i] = 0u;
+      poisoned = true;
+    }
+    wave_sync();
+#pragma unroll 1
+    for (int r = 0; r < kKeys; ++r) {
+      const uint32_t note = lane < 16 ? notes[stage][r][lane] : 0u;
+      if (!__any(note)) continue;
+#pragma unroll 1
+      for (int j = 0; j < 32; ++j) {
+        const bool hit = (k + r >= __shfl(span[0].lo, j)) & (k + r < __shfl(own_hi, j));
+        if (hit && note) atomicOr(&poison[j][lane >> 1], note << (16 * (lane & 1)));
+      }
+    }
+    wave_sync();
+  };
+  auto mine = [&](int k) { return k < R.hi && k + kKeys > R.lo; };  // whether this wave's rows see the tile
+  auto barrier = [&]() {
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+  };
+
+  if (k_beg < k_end) {
+    // Waves 0-3 and 4-7 (one of each a SIMD) alternate: while the one half forms its weights, the other
+    // half's products run.  Step t: weights of tile t, barrier, sums over V of t and scores of K of t + 1, barrier;
+    // the second half is one barrier behind.  Tile t's pair (V of t, K of t + 1) is waited for before the barrier
+    // that the first half's products follow, and its stage is free two barriers later.
+    const bool second = wave >= kWaves / 2;
+    int next_k = k_beg;   // first key of the V tile of the pair to load next
+    int64_t vat = address(k_beg, page_of(k_beg + 8 * wave));  // ... where it lies
+    int pg = page_of(k_beg + kKeys + 8 * wave);               // page of the K tile behind it
+    int load_stage = 1;
+    load_tile(L.K, vat, tiles_at + part);
+    auto load_pair = [&]() {
+      const uint32_t to = tiles_at + load_stage * kStage + part;
+      const int64_t kat = address(next_k + kKeys, pg);
+      load_tile(L.K, kat, to);
+      load_tile(L.V, vat, to + kTile);
+      vat = kat;
+      next_k += kKeys;
+      pg = page_of(next_k + kKeys + 8 * wave);
+      load_stage = load_stage == kStages - 1 ? 0 : load_stage + 1;
+    };
+    for (int i = 0; i < kStages - 1; ++i) load_pair();
+    wait_loads<4 * (kStages - 1)>();
+    barrier();
+    if (mine(k_beg)) scores(stage_of(0));
+    if (second) {
+      wait_loads<4 * (kStages - 2)>();
+      inspect(1, k_beg);
+      barrier();
+    }
+    int st = 1;  // stage of this step's pair
+    for (int k = k_beg; k < k_end; k += kKeys) {
+      const uint32_t bad = bad_of(k);
+      const uint32_t T = stage_of(st);
+      const bool own = mine(k), after = mine(k + kKeys) && k + kKeys < k_end;
+      if (second) load_pair();
+      if (own) softmax(k, bad);
+      if (!second) {
+        wait_loads<4 * (kStages - 2)>();
+        inspect(st, k);
+      }
+      barrier();
+      if (!second) load_pair();
+      __builtin_amdgcn_s_setprio(1);
+      if (own) {
+        keep_notes(st, k, bad);
+        sums(T + kTile);
+      }
+      if (after) scores(T);
+      __builtin_amdgcn_s_setprio(0);
+      if (second) {
+        wait_loads<4 * (kStages - 2)>();
+        inspect(st == kStages - 1 ? 0 : st + 1, k + kKeys);
+      }
+      barrier();
+      st = st == kStages - 1 ? 0 : st + 1;
+    }
+    if (!second) barrier();
+    wait_loads<0>();
+    if (poisoned) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t note = poison[c][2 * d + j / 2] >> (16 * (j % 2) + 8 * half);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[d][4 * j + i] += poison_value((note >> (2 * i)) & 3u);
+        }
+      }
+    }
   }
 
   z += __shfl_xor(z, 32);
