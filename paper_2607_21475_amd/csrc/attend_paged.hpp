@@ -12,6 +12,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((address_space(4))) int32_t const_i32;  // read through the scalar cache
+typedef __attribute__((address_space(4))) int64_t const_i64;
 
 constexpr int kRowBytes = 2 * kHeadDim;
 
@@ -50,9 +51,10 @@ struct Seq {
 };
 __device__ __forceinline__ Seq sequence(const ebd_attend_paged_params &p, int s) {
   Seq q;
-  q.t0 = p.new_off[s];
-  const int64_t n = p.new_off[s + 1] - q.t0;
-  q.len = p.len[s];
+  const const_i64 *off = (const const_i64 *)p.new_off;
+  q.t0 = off[s];
+  const int64_t n = off[s + 1] - q.t0;
+  q.len = ((const const_i32 *)p.len)[s];
   q.first = q.len - n;
   q.status = (n > p.max_new || q.len > p.max_rows) ? EBD_ST_BAD_LAYOUT : 0u;
   q.seen = min(q.len, p.max_rows);
@@ -105,6 +107,16 @@ __device__ __forceinline__ uint32_t poison_of(uint32_t v) {
 }
 __device__ __forceinline__ float poison_value(uint32_t note) {
   return note == 0u ? 0.0f : note == 1u ? INFINITY : note == 2u ? -INFINITY : NAN;
+}
+
+// range_of the query rows of tokens j0 .. j1 without positions of their own (p.qpos is NULL): what they see moves
+// on with the token, so the first and the last that see anything tell.
+__device__ __forceinline__ Range range_of_tokens(const ebd_attend_paged_params &p, const Seq &q, int j0, int j1) {
+  const int64_t w = p.window > 0 ? p.window : INT64_MAX / 2;
+  const int64_t a = max(q.first + j0, (int64_t)0), b = min(q.first + min(j1, q.tokens - 1), q.seen - 2 + w);
+  if (a > b || q.seen <= 0) return {INT32_MAX, 0, 0, INT32_MAX};
+  return {(int)max((int64_t)0, a - w + 1), (int)min(b + 1, q.seen), (int)max((int64_t)0, b - w + 1),
+          (int)min(a + 1, q.seen)};
 }
 
 // Elements e .. e+7 of a finished row: token t, query head hq, sums o over weights that total Z with the

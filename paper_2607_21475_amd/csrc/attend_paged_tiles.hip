@@ -24,21 +24,31 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kKeys = 64;                 // keys per tile
 constexpr int kTile = kKeys * kRowBytes;  // bytes of its K, or of its V
 constexpr int kStage = 2 * kTile;
-constexpr int kStages = 3;
+constexpr int kStages = 4;
 constexpr int kWaves = 8;
 constexpr float kLazy = 8.0f;
 
-// The order of 16 products and their reads of LDS (READS a product): `ahead` products' operands are on their way,
-// no more, so that the registers suffice.
-template <int AHEAD, int READS>
+// The order of a step's products and their reads of LDS: 16 products with one read each, 16 with two, the
+// operands of four products on their way, no more, so that the registers suffice.
 __device__ __forceinline__ void feed() {
-  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+  constexpr int kRead = 0x100, kProduct = 0x008;
+  __builtin_amdgcn_sched_group_barrier(kRead, 4, 0);
 #pragma unroll
-  for (int i = 0; i < 16 - AHEAD; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  for (int i = 0; i < 12; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kProduct, 4, 0);
+}
+
+__device__ __forceinline__ Range uniform(const Range &r) {
+  return {__builtin_amdgcn_readfirstlane(r.lo), __builtin_amdgcn_readfirstlane(r.hi),
+          __builtin_amdgcn_readfirstlane(r.every_lo), __builtin_amdgcn_readfirstlane(r.every_hi)};
 }
 
 template <class T>
@@ -75,7 +85,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   __shared__ uint16_t notes[kStages][kKeys][16];  // of a tile's values, 16 bits a chunk
   __shared__ int noted[kStages][kWaves];          // ... whether a wave noted any
   __shared__ Range ranges[kWaves];
-  __shared__ int bad_pages;
+  __shared__ int bad_pages[kWaves];
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
   // heads vary fastest (work-groups go round the XCDs: a head's stay together for 8, 4, 2 heads and
@@ -98,46 +108,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   const int row = row0 + 32 * wave + c;
   Span span[1] = {span_of(p, sq, row)};
   const bool sees = span[0].lo < span[0].hi;
-  const Range R = range_of<1>(span);
-  if (threadIdx.x == 0) bad_pages = 0;
-  if (lane == 0) ranges[wave] = R;
-  __syncthreads();
-  int lo = INT32_MAX, hi = 0, every_lo = 0, every_hi = INT32_MAX;
+  Range R, all;
+  if (!p.qpos) {
+    R = range_of_tokens(p, sq, (row0 + 32 * wave) / G, (row0 + 32 * wave + 31) / G);
+    all = range_of_tokens(p, sq, row0 / G, (row0 + nrow - 1) / G);
+  } else {
+    R = range_of<1>(span);
+    if (lane == 0) ranges[wave] = R;
+    __syncthreads();
+    all = ranges[0];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    lo = min(lo, ranges[w].lo), hi = max(hi, ranges[w].hi);
-    every_lo = max(every_lo, ranges[w].every_lo), every_hi = min(every_hi, ranges[w].every_hi);
+    for (int w = 1; w < kWaves; ++w) {
+      all.lo = min(all.lo, ranges[w].lo), all.hi = max(all.hi, ranges[w].hi);
+      all.every_lo = max(all.every_lo, ranges[w].every_lo), all.every_hi = min(all.every_hi, ranges[w].every_hi);
+    }
   }
-  lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
-  every_lo = __builtin_amdgcn_readfirstlane(every_lo);
-  const int64_t start = (lo & -kKeys) + (int64_t)sp * L.split_rows;
-  const int k_end = start < hi ? (int)min((int64_t)hi, start + L.split_rows) : 0;
-  const int k_beg = start < hi ? (int)start : 0;
-  every_hi = min(__builtin_amdgcn_readfirstlane(every_hi), k_end);
-
+  R = uniform(R);
+  all = uniform(all);
+  const int64_t start = (all.lo & -kKeys) + (int64_t)sp * L.split_rows;
+  const int k_end = start < all.hi ? (int)min((int64_t)all.hi, start + L.split_rows) : 0;
+  const int k_beg = start < all.hi ? (int)start : 0;
+  const int every_lo = all.every_lo, every_hi = min(all.every_hi, k_end);
   const const_i32 *table = (const const_i32 *)(p.pages.page_table + (int64_t)s * p.pages.max_pages);
   const int slots = p.pages.page_size - 1;
-  {
-    bool bad = false;
-    if (k_end > k_beg)
-      for (int e = (k_beg >> L.shift) + (int)threadIdx.x; e <= (k_end - 1) >> L.shift; e += 64 * kWaves)
-        bad |= (uint32_t)table[e] >= (uint32_t)p.pages.num_pages;
-    if (bad) bad_pages = 1;
-  }
-
-  bf16x8 Q[8];  // B operand: column c is this lane's query row, dims 16 kb + 8 half .. + 7
-  {
-    const int j = sees ? row / G : 0, hq = h * G + (sees ? row % G : 0);
-    const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
-#pragma unroll
-    for (int kb = 0; kb < 8; ++kb)
-      Q[kb] = __builtin_bit_cast(bf16x8, sees ? reinterpret_cast<const uint4 *>(q)[2 * kb + half] : make_uint4(0u, 0u, 0u, 0u));
-  }
-#pragma unroll
-  for (int kb = 0; kb < 8; ++kb) asm volatile("" : "+v"(Q[kb]));
-  __syncthreads();
-  const bool any_bad = __builtin_amdgcn_readfirstlane(bad_pages) != 0;
-  if (any_bad && threadIdx.x == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
 
   // this wave's part of a tile: rows 8 wave .. + 7, four rows a load, of K and of V
   const uint32_t rs = (uint32_t)p.pages.row_stride * 2u;
@@ -148,7 +141,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     off[i] = (uint32_t)(lane >> 4) * rs + (uint32_t)((lane & 15) ^ chunk_turn(r)) * 16u;
   }
   const int64_t head = (int64_t)h * p.pages.head_stride;
-  auto page_of = [&](int k) -> int { return k < k_end ? table[k >> L.shift] : 0; };
+  // (past the range: some page of it.  What is loaded there is not used, but each step loads the same number of times.)
+  auto page_of = [&](int k) -> int { return table[min(k, k_end - 1) >> L.shift]; };
   // Step t reads V of tile t and K of tile t + 1: they travel together, in stage (t + 1) % kStages, K first.
   const uint32_t part = 8 * wave * kRowBytes;
   auto address = [&](int k, int pg) {
@@ -160,7 +154,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
 #pragma unroll
     for (int i = 0; i < 2; ++i) load_lds16(to + i * 4 * kRowBytes, x + (int64_t)(4 * i) * rs, off[i]);
   };
-  // (what lies past the range comes from page 0 and is not used: each step loads the same number of times)
 
   // LDS addresses within a tile: K operand row c, dims 16 kb + 8 half at ka ^ 32 kb; V operand rows
   // 4 half + c16 / 4 (+ 8), dims 32 d + .. at va ^ 64 d (tiles are aligned to 1024 bytes)
@@ -185,18 +178,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   uint32_t(*poison)[8] = poisons[wave];
   bool poisoned = false;
   f32x16 S[2];
-  bf16x8 W[4];
+  bf16x8 Q[8];  // B operand: column c is this lane's query row, dims 16 kb + 8 half .. + 7
+  bf16x8 W[4];  // weights, the B operand of the sums
+  bool any_bad = false;
 
+  auto keys = [&](uint32_t Kt, int i) {
+    return lds_read<bf16x8>(((Kt + ka) ^ (32 * (i / 2))) + (i % 2) * 32 * kRowBytes);
+  };
+  auto values = [&](uint32_t Vt, int i) {
+    const uint32_t d = 64 * (i % 4), ks = (i / 4) * 16 * kRowBytes;
+    return join8(lds_read_transposed(((Vt + va[0]) ^ d) + ks), lds_read_transposed(((Vt + va[1]) ^ d) + ks));
+  };
   auto scores = [&](uint32_t Kt) {
-    const uint32_t at = Kt + ka;
+    S[0] = S[1] = f32x16{};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      S[b] = f32x16{};
+    for (int i = 0; i < 16; ++i) S[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys(Kt, i), Q[i / 2], S[i % 2], 0, 0, 0);
+  };
+  auto sums = [&](uint32_t Vt) {
 #pragma unroll
-      for (int kb = 0; kb < 8; ++kb)
-        S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read<bf16x8>((at ^ (32 * kb)) + b * 32 * kRowBytes), Q[kb], S[b], 0, 0, 0);
-    }
-    feed<4, 1>();
+    for (int i = 0; i < 16; ++i) O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(Vt, i), W[i / 4], O[i % 4], 0, 0, 0);
   };
   auto mixed = [&](int k, uint32_t bad) { return bad || k < R.every_lo || k + kKeys > min(R.every_hi, k_end); };
   auto softmax = [&](int k, uint32_t bad) {
@@ -239,19 +239,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
         W[2 * b + i / 8][i % 8] = (__bf16)w;
       }
     }
-  };
-  auto sums = [&](uint32_t Vt) {
-    const uint32_t at0 = Vt + va[0], at1 = Vt + va[1];
-    auto values = [&](int d, int ks) {
-      return join8(lds_read_transposed((at0 ^ (64 * d)) + ks * 16 * kRowBytes),
-                   lds_read_transposed((at1 ^ (64 * d)) + ks * 16 * kRowBytes));
-    };
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-#pragma unroll
-      for (int d = 0; d < 4; ++d) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, ks), W[ks], O[d], 0, 0, 0);
-    }
-    feed<4, 2>();
   };
   auto bad_of = [&](int k) {
     uint32_t bad = 0;
@@ -320,31 +307,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
 
   if (k_beg < k_end) {
     // Waves 0-3 and 4-7 (one of each a SIMD) alternate: while the one half forms its weights, the other
-    // half's products run.  Step t: weights of tile t, barrier, sums over V of t and scores of K of t + 1, barrier;
+    // half's products run.  Step t: weights of tile t, barrier, scores of K of t + 1 and sums over V of t, barrier;
     // the second half is one barrier behind.  Tile t's pair (V of t, K of t + 1) is waited for before the barrier
-    // that the first half's products follow, and its stage is free two barriers later.
+    // that the first half's products follow; its stage is free two barriers later, and is written again by
+    // loads that a step between issues at its start (so that the products' phase holds nothing else).
     const bool second = wave >= kWaves / 2;
     int next_k = k_beg;   // first key of the V tile of the pair to load next
-    int64_t vat = address(k_beg, page_of(k_beg + 8 * wave));  // ... where it lies
     int pg = page_of(k_beg + kKeys + 8 * wave);               // page of the K tile behind it
+    int64_t vat = address(k_beg, page_of(k_beg + 8 * wave));  // where the V tile lies
     int load_stage = 1;
     load_tile(L.K, vat, tiles_at + part);
     auto load_pair = [&]() {
-      const uint32_t to = tiles_at + load_stage * kStage + part;
+      const uint32_t to = stage_of(load_stage) + part;
       const int64_t kat = address(next_k + kKeys, pg);
       load_tile(L.K, kat, to);
       load_tile(L.V, vat, to + kTile);
       vat = kat;
       next_k += kKeys;
       pg = page_of(next_k + kKeys + 8 * wave);
-      load_stage = load_stage == kStages - 1 ? 0 : load_stage + 1;
+      load_stage = (load_stage + 1) % kStages;
     };
-    for (int i = 0; i < kStages - 1; ++i) load_pair();
-    wait_loads<4 * (kStages - 1)>();
+    load_pair();
+    load_pair();
+    {
+      const int j = sees ? row / G : 0, hq = h * G + (sees ? row % G : 0);
+      const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
+#pragma unroll
+      for (int kb = 0; kb < 8; ++kb)
+        Q[kb] = __builtin_bit_cast(bf16x8, sees ? reinterpret_cast<const uint4 *>(q)[2 * kb + half] : make_uint4(0u, 0u, 0u, 0u));
+      bool bad = false;
+      for (int e = (k_beg >> L.shift) + (int)threadIdx.x; e <= (k_end - 1) >> L.shift; e += 64 * kWaves)
+        bad |= (uint32_t)p.pages.page_table[(int64_t)s * p.pages.max_pages + e] >= (uint32_t)p.pages.num_pages;
+      bad = __any(bad);
+      if (lane == 0) bad_pages[wave] = bad;
+#pragma unroll
+      for (int kb = 0; kb < 8; ++kb) asm volatile("" : "+v"(Q[kb]));
+    }
+    wait_loads<8>();
     barrier();
-    if (mine(k_beg)) scores(stage_of(0));
+    any_bad = __any(lane < kWaves && bad_pages[lane & (kWaves - 1)]);
+    if (any_bad && threadIdx.x == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+    scores(stage_of(0));
     if (second) {
-      wait_loads<4 * (kStages - 2)>();
+      wait_loads<4>();
       inspect(1, k_beg);
       barrier();
     }
@@ -353,27 +358,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
       const uint32_t bad = bad_of(k);
       const uint32_t T = stage_of(st);
       const bool own = mine(k), after = mine(k + kKeys) && k + kKeys < k_end;
-      if (second) load_pair();
-      if (own) softmax(k, bad);
+      load_pair();
+      if (own) {
+        softmax(k, bad);
+      } else {
+        W[0] = W[1] = W[2] = W[3] = bf16x8{};
+      }
       if (!second) {
-        wait_loads<4 * (kStages - 2)>();
+        wait_loads<8>();
         inspect(st, k);
       }
       barrier();
-      if (!second) load_pair();
       __builtin_amdgcn_s_setprio(1);
-      if (own) {
-        keep_notes(st, k, bad);
+      if (own) keep_notes(st, k, bad);
+      if (own || after) {  // (one path: a tile that this wave's rows do not see has weights of zero, and values looked through)
+        scores(T);
         sums(T + kTile);
+        feed();
       }
-      if (after) scores(T);
       __builtin_amdgcn_s_setprio(0);
       if (second) {
-        wait_loads<4 * (kStages - 2)>();
-        inspect(st == kStages - 1 ? 0 : st + 1, k + kKeys);
+        wait_loads<4>();
+        inspect((st + 1) % kStages, k + kKeys);
       }
       barrier();
-      st = st == kStages - 1 ? 0 : st + 1;
+      st = (st + 1) % kStages;
     }
     if (!second) barrier();
     wait_loads<0>();
