@@ -24,24 +24,21 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kKeys = 64;                 // keys per tile
 constexpr int kTile = kKeys * kRowBytes;  // bytes of its K, or of its V
 constexpr int kStage = 2 * kTile;
-constexpr int kStages = 4;
-constexpr int kWaves = 8;
+constexpr int kStages = 2;
+constexpr int kWaves = 4;
+constexpr int kPart = kKeys / kWaves;       // rows of a tile that a wave loads
 constexpr float kLazy = 8.0f;
 
-// The order of a step's products and their reads of LDS: 16 products with one read each, 16 with two, the
-// operands of four products on their way, no more, so that the registers suffice.
+// The order of 16 products and their READS of LDS each: the operands of four products on their way, no more, so
+// that the registers suffice.
+template <int READS>
 __device__ __forceinline__ void feed() {
   constexpr int kRead = 0x100, kProduct = 0x008;
-  __builtin_amdgcn_sched_group_barrier(kRead, 4, 0);
+  __builtin_amdgcn_sched_group_barrier(kRead, 4 * READS, 0);
 #pragma unroll
   for (int i = 0; i < 12; ++i) {
     __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
   }
   __builtin_amdgcn_sched_group_barrier(kProduct, 4, 0);
 }
@@ -134,25 +131,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
 
   // this wave's part of a tile: rows 8 wave .. + 7, four rows a load, of K and of V
   const uint32_t rs = (uint32_t)p.pages.row_stride * 2u;
-  uint32_t off[2];
+  uint32_t off[kPart / 4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = 8 * wave + 4 * i + (lane >> 4);
+  for (int i = 0; i < kPart / 4; ++i) {
+    const int r = kPart * wave + 4 * i + (lane >> 4);
     off[i] = (uint32_t)(lane >> 4) * rs + (uint32_t)((lane & 15) ^ chunk_turn(r)) * 16u;
   }
   const int64_t head = (int64_t)h * p.pages.head_stride;
   // (past the range: some page of it.  What is loaded there is not used, but each step loads the same number of times.)
   auto page_of = [&](int k) -> int { return table[min(k, k_end - 1) >> L.shift]; };
   // Step t reads V of tile t and K of tile t + 1: they travel together, in stage (t + 1) % kStages, K first.
-  const uint32_t part = 8 * wave * kRowBytes;
+  const uint32_t part = kPart * wave * kRowBytes;
   auto address = [&](int k, int pg) {
     if ((uint32_t)pg >= (uint32_t)p.pages.num_pages) pg = 0;  // its rows are masked
-    return 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)((k + 8 * wave) & slots) * rs;
+    return 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)((k + kPart * wave) & slots) * rs;
   };
   auto load_tile = [&](const uint16_t *pool, int64_t at, uint32_t to) {
     const uint8_t *x = reinterpret_cast<const uint8_t *>(pool) + at;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) load_lds16(to + i * 4 * kRowBytes, x + (int64_t)(4 * i) * rs, off[i]);
+    for (int i = 0; i < kPart / 4; ++i) load_lds16(to + i * 4 * kRowBytes, x + (int64_t)(4 * i) * rs, off[i]);
   };
 
   // LDS addresses within a tile: K operand row c, dims 16 kb + 8 half at ka ^ 32 kb; V operand rows
@@ -258,8 +255,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     if (!partial(k, bad)) return;
     bool any = false;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = 8 * wave + (lane >> 4) + 4 * i;
+    for (int i = 0; i < kPart / 4; ++i) {
+      const int r = kPart * wave + (lane >> 4) + 4 * i;
       const uint32_t at = stage_of(stage) + kTile + r * kRowBytes + (lane & 15) * 16;
       u32x4 v = lds_read<u32x4>(at);
       uint32_t note = 0;
@@ -306,29 +303,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   };
 
   if (k_beg < k_end) {
-    // Waves 0-3 and 4-7 (one of each a SIMD) alternate: while the one half forms its weights, the other
-    // half's products run.  Step t: weights of tile t, barrier, scores of K of t + 1 and sums over V of t, barrier;
-    // the second half is one barrier behind.  Tile t's pair (V of t, K of t + 1) is waited for before the barrier
-    // that the first half's products follow; its stage is free two barriers later, and is written again by
-    // loads that a step between issues at its start (so that the products' phase holds nothing else).
-    const bool second = wave >= kWaves / 2;
-    int next_k = k_beg;   // first key of the V tile of the pair to load next
-    int pg = page_of(k_beg + kKeys + 8 * wave);               // page of the K tile behind it
-    int64_t vat = address(k_beg, page_of(k_beg + 8 * wave));  // where the V tile lies
-    int load_stage = 1;
-    load_tile(L.K, vat, tiles_at + part);
-    auto load_pair = [&]() {
-      const uint32_t to = stage_of(load_stage) + part;
-      const int64_t kat = address(next_k + kKeys, pg);
-      load_tile(L.K, kat, to);
-      load_tile(L.V, vat, to + kTile);
-      vat = kat;
-      next_k += kKeys;
-      pg = page_of(next_k + kKeys + 8 * wave);
-      load_stage = (load_stage + 1) % kStages;
+    int pg = page_of(k_beg + kPart * wave);
+    auto load = [&](int k, int stage) {
+      const int64_t at = address(k, pg);
+      load_tile(L.K, at, stage_of(stage) + part);
+      load_tile(L.V, at, stage_of(stage) + kTile + part);
+      pg = page_of(k + kKeys + kPart * wave);
     };
-    load_pair();
-    load_pair();
+    load(k_beg, 0);
     {
       const int j = sees ? row / G : 0, hq = h * G + (sees ? row % G : 0);
       const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
@@ -343,49 +325,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
 #pragma unroll
       for (int kb = 0; kb < 8; ++kb) asm volatile("" : "+v"(Q[kb]));
     }
-    wait_loads<8>();
     barrier();
     any_bad = __any(lane < kWaves && bad_pages[lane & (kWaves - 1)]);
     if (any_bad && threadIdx.x == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
-    scores(stage_of(0));
-    if (second) {
-      wait_loads<4>();
-      inspect(1, k_beg);
-      barrier();
-    }
-    int st = 1;  // stage of this step's pair
-    for (int k = k_beg; k < k_end; k += kKeys) {
-      const uint32_t bad = bad_of(k);
-      const uint32_t T = stage_of(st);
-      const bool own = mine(k), after = mine(k + kKeys) && k + kKeys < k_end;
-      load_pair();
-      if (own) {
-        softmax(k, bad);
-      } else {
-        W[0] = W[1] = W[2] = W[3] = bf16x8{};
-      }
-      if (!second) {
-        wait_loads<8>();
-        inspect(st, k);
-      }
-      barrier();
+    int st = 0;
+    for (int k = k_beg; k < k_end; k += kKeys, st ^= 1) {
+      wait_loads<0>();
+      inspect(st, k);
+      barrier();  // the tile is here, and the other stage has been read
+      if (k + kKeys < k_end) load(k + kKeys, st ^ 1);
+      if (!mine(k)) continue;
+      const uint32_t bad = bad_of(k), T = stage_of(st);
+      keep_notes(st, k, bad);
       __builtin_amdgcn_s_setprio(1);
-      if (own) keep_notes(st, k, bad);
-      if (own || after) {  // (one path: a tile that this wave's rows do not see has weights of zero, and values looked through)
-        scores(T);
-        sums(T + kTile);
-        feed();
-      }
+      scores(T);
+      feed<1>();
       __builtin_amdgcn_s_setprio(0);
-      if (second) {
-        wait_loads<4>();
-        inspect((st + 1) % kStages, k + kKeys);
-      }
-      barrier();
-      st = (st + 1) % kStages;
+      softmax(k, bad);
+      __builtin_amdgcn_s_setprio(1);
+      sums(T + kTile);
+      feed<2>();
+      __builtin_amdgcn_s_setprio(0);
     }
-    if (!second) barrier();
-    wait_loads<0>();
     if (poisoned) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) {

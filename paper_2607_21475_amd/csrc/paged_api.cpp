@@ -68,7 +68,7 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split until there are
 // 256 work-groups, one a CU; a split holds at least a tile for each wave (attend_rows) or eight tiles.
-constexpr int64_t kGroups = 256;
+constexpr int64_t kGroups = 512;
 constexpr int64_t kRowsLeast = 128;
 constexpr int64_t kTilesLeast = 512;
 AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
