@@ -45,7 +45,6 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   constexpr int kMerge = kRows * (kMergeRow * 4 + 8);  // a wave's sums and statistics, when the waves combine
   constexpr int kPoison = kRowsStages * 2 * kTileBytes;  // (read before the waves combine)
   constexpr int kWaveLds = kPoison + kRows * kHeadDim > kMerge ? kPoison + kRows * kHeadDim : kMerge;
-  constexpr int kPair = NQ < 2 ? 1 : 2;
   __shared__ __align__(1024) uint8_t lds[kRowsWaves * kWaveLds];
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
@@ -66,30 +65,11 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   Span span[NQ];
 #pragma unroll
   for (int b = 0; b < NQ; ++b) span[b] = span_of(p, sq, row0 + 16 * b + c);
-  const Range R = range_of<NQ>(span);
+  const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, row0 / G, (row0 + nrow - 1) / G);
   // this split's keys
   const int64_t start = (R.lo & -kTileKeys) + (int64_t)sp * L.split_rows;
   const int k_end = start < R.hi ? (int)min((int64_t)R.hi, start + L.split_rows) : 0;
   const int k_beg = start < R.hi ? (int)start : 0;  // rows stay below 2^30: no sum below overflows
-
-  bf16x8 Q[NQ][4];  // B operand: column c of block b is query row 16 b + c
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    const int row = row0 + 16 * b + c;
-    const bool ok = span[b].lo < span[b].hi;
-    const int j = ok ? row / G : 0, hq = h * G + (ok ? row % G : 0);
-    const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb)
-      Q[b][kb] = __builtin_bit_cast(bf16x8, ok ? reinterpret_cast<const uint4 *>(q)[4 * kb + g] : make_uint4(0u, 0u, 0u, 0u));
-  }
-
-  // the queries are here before any tile is asked for: a wait for them in the loop would be one for all loads
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) asm volatile("" : "+v"(Q[b][kb]));
-  }
 
   f32x4 O[NQ][8];
   float m[NQ], z[NQ];
@@ -153,6 +133,25 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     bad = issue(k, page_of(k), page_of(k + 16), 0);
     pg0 = page_of(k + stride), pg1 = page_of(k + stride + 16);
   }
+  bf16x8 Q[NQ][4];  // B operand: column c of block b is query row 16 b + c
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    const int row = row0 + 16 * b + c;
+    const bool ok = span[b].lo < span[b].hi;
+    const int j = ok ? row / G : 0, hq = h * G + (ok ? row % G : 0);
+    const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+      Q[b][kb] = __builtin_bit_cast(bf16x8, ok ? reinterpret_cast<const uint4 *>(q)[4 * kb + g] : make_uint4(0u, 0u, 0u, 0u));
+  }
+
+  // (asked for behind the first tile, and here before the next: a wait for them in the loop would be one for all loads)
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) asm volatile("" : "+v"(Q[b][kb]));
+  }
+
   for (; k < k_end; k += stride, stage ^= 1) {
     uint32_t next_bad = 0;
     if (k + stride < k_end) {
@@ -219,68 +218,62 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
         wave_sync();
       }
     }
-    // two blocks of query rows at a time: more would not fit the registers, and the tile's second reads from
-    // LDS cost nothing beside the memory's
+    f32x4 S[NQ][2];
 #pragma unroll
-    for (int b0 = 0; b0 < NQ; b0 += kPair) {
-      if (b0) asm volatile("" ::: "memory");
-      f32x4 S[kPair][2];
+    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int b = 0; b < NQ; ++b) S[b][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int b = 0; b < kPair; ++b) S[b][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int kb = 0; kb < 4; ++kb) {
+        const bf16x8 A = *reinterpret_cast<const bf16x8 *>(Kt + (16 * t + c) * kRowBytes + ((4 * kb + g) ^ c) * 16);
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-          const bf16x8 A = *reinterpret_cast<const bf16x8 *>(Kt + (16 * t + c) * kRowBytes + ((4 * kb + g) ^ c) * 16);
-#pragma unroll
-          for (int b = 0; b < kPair; ++b)
-            S[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Q[b0 + b][kb], S[b][t], 0, 0, 0);
-        }
+        for (int b = 0; b < NQ; ++b)
+          S[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Q[b][kb], S[b][t], 0, 0, 0);
       }
-      float w[kPair][8];
-      bf16x8 hi[kPair], lo[kPair];
+    }
+    float w[NQ][8];
+    bf16x8 hi[NQ], lo[NQ];
 #pragma unroll
-      for (int b = 0; b < kPair; ++b) {
-        const int B = b0 + b, own_hi = min(span[B].hi, k_end);
-        auto visible = [&](int i) {
-          const int key = k + 16 * (i / 4) + 4 * g + i % 4;
-          return (key >= span[B].lo) & (key < own_hi) & !((bad >> (i / 4)) & 1u);
-        };
+    for (int b = 0; b < NQ; ++b) {
+      const int own_hi = min(span[b].hi, k_end);
+      auto visible = [&](int i) {
+        const int key = k + 16 * (i / 4) + 4 * g + i % 4;
+        return (key >= span[b].lo) & (key < own_hi) & !((bad >> (i / 4)) & 1u);
+      };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[b][i] = S[b][i / 4][i % 4] * sc2;
-        if (mixed) {
+      for (int i = 0; i < 8; ++i) w[b][i] = S[b][i / 4][i % 4] * sc2;
+      if (mixed) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[b][i] = visible(i) ? w[b][i] : -INFINITY;
-        }
-        float t = fmaxf(fmaxf(fmaxf(w[b][0], w[b][1]), fmaxf(w[b][2], w[b][3])),
-                        fmaxf(fmaxf(w[b][4], w[b][5]), fmaxf(w[b][6], w[b][7])));
-        t = max_xor16_32(t);
-        if (__any(t > m[B])) {
-          const float mn = fmaxf(m[B], t);
-          const float a = mn == -INFINITY ? 1.0f : fast_exp2(m[B] - mn);
-          m[B] = mn;
-          z[B] *= a;
-#pragma unroll
-          for (int d = 0; d < 8; ++d) O[B][d] *= a;
-        }
-        const float mu = m[B] == -INFINITY ? 0.0f : m[B];  // nothing seen yet: every l is -inf
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          w[b][i] = fast_exp2(w[b][i] - mu);
-          z[B] += w[b][i];
-          hi[b][i] = (__bf16)w[b][i];
-          lo[b][i] = (__bf16)(w[b][i] - (float)hi[b][i]);
-        }
+        for (int i = 0; i < 8; ++i) w[b][i] = visible(i) ? w[b][i] : -INFINITY;
       }
+      float t = fmaxf(fmaxf(fmaxf(w[b][0], w[b][1]), fmaxf(w[b][2], w[b][3])),
+                      fmaxf(fmaxf(w[b][4], w[b][5]), fmaxf(w[b][6], w[b][7])));
+      t = max_xor16_32(t);
+      if (__any(t > m[b])) {
+        const float mn = fmaxf(m[b], t);
+        const float a = mn == -INFINITY ? 1.0f : fast_exp2(m[b] - mn);
+        m[b] = mn;
+        z[b] *= a;
 #pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        const bf16x8 A = values(d);
+        for (int d = 0; d < 8; ++d) O[b][d] *= a;
+      }
+      const float mu = m[b] == -INFINITY ? 0.0f : m[b];  // nothing seen yet: every l is -inf
 #pragma unroll
-        for (int b = 0; b < kPair; ++b) {
-          f32x4 &o = O[b0 + b][d];
-          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, lo[b], o, 0, 0, 0);
-          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, hi[b], o, 0, 0, 0);
-        }
+      for (int i = 0; i < 8; ++i) {
+        w[b][i] = fast_exp2(w[b][i] - mu);
+        z[b] += w[b][i];
+        hi[b][i] = (__bf16)w[b][i];
+        lo[b][i] = (__bf16)(w[b][i] - (float)hi[b][i]);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      const bf16x8 A = values(d);
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        f32x4 &o = O[b][d];
+        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, lo[b], o, 0, 0, 0);
+        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, hi[b], o, 0, 0, 0);
       }
     }
     bad_any |= bad;
@@ -408,11 +401,10 @@ int64_t attend_paged_groups(const AttendPagedLaunch &L) {
 }
 
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
-  if (L.rows == kTileRows) return launch_attend_tiles(L, s);
+  if (L.rows > kRowsKernelMax) return launch_attend_tiles(L, s);
   const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
   if (L.rows == 16) hipLaunchKernelGGL(attend_rows_kernel<1>, grid, block, 0, s, L);
-  else if (L.rows == 32) hipLaunchKernelGGL(attend_rows_kernel<2>, grid, block, 0, s, L);
-  else hipLaunchKernelGGL(attend_rows_kernel<4>, grid, block, 0, s, L);
+  else hipLaunchKernelGGL(attend_rows_kernel<2>, grid, block, 0, s, L);
   return hipGetLastError();
 }
 

@@ -21,22 +21,16 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kKeys = 64;                 // keys per tile
-constexpr int kTile = kKeys * kRowBytes;  // bytes of its K, or of its V
-constexpr int kStage = 2 * kTile;
-constexpr int kStages = 2;
-constexpr int kWaves = 4;
-constexpr int kPart = kKeys / kWaves;       // rows of a tile that a wave loads
 constexpr float kLazy = 8.0f;
 
-// The order of 16 products and their READS of LDS each: the operands of four products on their way, no more, so
+// The order of N products and their READS of LDS each: the operands of four products on their way, no more, so
 // that the registers suffice.
-template <int READS>
+template <int N, int READS>
 __device__ __forceinline__ void feed() {
   constexpr int kRead = 0x100, kProduct = 0x008;
   __builtin_amdgcn_sched_group_barrier(kRead, 4 * READS, 0);
 #pragma unroll
-  for (int i = 0; i < 12; ++i) {
+  for (int i = 0; i < N - 4; ++i) {
     __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
     __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
   }
@@ -76,13 +70,23 @@ __device__ __forceinline__ float max_halves(float x) {
 
 }  // namespace
 
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
-  __shared__ __align__(1024) uint8_t tiles[kStages * kStage];
-  __shared__ uint32_t poisons[kWaves][32][8];     // of each query row, two bits an element
-  __shared__ uint16_t notes[kStages][kKeys][16];  // of a tile's values, 16 bits a chunk
-  __shared__ int noted[kStages][kWaves];          // ... whether a wave noted any
+// RW waves of 32 query rows each, KG groups of them that take every KG'th tile of KEYS keys.
+template <int RW, int KG, int KEYS>
+__global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
+  constexpr int kWaves = RW * KG, kRows = 32 * RW;
+  constexpr int kSub = KEYS / 32;             // blocks of 32 keys of a tile
+  constexpr int kPart = KEYS / RW;            // rows of a tile that a wave loads
+  constexpr int kTile = KEYS * kRowBytes;     // bytes of a tile's K, or of its V
+  constexpr int kStage = KG * 2 * kTile;
+  constexpr int kMergeRow = 132;              // floats of a row's sums in LDS, padded
+  constexpr int kMerge = KG > 1 ? KG * kRows * kMergeRow * 4 : 0;
+  __shared__ __align__(1024) uint8_t tiles[2 * kStage > kMerge ? 2 * kStage : kMerge];
+  __shared__ uint32_t poisons[kWaves][32][8];   // of each query row, two bits an element
+  __shared__ uint16_t notes[2][KG][KEYS][16];   // of a tile's values, 16 bits a chunk
+  __shared__ int noted[2][KG][RW];              // ... whether a wave noted any
   __shared__ Range ranges[kWaves];
   __shared__ int bad_pages[kWaves];
+  __shared__ float2 merged[KG > 1 ? KG : 1][kRows];  // maximum and total weight of a group's rows
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
   // heads vary fastest (work-groups go round the XCDs: a head's stay together for 8, 4, 2 heads and
@@ -96,18 +100,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   const int lane = threadIdx.x & 63, half = lane >> 5, c = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
+  const int rw = wave % RW, kg = wave / RW;
+
   const Seq sq = sequence(p, s);
-  const int row0 = rb * 32 * kWaves, nrow = min(32 * kWaves, sq.tokens * G - row0);
+  const int row0 = rb * kRows, nrow = min(kRows, sq.tokens * G - row0);
   if (threadIdx.x == 0 && rb == 0 && sp == 0 && h == 0 && L.status && sq.status) atomicOr(&L.status[s], sq.status);
   if (nrow <= 0) return;
 
   // what this wave's rows see, and the work-group's
-  const int row = row0 + 32 * wave + c;
+  const int row = row0 + 32 * rw + c;
   Span span[1] = {span_of(p, sq, row)};
   const bool sees = span[0].lo < span[0].hi;
   Range R, all;
   if (!p.qpos) {
-    R = range_of_tokens(p, sq, (row0 + 32 * wave) / G, (row0 + 32 * wave + 31) / G);
+    R = range_of_tokens(p, sq, (row0 + 32 * rw) / G, (row0 + 32 * rw + 31) / G);
     all = range_of_tokens(p, sq, row0 / G, (row0 + nrow - 1) / G);
   } else {
     R = range_of<1>(span);
@@ -115,36 +121,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     __syncthreads();
     all = ranges[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
+    for (int w = 1; w < RW; ++w) {
       all.lo = min(all.lo, ranges[w].lo), all.hi = max(all.hi, ranges[w].hi);
       all.every_lo = max(all.every_lo, ranges[w].every_lo), all.every_hi = min(all.every_hi, ranges[w].every_hi);
     }
   }
   R = uniform(R);
   all = uniform(all);
-  const int64_t start = (all.lo & -kKeys) + (int64_t)sp * L.split_rows;
+  const int64_t start = (all.lo & -KEYS) + (int64_t)sp * L.split_rows;
   const int k_end = start < all.hi ? (int)min((int64_t)all.hi, start + L.split_rows) : 0;
   const int k_beg = start < all.hi ? (int)start : 0;
   const int every_lo = all.every_lo, every_hi = min(all.every_hi, k_end);
   const const_i32 *table = (const const_i32 *)(p.pages.page_table + (int64_t)s * p.pages.max_pages);
   const int slots = p.pages.page_size - 1;
 
-  // this wave's part of a tile: rows 8 wave .. + 7, four rows a load, of K and of V
+  // this wave's part of a tile: kPart rows, four rows a load, of K and of V
   const uint32_t rs = (uint32_t)p.pages.row_stride * 2u;
   uint32_t off[kPart / 4];
 #pragma unroll
   for (int i = 0; i < kPart / 4; ++i) {
-    const int r = kPart * wave + 4 * i + (lane >> 4);
+    const int r = kPart * rw + 4 * i + (lane >> 4);
     off[i] = (uint32_t)(lane >> 4) * rs + (uint32_t)((lane & 15) ^ chunk_turn(r)) * 16u;
   }
   const int64_t head = (int64_t)h * p.pages.head_stride;
   // (past the range: some page of it.  What is loaded there is not used, but each step loads the same number of times.)
   auto page_of = [&](int k) -> int { return table[min(k, k_end - 1) >> L.shift]; };
-  // Step t reads V of tile t and K of tile t + 1: they travel together, in stage (t + 1) % kStages, K first.
-  const uint32_t part = kPart * wave * kRowBytes;
+  const uint32_t part = kPart * rw * kRowBytes;
   auto address = [&](int k, int pg) {
     if ((uint32_t)pg >= (uint32_t)p.pages.num_pages) pg = 0;  // its rows are masked
-    return 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)((k + kPart * wave) & slots) * rs;
+    return 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)((k + kPart * rw) & slots) * rs;
   };
   auto load_tile = [&](const uint16_t *pool, int64_t at, uint32_t to) {
     const uint8_t *x = reinterpret_cast<const uint8_t *>(pool) + at;
@@ -170,36 +175,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   const float sc2 = L.scale * kLog2e;
 
   const uint32_t tiles_at = lds_at(tiles);
-  auto stage_of = [&](int i) { return tiles_at + i * kStage; };
+  auto tile_of = [&](int stage) { return tiles_at + stage * kStage + kg * 2 * kTile; };  // this group's
   const int own_hi = min(span[0].hi, k_end);
   uint32_t(*poison)[8] = poisons[wave];
   bool poisoned = false;
-  f32x16 S[2];
+  f32x16 S[kSub];
   bf16x8 Q[8];  // B operand: column c is this lane's query row, dims 16 kb + 8 half .. + 7
-  bf16x8 W[4];  // weights, the B operand of the sums
+  bf16x8 W[2 * kSub];  // weights, the B operand of the sums
   bool any_bad = false;
 
   auto keys = [&](uint32_t Kt, int i) {
-    return lds_read<bf16x8>(((Kt + ka) ^ (32 * (i / 2))) + (i % 2) * 32 * kRowBytes);
+    return lds_read<bf16x8>(((Kt + ka) ^ (32 * (i / kSub))) + (i % kSub) * 32 * kRowBytes);
   };
   auto values = [&](uint32_t Vt, int i) {
     const uint32_t d = 64 * (i % 4), ks = (i / 4) * 16 * kRowBytes;
     return join8(lds_read_transposed(((Vt + va[0]) ^ d) + ks), lds_read_transposed(((Vt + va[1]) ^ d) + ks));
   };
   auto scores = [&](uint32_t Kt) {
-    S[0] = S[1] = f32x16{};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) S[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys(Kt, i), Q[i / 2], S[i % 2], 0, 0, 0);
+    for (int b = 0; b < kSub; ++b) S[b] = f32x16{};
+#pragma unroll
+    for (int i = 0; i < 8 * kSub; ++i)
+      S[i % kSub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys(Kt, i), Q[i / kSub], S[i % kSub], 0, 0, 0);
   };
   auto sums = [&](uint32_t Vt) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(Vt, i), W[i / 4], O[i % 4], 0, 0, 0);
+    for (int i = 0; i < 8 * kSub; ++i) O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(Vt, i), W[i / 4], O[i % 4], 0, 0, 0);
   };
-  auto mixed = [&](int k, uint32_t bad) { return bad || k < R.every_lo || k + kKeys > min(R.every_hi, k_end); };
+  auto mixed = [&](int k, uint32_t bad) { return bad || k < R.every_lo || k + KEYS > min(R.every_hi, k_end); };
   auto softmax = [&](int k, uint32_t bad) {
     if (mixed(k, bad)) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < kSub; ++b) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = k + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
@@ -208,14 +215,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
         }
       }
     }
-    // (the first maxima read both accumulators' last products, which the compiler waits for, and the rest
-    // depend on them)
-    float t0 = fmaxf(S[0][0], S[1][0]), t1 = fmaxf(S[0][1], S[1][1]);
-    t1 = fmaxf(t1, t0);
+    // (the first maximum reads every accumulator's last products, which the compiler waits for, and the rest
+    // depend on it)
+    float t0 = fmaxf(S[0][0], S[kSub - 1][1]), t1 = fmaxf(fmaxf(S[0][1], S[kSub - 1][0]), t0);
 #pragma unroll
-    for (int i = 2; i < 16; i += 2) {
-      t0 = max3(t0, S[0][i], S[0][i + 1]);
-      t1 = max3(t1, S[1][i], S[1][i + 1]);
+    for (int i = 2; i < 16 * kSub; i += 4) {
+      t0 = max3(t0, S[i / 16][i % 16], S[i / 16][i % 16 + 1]);
+      if (i + 2 < 16 * kSub) t1 = max3(t1, S[(i + 2) / 16][(i + 2) % 16], S[(i + 2) / 16][(i + 2) % 16 + 1]);
     }
     const float t = max_halves(fmaxf(t0, t1)) * sc2;
     if (__any(t > m + kLazy)) {
@@ -228,7 +234,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     }
     const float mu = m == -INFINITY ? 0.0f : m;  // nothing seen yet: every score is -inf
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kSub; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float w = fast_exp2(__builtin_fmaf(S[b][i], sc2, -mu));
@@ -241,7 +247,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     uint32_t bad = 0;
     if (any_bad) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b) bad |= (uint32_t)((uint32_t)page_of(k + 16 * b) >= (uint32_t)p.pages.num_pages) << b;
+      for (int b = 0; b < 2 * kSub; ++b) bad |= (uint32_t)((uint32_t)page_of(k + 16 * b) >= (uint32_t)p.pages.num_pages) << b;
     }
     return bad;
   };
@@ -249,15 +255,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   // query row sees in part, each wave looks through the values that it loaded: rows that none may see become
   // zeros, and elsewhere what is not finite becomes zero and is noted, two bits an element; then
   // the waves whose query rows see such a key keep the notes (poison), and add them to their sums at the end.
-  auto partial = [&](int k, uint32_t bad) { return bad || k < every_lo || k + kKeys > every_hi; };
+  auto partial = [&](int k, uint32_t bad) { return bad || k < every_lo || k + KEYS > every_hi; };
   auto inspect = [&](int stage, int k) {
     const uint32_t bad = bad_of(k);
     if (!partial(k, bad)) return;
     bool any = false;
 #pragma unroll
     for (int i = 0; i < kPart / 4; ++i) {
-      const int r = kPart * wave + (lane >> 4) + 4 * i;
-      const uint32_t at = stage_of(stage) + kTile + r * kRowBytes + (lane & 15) * 16;
+      const int r = kPart * rw + (lane >> 4) + 4 * i;
+      const uint32_t at = tile_of(stage) + kTile + r * kRowBytes + (lane & 15) * 16;
       u32x4 v = lds_read<u32x4>(at);
       uint32_t note = 0;
       if (k + r >= k_end || ((bad >> (r / 16)) & 1u)) {
@@ -270,23 +276,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
           note |= (n0 | n1 << 2) << (4 * e);
         }
       }
-      notes[stage][r][(lane & 15) ^ chunk_turn(r)] = (uint16_t)note;
+      notes[stage][kg][r][(lane & 15) ^ chunk_turn(r)] = (uint16_t)note;
       lds_write(at, v);
       any |= note != 0u;
     }
     any = __any(any);
-    if (lane == 0) noted[stage][wave] = any;
+    if (lane == 0) noted[stage][kg][rw] = any;
   };
   auto keep_notes = [&](int stage, int k, uint32_t bad) {
-    if (!partial(k, bad) || !__any(lane < kWaves && noted[stage][lane & (kWaves - 1)])) return;
+    if (!partial(k, bad) || !__any(lane < RW && noted[stage][kg][lane & (RW - 1)])) return;
     if (!poisoned) {
       for (int i = lane; i < 256; i += 64) poison[0][i] = 0u;
       poisoned = true;
     }
     wave_sync();
 #pragma unroll 1
-    for (int r = 0; r < kKeys; ++r) {
-      const uint32_t note = lane < 16 ? notes[stage][r][lane] : 0u;
+    for (int r = 0; r < KEYS; ++r) {
+      const uint32_t note = lane < 16 ? notes[stage][kg][r][lane] : 0u;
       if (!__any(note)) continue;
 #pragma unroll 1
       for (int j = 0; j < 32; ++j) {
@@ -296,21 +302,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     }
     wave_sync();
   };
-  auto mine = [&](int k) { return k < R.hi && k + kKeys > R.lo; };  // whether this wave's rows see the tile
+  auto mine = [&](int k) { return k < min(R.hi, k_end) && k + KEYS > R.lo; };  // whether this wave's rows see the tile
   auto barrier = [&]() {
     wait_lds();
     __builtin_amdgcn_s_barrier();
   };
 
   if (k_beg < k_end) {
-    int pg = page_of(k_beg + kPart * wave);
+    const int step = KG * KEYS;
+    int k = k_beg + kg * KEYS;  // this group's tile
+    int pg = page_of(k + kPart * rw);
     auto load = [&](int k, int stage) {
       const int64_t at = address(k, pg);
-      load_tile(L.K, at, stage_of(stage) + part);
-      load_tile(L.V, at, stage_of(stage) + kTile + part);
-      pg = page_of(k + kKeys + kPart * wave);
+      load_tile(L.K, at, tile_of(stage) + part);
+      load_tile(L.V, at, tile_of(stage) + kTile + part);
+      pg = page_of(k + step + kPart * rw);
     };
-    load(k_beg, 0);
+    load(k, 0);
     {
       const int j = sees ? row / G : 0, hq = h * G + (sees ? row % G : 0);
       const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
@@ -329,22 +337,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
     any_bad = __any(lane < kWaves && bad_pages[lane & (kWaves - 1)]);
     if (any_bad && threadIdx.x == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
     int st = 0;
-    for (int k = k_beg; k < k_end; k += kKeys, st ^= 1) {
+    for (int first = k_beg; first < k_end; first += step, k += step, st ^= 1) {
       wait_loads<0>();
       inspect(st, k);
-      barrier();  // the tile is here, and the other stage has been read
-      if (k + kKeys < k_end) load(k + kKeys, st ^ 1);
+      barrier();  // the tiles are here, and the other stage has been read
+      if (first + step < k_end) load(k + step, st ^ 1);
       if (!mine(k)) continue;
-      const uint32_t bad = bad_of(k), T = stage_of(st);
+      const uint32_t bad = bad_of(k), T = tile_of(st);
       keep_notes(st, k, bad);
       __builtin_amdgcn_s_setprio(1);
       scores(T);
-      feed<1>();
+      feed<8 * kSub, 1>();
       __builtin_amdgcn_s_setprio(0);
       softmax(k, bad);
       __builtin_amdgcn_s_setprio(1);
       sums(T + kTile);
-      feed<2>();
+      feed<8 * kSub, 2>();
       __builtin_amdgcn_s_setprio(0);
     }
     if (poisoned) {
@@ -361,16 +369,56 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
   }
 
   z += __shfl_xor(z, 32);
-  if (32 * wave + c >= nrow) return;
-  const int64_t slot = ((((int64_t)s * H + h) * L.blocks + rb) * L.nsplit + sp) * (32 * kWaves) + 32 * wave + c;
+  const int64_t slot = ((((int64_t)s * H + h) * L.blocks + rb) * L.nsplit + sp) * kRows;
+  if constexpr (KG > 1) {
+    // the groups' sums, combined in order
+    __syncthreads();
+    float *sums_of = reinterpret_cast<float *>(tiles);  // [KG][kRows][kMergeRow]
+    float *Ow = sums_of + (kg * kRows + 32 * rw + c) * kMergeRow + 4 * half;
+    if (half == 0) merged[kg][32 * rw + c] = sees ? make_float2(m, z) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4 *>(Ow + 32 * d + 8 * j) = f32x4{O[d][4 * j], O[d][4 * j + 1], O[d][4 * j + 2], O[d][4 * j + 3]};
+    }
+    __syncthreads();
+    const int e = (threadIdx.x & 15) * 8;
+    for (int r = threadIdx.x >> 4; r < nrow; r += 4 * kWaves) {
+      float M = -INFINITY, Z = 0.0f, o[8] = {};
+#pragma unroll
+      for (int v = 0; v < KG; ++v) M = fmaxf(M, merged[v][r].x);
+#pragma unroll
+      for (int v = 0; v < KG; ++v) {
+        const float2 t = merged[v][r];
+        if (t.x == -INFINITY) continue;  // this group saw nothing of the row
+        const float a = fast_exp2(t.x - M);
+        Z += a * t.y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] += a * sums_of[(v * kRows + r) * kMergeRow + e + i];
+      }
+      if (L.nsplit > 1) {
+        if (e == 0) L.stats[slot + r] = make_float2(M, Z);
+        if (M == -INFINITY) continue;
+        float *part_of = L.part + (slot + r) * kHeadDim + e;
+        *reinterpret_cast<f32x4 *>(part_of) = f32x4{o[0], o[1], o[2], o[3]};
+        *reinterpret_cast<f32x4 *>(part_of + 4) = f32x4{o[4], o[5], o[6], o[7]};
+      } else {
+        store_row(L, sq.t0 + (row0 + r) / G, h * G + (row0 + r) % G, e, M, Z, o);
+      }
+    }
+    return;
+  }
+  const int r = 32 * rw + c;
+  if (r >= nrow) return;
   if (L.nsplit > 1) {
-    if (half == 0) L.stats[slot] = sees ? make_float2(m, z) : make_float2(-INFINITY, 0.0f);
+    if (half == 0) L.stats[slot + r] = sees ? make_float2(m, z) : make_float2(-INFINITY, 0.0f);
     if (!sees || m == -INFINITY) return;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4 *>(L.part + slot * kHeadDim + 32 * d + 8 * j + 4 * half) =
+        *reinterpret_cast<f32x4 *>(L.part + (slot + r) * kHeadDim + 32 * d + 8 * j + 4 * half) =
             f32x4{O[d][4 * j], O[d][4 * j + 1], O[d][4 * j + 2], O[d][4 * j + 3]};
     }
     return;
@@ -394,7 +442,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tiles_kernel(AttendPage
 }
 
 hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {
-  hipLaunchKernelGGL(attend_tiles_kernel, dim3((unsigned)attend_paged_groups(L)), dim3(64 * kWaves), 0, s, L);
+  const dim3 grid((unsigned)attend_paged_groups(L));
+  if (L.rows == kFewRows) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32>), grid, dim3(512), 0, s, L);
+  else hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64>), grid, dim3(256), 0, s, L);
   return hipGetLastError();
 }
 

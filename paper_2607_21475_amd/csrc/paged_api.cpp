@@ -68,14 +68,14 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split until there are
 // 256 work-groups, one a CU; a split holds at least a tile for each wave (attend_rows) or eight tiles.
-constexpr int64_t kGroups = 512;
+constexpr int64_t kGroups = 256;
 constexpr int64_t kRowsLeast = 128;
 constexpr int64_t kTilesLeast = 512;
 AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   AttendPagedLaunch L{};
   L.p = *p;
   const int64_t rows = (int64_t)p->max_new * p->group;
-  L.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= kRowsKernelMax ? 64 : kTileRows;
+  L.rows = rows <= 16 ? 16 : rows <= kRowsKernelMax ? 32 : rows <= kFewRows ? kFewRows : kTileRows;
   const bool tiles = L.rows == kTileRows;
   L.blocks = (int32_t)std::max<int64_t>(1, (rows + L.rows - 1) / L.rows);
   // the most rows a block of query rows sees, from a tile's border on
@@ -83,7 +83,7 @@ AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows / p->group + 1);
   span = std::max<int64_t>(span, 1) + 63;
   const int64_t units = std::max<int64_t>(1, (int64_t)p->pages.num_seqs * p->pages.kv_heads * L.blocks);
-  int64_t ns = std::max<int64_t>(1, kGroups / units);
+  int64_t ns = std::max<int64_t>(1, (tiles ? 2 * kGroups : kGroups) / units);
   ns = std::min<int64_t>(ns, std::max<int64_t>(1, span / (tiles ? kTilesLeast : kRowsLeast)));
   L.split_rows = (int32_t)(((span + ns - 1) / ns + 127) / 128 * 128);
   L.nsplit = (int32_t)((span + L.split_rows - 1) / L.split_rows);

@@ -243,6 +243,9 @@ BITS = 8
     ([600, 511, 90], [300, 1, 90], 2, 4, 64, "tokens", 100),
     ([1000, 40], [1, 1], 2, 16, 256, "heads", 33),
     ([300], [64], 1, 17, 16, "heads", 1),
+    ([900, 33, 40], [8, 5, 0], 2, 8, 16, "heads", 0),
+    ([1500, 70], [20, 20], 1, 3, 32, "tokens", 40),
+    ([500, 31], [9, 7], 3, 3, 64, "heads", 7),
     ([2049, 33], [513, 33], 1, 2, 64, "heads", 700),
     ([64, 0, 5], [64, 0, 5], 2, 1, 16, "heads", 0),
 ])
@@ -257,7 +260,7 @@ def test_attend(lens, news, kv, G, page, order, window):
     assert bool((y[-2:] == 7).all()) and bool((lse[-2:] == 7).all())
 
 
-@pytest.mark.parametrize("news", [[1, 1, 1], [8, 2, 7], [70, 33, 129]])
+@pytest.mark.parametrize("news", [[1, 1, 1], [8, 2, 7], [12, 16, 3], [70, 33, 129]])
 def test_attend_query_positions(news):
     """Positions in any order, padding that sees nothing, positions past the cache; no lse asked for."""
     _say("attend qpos", news)
@@ -279,7 +282,7 @@ def test_attend_query_positions(news):
 
 
 @pytest.mark.parametrize("what", [math.nan, INF, -INF])
-@pytest.mark.parametrize("news,G", [([4], 2), ([16], 1), ([100], 4), ([300], 1)])
+@pytest.mark.parametrize("news,G", [([4], 2), ([16], 1), ([10], 3), ([15], 4), ([100], 4), ([300], 1)])
 def test_attend_unseen_rows_have_no_effect(news, G, what):
     """Keys and values of rows that some query rows see and others do not hold infinities and NaN."""
     _say("attend unseen", news, G, what)
@@ -303,7 +306,7 @@ def test_attend_unseen_rows_have_no_effect(news, G, what):
 
 
 def test_attend_rows_without_a_page():
-    for m in (1, 60):
+    for m in (1, 9, 20, 60):
         c = ref.Cache([200, 90], 2, 32, _gen(8), fill=math.nan)
         c.table[0, 2], c.table[0, 5] = -1, 10 ** 6
         gone = torch.zeros(200, dtype=torch.bool, device="cuda")
@@ -327,7 +330,7 @@ def test_attend_rows_without_a_page():
     assert st.tolist() == [ebd.EBD_ST_BAD_PAGE]
 
 
-@pytest.mark.parametrize("news", [[3, 5], [60, 90]])
+@pytest.mark.parametrize("news", [[3, 5], [16, 20], [25, 30], [60, 90]])
 def test_attend_beyond_the_bounds(news):
     """Sequences with more rows or new tokens than the host said: flagged, the rest as asked."""
     import paper_2607_21475_amd as ebd
@@ -344,7 +347,7 @@ def test_attend_beyond_the_bounds(news):
     ref.check(lse[:2 * t], rl[:2 * t], tl[:2 * t], "lse")
 
 
-@pytest.mark.parametrize("news", [[1], [2], [40], [200]])
+@pytest.mark.parametrize("news", [[1], [2], [7], [13], [40], [200]])
 def test_attend_sharp_and_flat_rows(news):
     """Logits of hundreds (one row takes all), a scale that makes them all alike, rows growing along the cache."""
     g = _gen(8)
