@@ -39,7 +39,7 @@ __device__ __forceinline__ float max_xor16_32(float x) {
 
 }  // namespace
 
-template <int NQ>
+template <int NQ, bool NT>
 __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L) {
   constexpr int kRows = 16 * NQ;
   constexpr int kMerge = kRows * (kMergeRow * 4 + 8);  // a wave's sums and statistics, when the waves combine
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
       const uint32_t to = lds_at(my + stage * 2 * kTileBytes + b * 16 * kRowBytes);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        load_lds16(to + i * 4 * kRowBytes, pk + (int64_t)(4 * i) * rs, off[i]);
-        load_lds16(to + kTileBytes + i * 4 * kRowBytes, pv + (int64_t)(4 * i) * rs, off[i]);
+        load_lds16<NT>(to + i * 4 * kRowBytes, pk + (int64_t)(4 * i) * rs, off[i]);
+        load_lds16<NT>(to + kTileBytes + i * 4 * kRowBytes, pv + (int64_t)(4 * i) * rs, off[i]);
       }
     }
     return bad;
@@ -403,8 +403,10 @@ int64_t attend_paged_groups(const AttendPagedLaunch &L) {
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
   if (L.rows > kRowsKernelMax) return launch_attend_tiles(L, s);
   const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
-  if (L.rows == 16) hipLaunchKernelGGL(attend_rows_kernel<1>, grid, block, 0, s, L);
-  else hipLaunchKernelGGL(attend_rows_kernel<2>, grid, block, 0, s, L);
+  if (L.rows == 16 && L.once) hipLaunchKernelGGL((attend_rows_kernel<1, true>), grid, block, 0, s, L);
+  else if (L.rows == 16) hipLaunchKernelGGL((attend_rows_kernel<1, false>), grid, block, 0, s, L);
+  else if (L.once) hipLaunchKernelGGL((attend_rows_kernel<2, true>), grid, block, 0, s, L);
+  else hipLaunchKernelGGL((attend_rows_kernel<2, false>), grid, block, 0, s, L);
   return hipGetLastError();
 }
 

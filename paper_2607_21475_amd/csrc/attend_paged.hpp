@@ -20,12 +20,17 @@ __device__ __forceinline__ uint32_t lds_at(const void *p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8 *)(uint8_t *)p);
 }
 
-// 16 bytes per lane from base + off straight into LDS at `to` + 16 lane.  Written as assembly because the
-// compiler would wait for all of them before any read of LDS; it holds no result register, and the
-// waits below order it.
+// 16 bytes per lane from base + off straight into LDS at `to` + 16 lane; NT: the non-temporal hint.  Written as
+// assembly because the compiler would wait for all of them before any read of LDS; it holds no result register, and
+// the waits below order it.
+template <bool NT>
 __device__ __forceinline__ void load_lds16(uint32_t to, const uint8_t *base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base)
-               : "memory");
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(off), "s"(base)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base)
+                 : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {

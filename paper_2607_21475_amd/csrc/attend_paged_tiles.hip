@@ -71,7 +71,7 @@ __device__ __forceinline__ float max_halves(float x) {
 }  // namespace
 
 // RW waves of 32 query rows each, KG groups of them that take every KG'th tile of KEYS keys.
-template <int RW, int KG, int KEYS>
+template <int RW, int KG, int KEYS, bool NT>
 __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
   constexpr int kWaves = RW * KG, kRows = 32 * RW;
   constexpr int kSub = KEYS / 32;             // blocks of 32 keys of a tile
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   auto load_tile = [&](const uint16_t *pool, int64_t at, uint32_t to) {
     const uint8_t *x = reinterpret_cast<const uint8_t *>(pool) + at;
 #pragma unroll
-    for (int i = 0; i < kPart / 4; ++i) load_lds16(to + i * 4 * kRowBytes, x + (int64_t)(4 * i) * rs, off[i]);
+    for (int i = 0; i < kPart / 4; ++i) load_lds16<NT>(to + i * 4 * kRowBytes, x + (int64_t)(4 * i) * rs, off[i]);
   };
 
   // LDS addresses within a tile: K operand row c, dims 16 kb + 8 half at ka ^ 32 kb; V operand rows
@@ -443,8 +443,9 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
 
 hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {
   const dim3 grid((unsigned)attend_paged_groups(L));
-  if (L.rows == kFewRows) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32>), grid, dim3(512), 0, s, L);
-  else hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64>), grid, dim3(256), 0, s, L);
+  if (L.rows == kFewRows && L.once) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, true>), grid, dim3(512), 0, s, L);
+  else if (L.rows == kFewRows) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, false>), grid, dim3(512), 0, s, L);
+  else hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64, false>), grid, dim3(256), 0, s, L);
   return hipGetLastError();
 }
 

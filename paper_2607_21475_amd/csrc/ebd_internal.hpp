@@ -200,6 +200,7 @@ struct AttendPagedLaunch {
   int32_t blocks;      // ... blocks per sequence and KV head
   int32_t nsplit;      // splits of the rows a block sees
   int32_t split_rows;  // ... rows each
+  int32_t once;        // keys and values are read once, and more of them than caches hold: non-temporal loads
   float *part;         // [groups, rows, 128] sums of the splits, then
   float2 *stats;       // [groups, rows] their maximum and total weight
 };

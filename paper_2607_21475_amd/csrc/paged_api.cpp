@@ -66,11 +66,32 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
          p->num_tokens <= kGridMax && p->max_rows <= kRowsMax && (int64_t)p->max_new * p->group <= INT32_MAX / 2;
 }
 
-// How a launch is cut.  Units (sequence, KV head, block of query rows) are split until there are
-// 256 work-groups, one a CU; a split holds at least a tile for each wave (attend_rows) or eight tiles.
-constexpr int64_t kGroups = 256;
-constexpr int64_t kRowsLeast = 128;
+// How a launch is cut.  Units (sequence, KV head, block of query rows) are split over the rows they see where that
+// ends the launch sooner: its work-groups run in rounds of as many as the chip holds (one a CU, or two
+// of attend_tiles with 128 query rows), and each takes its split's rows and what a start, an end and a share of
+// the join cost, about as long as kStartRows more.  us, splits by the fewest rounds / by this rule: 33 sequences
+// of 2000 to 15000 rows (264 units) 218 / 206; rounds of 384, 512, 768 or 1024 work-groups instead of 256: 8 sequences of
+// 16384 rows 95, 94, 93, 97 / 90, 16 of up to 6144 rows 40, 36, 38, 40 / 32.
+constexpr int64_t kCus = 256;
+constexpr int64_t kRowsLeast = 128;  // fewest rows of a split: a tile for each wave, or eight tiles
 constexpr int64_t kTilesLeast = 512;
+constexpr int64_t kStartRows = 320;
+constexpr int64_t kTilesStartRows = 640;
+constexpr int64_t kSplitsMost = 256;
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // of the last-level cache
+
+int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start) {
+  int64_t best = 1, cost = INT64_MAX;
+  for (int64_t ns = 1; ns <= std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least)); ++ns) {
+    const int64_t rows = ((span + ns - 1) / ns + 127) / 128 * 128;
+    const int64_t used = (span + rows - 1) / rows;  // splits that the rounded size leaves
+    const int64_t c = (units * used + slots - 1) / slots * (rows + start);
+    if (c < cost) best = ns, cost = c;
+    if (units * ns >= 16 * slots) break;  // rounds are many: finer ones gain nothing
+  }
+  return best;
+}
+
 AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   AttendPagedLaunch L{};
   L.p = *p;
@@ -83,10 +104,15 @@ AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows / p->group + 1);
   span = std::max<int64_t>(span, 1) + 63;
   const int64_t units = std::max<int64_t>(1, (int64_t)p->pages.num_seqs * p->pages.kv_heads * L.blocks);
-  int64_t ns = std::max<int64_t>(1, (tiles ? 2 * kGroups : kGroups) / units);
-  ns = std::min<int64_t>(ns, std::max<int64_t>(1, span / (tiles ? kTilesLeast : kRowsLeast)));
+  const int64_t ns = tiles ? splits(units, span, 2 * kCus, kTilesLeast, kTilesStartRows)
+                           : splits(units, span, kCus, kRowsLeast, kStartRows);
   L.split_rows = (int32_t)(((span + ns - 1) / ns + 127) / 128 * 128);
   L.nsplit = (int32_t)((span + L.split_rows - 1) / L.split_rows);
+  // keys and values that one work-group alone reads, more of them than the last-level cache could still hold from
+  // the step before (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
+  // to 4096 rows 124 / 111, 16 of 4096 rows and 12 tokens 66 / 60; but 16 of up to 6144 rows, 8 tokens, 37 / 41,
+  // one of 4096 rows 14.4 / 15.3
+  L.once = L.blocks == 1 && p->pages.num_seqs * span * p->pages.kv_heads * 4 * kHeadDim > kCacheBytes;
   L.shift = log2_of(p->pages.page_size);
   L.scale = p->scale > 0.0f ? p->scale : 1.0f / std::sqrt((float)kHeadDim);
   return L;
