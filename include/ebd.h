@@ -420,7 +420,7 @@ typedef struct ebd_pages {
  *   num_tokens  new tokens in k_new, v_new (and q, q_out).
  *   new_off     [num_seqs + 1] device int64, non-decreasing: sequence s owns new tokens
  *               new_off[s] .. new_off[s+1]-1; tokens before new_off[0] or from new_off[num_seqs] on are
- *               padding: nothing is read from or written for them.
+ *               padding: nothing is written for them.
  *   len         [num_seqs] device int32: the rows sequence s holds with its new tokens, which are its last
  *               ones: token new_off[s] + j becomes row len[s] - (new_off[s+1] - new_off[s]) + j.
  *   pos         [num_tokens] device int32 rotary positions, or NULL: a token's row index.

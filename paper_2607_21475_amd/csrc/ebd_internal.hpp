@@ -167,7 +167,7 @@ struct RopeLaunch {
   ebd_rope_params p;  // amplitude resolved
   const uint16_t *x;
   uint16_t *y;
-  int32_t tpb;  // tokens per work-group
+  int32_t per, tpb;  // threads per token, tokens per work-group
 };
 
 struct AppendPagedLaunch {
@@ -176,7 +176,7 @@ struct AppendPagedLaunch {
   uint16_t *K, *V, *q_out;
   uint32_t *status;
   int32_t shift;  // log2 page_size
-  int32_t tpb;
+  int32_t per, tpb;
 };
 
 struct GatherPagedLaunch {

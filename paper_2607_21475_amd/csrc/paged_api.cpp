@@ -99,10 +99,10 @@ AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
   L.rows = rows <= 16 ? 16 : rows <= kRowsKernelMax ? 32 : rows <= kFewRows ? kFewRows : kTileRows;
   const bool tiles = L.rows == kTileRows;
   L.blocks = (int32_t)std::max<int64_t>(1, (rows + L.rows - 1) / L.rows);
-  // the most rows a block of query rows sees, from a tile's border on
+  // the most rows a block of query rows sees, under a window from a tile's border on
   int64_t span = p->max_rows;
   if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows / p->group + 1);
-  span = std::max<int64_t>(span, 1) + 63;
+  span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
   const int64_t units = std::max<int64_t>(1, (int64_t)p->pages.num_seqs * p->pages.kv_heads * L.blocks);
   const int64_t ns = tiles ? splits(units, span, 2 * kCus, kTilesLeast, kTilesStartRows)
                            : splits(units, span, kCus, kRowsLeast, kStartRows);

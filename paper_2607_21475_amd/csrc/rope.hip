@@ -8,19 +8,20 @@
 //
 // Both kernels read and write each row once: the memory's rate bounds large calls, the chain of dependent
 // loads (sequence, length, page, row) small ones.  Eight lanes take a row, 32 bytes each in two 16-byte
-// accesses that hold both elements of its pairs; a work-group takes up to 32 rows of a token (all that most
-// models have), so one token's sines cost a wave's worth of work per 8 KB moved.  Tokens of few rows share a
-// work-group, a wave or two each.
+// accesses that hold both elements of its pairs.  A work-group has as many waves as a token's rows need (up to 128 of
+// them), so that a token's sines are made once, by one wave's worth of work, and no lane idles over rows that are not
+// there; tokens of few rows share a work-group.
 #include "ebd.h"
 #include "ebd_internal.hpp"
 #include "paged_device.hpp"
+
+#include <algorithm>
 
 namespace ebd {
 
 namespace {
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopeRows = 32;  // rows of a work-group: 8 lanes each
+constexpr int kRopeRows = 128;  // most rows of a work-group: 8 lanes each
 
 // cos and sin (times the amplitude) of pair `i` at position `pos`.
 __device__ __forceinline__ float2 turn(const ebd_rotary &R, int i, int64_t pos) {
@@ -99,11 +100,16 @@ __device__ __forceinline__ void store16(uint16_t *p, const uint4 &v) { *reinterp
 
 }  // namespace
 
-// Work-group (token group, block of 32 rows): threads / tpb threads per token.
-__global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch L) {
+// Work-group (token group, block of rows): `per` threads, whole waves, for each of up to four tokens.
+__device__ __forceinline__ int token_slot(int per) {
+  const int t = threadIdx.x;
+  return (t >= per) + (t >= 2 * per) + (t >= 3 * per);
+}
+
+__global__ __launch_bounds__(8 * kRopeRows) void rope_kernel(RopeLaunch L) {
   __shared__ float2 cs[4][kHeadDim / 2];
   const ebd_rope_params &p = L.p;
-  const int per = kRopeThreads / L.tpb, slot = threadIdx.x / per, i = threadIdx.x % per;
+  const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per;
   const int64_t t = (int64_t)blockIdx.x * L.tpb + slot;
   const int h = blockIdx.y * kRopeRows + i / 8;
   const bool live = t < p.num_tokens && h < p.num_heads;
@@ -128,26 +134,27 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch L) {
 }
 
 // Rows of a token in order: its keys, its queries, its values.
-__global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedLaunch L) {
+__global__ __launch_bounds__(8 * kRopeRows) void append_paged_kernel(AppendPagedLaunch L) {
   __shared__ float2 cs[4][kHeadDim / 2];
   const ebd_append_paged_params &p = L.p;
-  const int per = kRopeThreads / L.tpb, slot = threadIdx.x / per, i = threadIdx.x % per;
+  const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per;
   const int64_t t = (int64_t)blockIdx.x * L.tpb + slot;
   const int row = blockIdx.y * kRopeRows + i / 8;
   const int kv = p.pages.kv_heads, S = p.pages.num_seqs;
-  // the wave's token: its sequence, row and page
-  const int s = t < p.num_tokens ? find_seq(p.new_off, S, t) : -1;
   const bool isk = row < kv, isq = !isk && row < kv + p.q_heads;
-  const bool live = s >= 0 && row < 2 * kv + p.q_heads;
+  const bool here = t < p.num_tokens && row < 2 * kv + p.q_heads;
   const int h = isk ? row : (isq ? row - kv : row - kv - p.q_heads);
   const Split sp = split_row(p.rot, i % 8, isk || isq);
   const ebd_rows &in = isq ? p.q_rows : (isk ? p.k_rows : p.v_rows);
   const uint16_t *x = (isq ? L.q : (isk ? L.k_new : L.v_new)) + t * in.token_stride + h * in.head_stride;
   uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-  if (live && sp.how != kOdd) {
+  if (here && sp.how != kOdd) {  // asked for before the token's place is known
     a = load16(x + sp.e0);
     b = load16(x + sp.e1);
   }
+  // the wave's token: its sequence, row and page
+  const int s = t < p.num_tokens ? find_seq(p.new_off, S, t) : -1;
+  const bool live = here && s >= 0;
   int64_t base = -1;
   if (s >= 0) {
     const int64_t r = (int64_t)p.len[s] - p.new_off[s + 1] + t;
@@ -169,23 +176,26 @@ __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedL
 }
 
 namespace {
-// Tokens per work-group: one, or two or four of few rows, whole waves each.
-int tokens_per_group(int64_t rows) { return rows <= 8 ? 4 : (rows <= 16 ? 2 : 1); }
+// Threads of a token and tokens of a work-group.
+void cut(int64_t rows, int32_t *per, int32_t *tpb) {
+  *per = (int32_t)((std::min<int64_t>(rows, kRopeRows) * 8 + 63) / 64 * 64);
+  *tpb = std::max(1, std::min(4, 256 / *per));
+}
 dim3 rope_grid(int64_t tokens, int64_t rows, int tpb) {
   return dim3((unsigned)((tokens + tpb - 1) / tpb), (unsigned)((rows + kRopeRows - 1) / kRopeRows));
 }
 }  // namespace
 
 hipError_t launch_rope(RopeLaunch L, hipStream_t s) {
-  L.tpb = tokens_per_group(L.p.num_heads);
-  hipLaunchKernelGGL(rope_kernel, rope_grid(L.p.num_tokens, L.p.num_heads, L.tpb), dim3(kRopeThreads), 0, s, L);
+  cut(L.p.num_heads, &L.per, &L.tpb);
+  hipLaunchKernelGGL(rope_kernel, rope_grid(L.p.num_tokens, L.p.num_heads, L.tpb), dim3(L.per * L.tpb), 0, s, L);
   return hipGetLastError();
 }
 
 hipError_t launch_append_paged(AppendPagedLaunch L, hipStream_t s) {
   const int64_t rows = 2 * (int64_t)L.p.pages.kv_heads + L.p.q_heads;
-  L.tpb = tokens_per_group(rows);
-  hipLaunchKernelGGL(append_paged_kernel, rope_grid(L.p.num_tokens, rows, L.tpb), dim3(kRopeThreads), 0, s, L);
+  cut(rows, &L.per, &L.tpb);
+  hipLaunchKernelGGL(append_paged_kernel, rope_grid(L.p.num_tokens, rows, L.tpb), dim3(L.per * L.tpb), 0, s, L);
   return hipGetLastError();
 }
 
