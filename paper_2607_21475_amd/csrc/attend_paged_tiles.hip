@@ -233,15 +233,18 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       for (int d = 0; d < 4; ++d) O[d] *= a;
     }
     const float mu = m == -INFINITY ? 0.0f : m;  // nothing seen yet: every score is -inf
+    // a tile's weights are added up by themselves: z takes one rounding a tile
+    float part_z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int b = 0; b < kSub; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float w = fast_exp2(__builtin_fmaf(S[b][i], sc2, -mu));
-        z += w;
+        part_z[i % 4] += w;
         W[2 * b + i / 8][i % 8] = (__bf16)w;
       }
     }
+    z += (part_z[0] + part_z[1]) + (part_z[2] + part_z[3]);
   };
   auto bad_of = [&](int k) {
     uint32_t bad = 0;

@@ -78,7 +78,7 @@ constexpr int64_t kTilesLeast = 512;
 constexpr int64_t kStartRows = 320;
 constexpr int64_t kTilesStartRows = 640;
 constexpr int64_t kSplitsMost = 256;
-constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // of the last-level cache
+constexpr int64_t kCacheBytes = (int64_t)64 << 20;
 
 int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start) {
   int64_t best = 1, cost = INT64_MAX;
@@ -108,10 +108,9 @@ AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
                            : splits(units, span, kCus, kRowsLeast, kStartRows);
   L.split_rows = (int32_t)(((span + ns - 1) / ns + 127) / 128 * 128);
   L.nsplit = (int32_t)((span + L.split_rows - 1) / L.split_rows);
-  // keys and values that one work-group alone reads, more of them than the last-level cache could still hold from
-  // the step before (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
-  // to 4096 rows 124 / 111, 16 of 4096 rows and 12 tokens 66 / 60; but 16 of up to 6144 rows, 8 tokens, 37 / 41,
-  // one of 4096 rows 14.4 / 15.3
+  // keys and values that one work-group alone reads, and too many to stay in the last-level cache until the next call
+  // on the same layer (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
+  // to 4096 rows 124 / 111, 16 of up to 6144 rows, 8 tokens, 41.5 / 39.1; one of 4096 rows, found in the cache, 14.4 / 15.3
   L.once = L.blocks == 1 && p->pages.num_seqs * span * p->pages.kv_heads * 4 * kHeadDim > kCacheBytes;
   L.shift = log2_of(p->pages.page_size);
   L.scale = p->scale > 0.0f ? p->scale : 1.0f / std::sqrt((float)kHeadDim);
