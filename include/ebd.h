@@ -462,7 +462,8 @@ ebd_status ebd_append_paged(const ebd_append_paged_params *p, const uint16_t *k_
  *   (before new_off[0], from new_off[num_seqs] on) are left as they were.
  *   max_new, max_rows: host bounds on the new tokens and on the rows of a sequence (they size the grid).  Of
  *   a sequence with more, new tokens past max_new get no output and rows past max_rows are not seen, and
- *   EBD_ST_BAD_LAYOUT is set.
+ *   EBD_ST_BAD_LAYOUT is set (a sequence without new tokens is not looked at).  A call with a long chunk and many
+ *   short ones is served by a launch for each kind.
  *   scale: logit scale (0 means 1/sqrt(head_dim)).
  *   status [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a row that some token sees has no page
  *   (it is not seen), EBD_ST_BAD_LAYOUT as above.

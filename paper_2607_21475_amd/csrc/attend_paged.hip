@@ -48,28 +48,23 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   __shared__ __align__(1024) uint8_t lds[kRowsWaves * kWaveLds];
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
-  int bid = blockIdx.x;
-  const int sp = bid % L.nsplit;
-  bid /= L.nsplit;
-  const int rb = bid % L.blocks;
-  bid /= L.blocks;
-  const int h = bid % H, s = bid / H;
+  const int sp = blockIdx.x % L.nsplit, uh = blockIdx.x / L.nsplit, h = uh % H;
+  const Place at = place_of(L, uh / H);
+  const int s = at.s, rb = at.rb;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   const Seq sq = sequence(p, s);
   const int row0 = rb * kRows, nrow = min(kRows, sq.tokens * G - row0);
+  if (nrow <= 0 || !takes(L, (int64_t)sq.tokens * G)) return;
   if (threadIdx.x == 0 && rb == 0 && sp == 0 && h == 0 && L.status && sq.status) atomicOr(&L.status[s], sq.status);
-  if (nrow <= 0) return;
 
   Span span[NQ];
 #pragma unroll
   for (int b = 0; b < NQ; ++b) span[b] = span_of(p, sq, row0 + 16 * b + c);
   const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, row0 / G, (row0 + nrow - 1) / G);
-  // this split's keys
-  const int64_t start = (R.lo & -kTileKeys) + (int64_t)sp * L.split_rows;
-  const int k_end = start < R.hi ? (int)min((int64_t)R.hi, start + L.split_rows) : 0;
-  const int k_beg = start < R.hi ? (int)start : 0;  // rows stay below 2^30: no sum below overflows
+  const Keys split = split_of(L, R.lo, R.hi, kTileKeys, sp);
+  const int k_beg = split.beg, k_end = split.end;  // (below 2^30: no sum below overflows)
 
   f32x4 O[NQ][8];
   float m[NQ], z[NQ];
@@ -341,20 +336,18 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
-  int bid = blockIdx.x;
-  const int sub = bid % (L.rows / 4);
-  bid /= L.rows / 4;
-  const int64_t slot0 = (int64_t)bid * L.nsplit;
-  const int rb = bid % L.blocks;
-  bid /= L.blocks;
-  const int h = bid % H, s = bid / H;
+  const int sub = blockIdx.x % (L.rows / 4), uh = blockIdx.x / (L.rows / 4), h = uh % H;
+  const int64_t slot0 = (int64_t)uh * L.nsplit;
+  const Place at = place_of(L, uh / H);
+  if (at.s < 0) return;
+  const int s = at.s, rb = at.rb;
   const int r = 4 * sub + (threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, e = (lane & 15) * 8;
   const int row = rb * L.rows + r;
   const float2 *stats = L.stats + slot0 * L.rows + r;
   const float *part = L.part + (slot0 * L.rows + r) * kHeadDim + e;
   const int64_t step = (int64_t)L.rows * kHeadDim;
   const Seq sq = sequence(p, s);
-  if (row >= sq.tokens * G) return;
+  if (row >= sq.tokens * G || !takes(L, (int64_t)sq.tokens * G)) return;
   float M = -INFINITY, Z = 0.0f, o[8] = {};
   for (int v0 = 0; v0 < L.nsplit; v0 += 16) {
     float2 t[4];
@@ -397,7 +390,7 @@ size_t attend_paged_part_bytes(const AttendPagedLaunch &L) {
 }
 
 int64_t attend_paged_groups(const AttendPagedLaunch &L) {
-  return (int64_t)L.p.pages.num_seqs * L.p.pages.kv_heads * L.blocks * L.nsplit;
+  return L.units * L.p.pages.kv_heads * L.nsplit;
 }
 
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {

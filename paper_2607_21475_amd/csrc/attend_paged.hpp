@@ -54,11 +54,16 @@ struct Seq {
   int64_t seen;     // ... of which the launch can see
   uint32_t status;
 };
+// New tokens of a sequence that get an output: tokens t0 .. t1 - 1, as far as the bounds allow.
+__device__ __forceinline__ int tokens_of(const ebd_attend_paged_params &p, int64_t t0, int64_t t1) {
+  if (t0 < 0) return 0;
+  return (int)max((int64_t)0, min(min(t1 - t0, (int64_t)p.max_new), p.num_tokens - t0));
+}
 __device__ __forceinline__ Seq sequence(const ebd_attend_paged_params &p, int s) {
   Seq q;
   const const_i64 *off = (const const_i64 *)p.new_off;
   q.t0 = off[s];
-  const int64_t n = off[s + 1] - q.t0;
+  const int64_t t1 = off[s + 1], n = t1 - q.t0;
   q.len = ((const const_i32 *)p.len)[s];
   q.first = q.len - n;
   q.status = (n > p.max_new || q.len > p.max_rows) ? EBD_ST_BAD_LAYOUT : 0u;
@@ -68,9 +73,62 @@ __device__ __forceinline__ Seq sequence(const ebd_attend_paged_params &p, int s)
     q.status |= EBD_ST_BAD_PAGE;
     q.seen = room;
   }
-  q.tokens = (int)max((int64_t)0, min(min(n, (int64_t)p.max_new), p.num_tokens - q.t0));
-  if (q.t0 < 0) q.tokens = 0;
+  q.tokens = tokens_of(p, q.t0, t1);
   return q;
+}
+
+// Whether a launch takes a sequence with this many query rows.
+__device__ __forceinline__ bool takes(const AttendPagedLaunch &L, int64_t rows) {
+  return rows > L.more_than && rows <= L.at_most;
+}
+
+// The u'th block of query rows of a launch: its sequence (-1: there is none) and which of its blocks.  With
+// L.blocks blocks set aside for each sequence that is a division; otherwise (sequences of very different
+// lengths, of which most would stay empty) the sequences' own blocks are counted, 64 sequences at a time.
+// u is uniform over the wave, and so is the result.
+struct Place {
+  int s, rb;
+};
+__device__ __forceinline__ Place place_of(const AttendPagedLaunch &L, int u) {
+  if (L.blocks > 0) return {u / L.blocks, u % L.blocks};
+  const ebd_attend_paged_params &p = L.p;
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < p.pages.num_seqs; base += 64) {
+    const int s = base + lane;
+    int n = 0;
+    if (s < p.pages.num_seqs) {
+      const int64_t rows = (int64_t)tokens_of(p, p.new_off[s], p.new_off[s + 1]) * p.group;
+      if (takes(L, rows)) n = (int)((rows + L.rows - 1) / L.rows);
+    }
+    int upto = n;  // blocks of the sequences up to this lane's
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t behind = __ballot(upto > u);
+    if (behind) {
+      const int l = __builtin_ctzll(behind);
+      return {base + l, u - __builtin_amdgcn_readlane(upto - n, l)};
+    }
+    u -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return {-1, 0};
+}
+
+// The keys of split sp of a block that sees the rows lo .. hi - 1: its own rows, from a tile's border on, dealt
+// evenly over the splits, at least L.least (a multiple of 128) each.
+struct Keys {
+  int beg, end;
+};
+__device__ __forceinline__ Keys split_of(const AttendPagedLaunch &L, int lo, int hi, int tile, int sp) {
+  if (lo >= hi) return {0, 0};
+  lo &= -tile;
+  int rows = hi - lo;
+  if (L.nsplit > 1) rows = max(L.least, ((rows + L.nsplit - 1) / L.nsplit + 127) / 128 * 128);
+  const int64_t beg = lo + (int64_t)sp * rows;
+  if (beg >= hi) return {0, 0};
+  return {(int)beg, (int)min((int64_t)hi, beg + rows)};
 }
 
 // The rows lo .. hi - 1 that query row `row` sees (lo >= hi: none).

@@ -91,12 +91,11 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const int H = p.pages.kv_heads, G = p.group;
   // heads vary fastest (work-groups go round the XCDs: a head's stay together for 8, 4, 2 heads and
   // share its keys through the XCD's L2), then query blocks, the last (which see most) first
-  int bid = blockIdx.x;
-  const int h = bid % H;
-  bid /= H;
-  const int rb = L.blocks - 1 - bid % L.blocks;
-  bid /= L.blocks;
-  const int sp = bid % L.nsplit, s = bid / L.nsplit;
+  const int h = blockIdx.x % H, us = blockIdx.x / H;
+  const int u = (int)L.units - 1 - us % (int)L.units, sp = us / (int)L.units;
+  const Place place = place_of(L, u);
+  if (place.s < 0) return;
+  const int s = place.s, rb = place.rb;
   const int lane = threadIdx.x & 63, half = lane >> 5, c = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -104,8 +103,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
 
   const Seq sq = sequence(p, s);
   const int row0 = rb * kRows, nrow = min(kRows, sq.tokens * G - row0);
+  if (nrow <= 0 || !takes(L, (int64_t)sq.tokens * G)) return;
   if (threadIdx.x == 0 && rb == 0 && sp == 0 && h == 0 && L.status && sq.status) atomicOr(&L.status[s], sq.status);
-  if (nrow <= 0) return;
 
   // what this wave's rows see, and the work-group's
   const int row = row0 + 32 * rw + c;
@@ -128,9 +127,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   }
   R = uniform(R);
   all = uniform(all);
-  const int64_t start = (all.lo & -KEYS) + (int64_t)sp * L.split_rows;
-  const int k_end = start < all.hi ? (int)min((int64_t)all.hi, start + L.split_rows) : 0;
-  const int k_beg = start < all.hi ? (int)start : 0;
+  const Keys split = split_of(L, all.lo, all.hi, KEYS, sp);
+  const int k_beg = split.beg, k_end = split.end;
   const int every_lo = all.every_lo, every_hi = min(all.every_hi, k_end);
   const const_i32 *table = (const const_i32 *)(p.pages.page_table + (int64_t)s * p.pages.max_pages);
   const int slots = p.pages.page_size - 1;
@@ -372,7 +370,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   }
 
   z += __shfl_xor(z, 32);
-  const int64_t slot = ((((int64_t)s * H + h) * L.blocks + rb) * L.nsplit + sp) * kRows;
+  const int64_t slot = (((int64_t)u * H + h) * L.nsplit + sp) * kRows;
   if constexpr (KG > 1) {
     // the groups' sums, combined in order
     __syncthreads();

@@ -197,9 +197,11 @@ struct AttendPagedLaunch {
   float scale;
   int32_t shift;
   int32_t rows;        // query rows per block
-  int32_t blocks;      // ... blocks per sequence and KV head
+  int32_t blocks;      // blocks set aside for each sequence, or 0: counted on the way
+  int64_t units;       // blocks of all sequences
+  int64_t more_than, at_most;  // query rows of the sequences that the launch takes
   int32_t nsplit;      // splits of the rows a block sees
-  int32_t split_rows;  // ... rows each
+  int32_t least;       // ... fewest rows of one
   int32_t once;        // keys and values are read once, and more of them than caches hold: non-temporal loads
   float *part;         // [groups, rows, 128] sums of the splits, then
   float2 *stats;       // [groups, rows] their maximum and total weight

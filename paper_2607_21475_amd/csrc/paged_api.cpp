@@ -67,11 +67,13 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
 }
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split over the rows they see where that
-// ends the launch sooner: its work-groups run in rounds of as many as the chip holds (one a CU, or two
-// of attend_tiles with 128 query rows), and each takes its split's rows and what a start, an end and a share of
-// the join cost, about as long as kStartRows more.  us, splits by the fewest rounds / by this rule: 33 sequences
-// of 2000 to 15000 rows (264 units) 218 / 206; rounds of 384, 512, 768 or 1024 work-groups instead of 256: 8 sequences of
-// 16384 rows 95, 94, 93, 97 / 90, 16 of up to 6144 rows 40, 36, 38, 40 / 32.
+// ends the launch sooner.  A work-group takes its split's rows and what a start, an end and a share of the join
+// cost, about as long as kStartRows more; as many run at once as the chip holds (one a CU, or two of attend_tiles
+// with 128 query rows).  Up to two rounds of them the launch ends with its last round, however full; past that the
+// work-groups are out of step and end about half of one after each other.  us, without splits beyond 256 work-groups / by
+// this rule: 33 sequences of up to 15000 rows (264 units) 218 / 193; by rounds alone, 32 chunks of up to 512 tokens over
+// up to 8192 rows 939, by this rule 770.  Units that fill the first round: 384, 512, 768 or 1024 work-groups / 256: 8
+// sequences of 16384 rows 95, 94, 93, 97 / 90, 16 of up to 6144 rows 40, 36, 38, 40 / 32.
 constexpr int64_t kCus = 256;
 constexpr int64_t kRowsLeast = 128;  // fewest rows of a split: a tile for each wave, or eight tiles
 constexpr int64_t kTilesLeast = 512;
@@ -81,41 +83,77 @@ constexpr int64_t kSplitsMost = 256;
 constexpr int64_t kCacheBytes = (int64_t)64 << 20;
 
 int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start) {
-  int64_t best = 1, cost = INT64_MAX;
+  int64_t best = 1;
+  double cost = 0.0;
   for (int64_t ns = 1; ns <= std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least)); ++ns) {
     const int64_t rows = ((span + ns - 1) / ns + 127) / 128 * 128;
-    const int64_t used = (span + rows - 1) / rows;  // splits that the rounded size leaves
-    const int64_t c = (units * used + slots - 1) / slots * (rows + start);
-    if (c < cost) best = ns, cost = c;
-    if (units * ns >= 16 * slots) break;  // rounds are many: finer ones gain nothing
+    const int64_t groups = units * ((span + rows - 1) / rows);  // (rounded up, the size may leave fewer splits)
+    const double rounds = groups <= 2 * slots ? (double)((groups + slots - 1) / slots) : (double)groups / (double)slots + 0.5;
+    const double c = rounds * (double)(rows + start);
+    if (ns == 1 || c < cost) best = ns, cost = c;
+    if (groups >= 16 * slots) break;
   }
   return best;
 }
 
-AttendPagedLaunch attend_paged_plan(const ebd_attend_paged_params *p) {
+// A launch for blocks of `rows` query rows; `sum` query rows in all, the sequences' most `rows_max` each.
+AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t rows, int64_t rows_max, int64_t sum) {
   AttendPagedLaunch L{};
   L.p = *p;
-  const int64_t rows = (int64_t)p->max_new * p->group;
-  L.rows = rows <= 16 ? 16 : rows <= kRowsKernelMax ? 32 : rows <= kFewRows ? kFewRows : kTileRows;
-  const bool tiles = L.rows == kTileRows;
-  L.blocks = (int32_t)std::max<int64_t>(1, (rows + L.rows - 1) / L.rows);
+  L.rows = rows;
+  L.at_most = INT64_MAX;
+  const bool tiles = rows == kTileRows;
+  const int64_t S = p->pages.num_seqs, H = p->pages.kv_heads;
+  // Every sequence has at most a block that is not full; blocks set aside for the longest sequence cost an
+  // empty work-group each where there are none (64 sequences, one of 2048 tokens: 32768 of them, about 130 us).
+  const int64_t aside = std::max<int64_t>(1, (rows_max + rows - 1) / rows), counted = sum / rows + S;
+  L.blocks = S * aside > counted + counted / 2 ? 0 : (int32_t)aside;
+  L.units = L.blocks ? S * aside : counted;
   // the most rows a block of query rows sees, under a window from a tile's border on
   int64_t span = p->max_rows;
-  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + L.rows / p->group + 1);
+  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + rows / p->group + 1);
   span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
-  const int64_t units = std::max<int64_t>(1, (int64_t)p->pages.num_seqs * p->pages.kv_heads * L.blocks);
-  const int64_t ns = tiles ? splits(units, span, 2 * kCus, kTilesLeast, kTilesStartRows)
-                           : splits(units, span, kCus, kRowsLeast, kStartRows);
-  L.split_rows = (int32_t)(((span + ns - 1) / ns + 127) / 128 * 128);
-  L.nsplit = (int32_t)((span + L.split_rows - 1) / L.split_rows);
+  const int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
+  L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
+  L.nsplit = (int32_t)(tiles ? splits(full * H, span, 2 * kCus, kTilesLeast, kTilesStartRows)
+                             : splits(full * H, span, kCus, kRowsLeast, kStartRows));
   // keys and values that one work-group alone reads, and too many to stay in the last-level cache until the next call
   // on the same layer (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
   // to 4096 rows 124 / 111, 16 of up to 6144 rows, 8 tokens, 41.5 / 39.1; one of 4096 rows, found in the cache, 14.4 / 15.3
-  L.once = L.blocks == 1 && p->pages.num_seqs * span * p->pages.kv_heads * 4 * kHeadDim > kCacheBytes;
+  L.once = aside == 1 && S * H * span * 4 * kHeadDim > kCacheBytes;
   L.shift = log2_of(p->pages.page_size);
   L.scale = p->scale > 0.0f ? p->scale : 1.0f / std::sqrt((float)kHeadDim);
   return L;
 }
+
+// The launches of a call.  One serves every sequence, in blocks that fit the longest chunk.  Where most sequences must
+// have far fewer new tokens than that (a prompt's chunk beside decode steps), those of up to 16 query rows (32 with
+// more query heads than that) get a launch of their own: us with one launch / with two, 8 KV heads of 4 query heads:
+// 2048 tokens over 4096 rows and 63 single ones over 8192: 857 / 507; 512 over 131072 and 31 over 4096: 2540 / 1155.
+struct AttendPagedPlan {
+  AttendPagedLaunch part[2];
+  int parts;
+};
+AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
+  const int64_t S = p->pages.num_seqs, G = p->group, most = (int64_t)p->max_new * G;
+  const int64_t sum = std::min<int64_t>(p->num_tokens * G, S * most);
+  const int32_t rows = most <= 16 ? 16 : most <= kRowsKernelMax ? 32 : most <= kFewRows ? kFewRows : kTileRows;
+  AttendPagedPlan plan;
+  plan.parts = 1;
+  if (rows == kTileRows && S > 1 && G <= kRowsKernelMax && 4 * (sum - most) <= (S - 1) * most) {
+    const int32_t small = G <= 16 ? 16 : kRowsKernelMax;
+    plan.parts = 2;
+    plan.part[1] = attend_paged_part(p, small, small, S * small);
+    plan.part[1].at_most = small;
+    plan.part[0] = attend_paged_part(p, rows, most, sum);
+    plan.part[0].more_than = small;
+  } else {
+    plan.part[0] = attend_paged_part(p, rows, most, sum);
+  }
+  return plan;
+}
+
+size_t part_bytes(const AttendPagedLaunch &L) { return (attend_paged_part_bytes(L) + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -123,7 +161,10 @@ namespace ebd {
 
 size_t attend_paged_workspace(const ebd_attend_paged_params *p) {
   if (!valid_attend_paged(p) || !supported_attend_paged(p)) return 0;
-  return (attend_paged_part_bytes(attend_paged_plan(p)) + 256) / 256 * 256;
+  const AttendPagedPlan plan = attend_paged_plan(p);
+  size_t bytes = 256;
+  for (int i = 0; i < plan.parts; ++i) bytes += part_bytes(plan.part[i]);
+  return bytes;
 }
 
 }  // namespace ebd
@@ -188,24 +229,30 @@ ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q,
   if (!q || !K || !V || !y || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(y) || ((uintptr_t)lse & 3))
     return EBD_ERR_INVALID_ARG;
-  AttendPagedLaunch L = attend_paged_plan(p);
-  if (attend_paged_groups(L) > kGridMax) return EBD_ERR_UNSUPPORTED;
+  AttendPagedPlan plan = attend_paged_plan(p);
+  for (int i = 0; i < plan.parts; ++i)
+    if (attend_paged_groups(plan.part[i]) > kGridMax / 2) return EBD_ERR_UNSUPPORTED;
   if (!workspace || ws_bytes < attend_paged_workspace(p) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
   const ebd_status ds = device_ok();
   if (ds != EBD_OK) return ds;
-  L.q = q;
-  L.K = K;
-  L.V = V;
-  L.y = y;
-  L.lse = lse;
-  L.status = status;
-  L.part = static_cast<float *>(workspace);
-  L.stats = reinterpret_cast<float2 *>(L.part + attend_paged_groups(L) * L.rows * kHeadDim);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (timed_launch("attend_paged", s, [&] { return launch_attend_paged(L, s); }) != hipSuccess) return EBD_ERR_HIP;
-  if (L.nsplit > 1 &&
-      timed_launch("attend_paged_join", s, [&] { return launch_attend_paged_join(L, s); }) != hipSuccess)
-    return EBD_ERR_HIP;
+  char *ws = static_cast<char *>(workspace);
+  for (int i = 0; i < plan.parts; ++i) {
+    AttendPagedLaunch &L = plan.part[i];
+    L.q = q;
+    L.K = K;
+    L.V = V;
+    L.y = y;
+    L.lse = lse;
+    L.status = status;
+    L.part = reinterpret_cast<float *>(ws);
+    L.stats = reinterpret_cast<float2 *>(L.part + attend_paged_groups(L) * L.rows * kHeadDim);
+    ws += part_bytes(L);
+    if (timed_launch("attend_paged", s, [&] { return launch_attend_paged(L, s); }) != hipSuccess) return EBD_ERR_HIP;
+    if (L.nsplit > 1 &&
+        timed_launch("attend_paged_join", s, [&] { return launch_attend_paged_join(L, s); }) != hipSuccess)
+      return EBD_ERR_HIP;
+  }
   return EBD_OK;
 }
 

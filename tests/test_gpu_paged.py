@@ -248,6 +248,11 @@ BITS = 8
     ([500, 31], [9, 7], 3, 3, 64, "heads", 7),
     ([2049, 33], [513, 33], 1, 2, 64, "heads", 700),
     ([64, 0, 5], [64, 0, 5], 2, 1, 16, "heads", 0),
+    # a long chunk among many short ones, sequences without new tokens between them
+    ([300] + [20 + 7 * i for i in range(70)], [150] + [1 + i % 3 * (i % 2) for i in range(70)], 1, 4, 16, "heads", 0),
+    ([9, 700, 30, 40, 2, 90], [2, 400, 0, 30, 1, 60], 2, 2, 32, "tokens", 0),
+    ([50 + i for i in range(66)] + [400], [1] * 66 + [130], 2, 17, 16, "heads", 64),
+    ([40] * 3 + [300] * 2 + [8] * 9, [33] * 3 + [180, 7] + [8] * 9, 1, 5, 16, "heads", 0),
 ])
 def test_attend(lens, news, kv, G, page, order, window):
     _say("attend", lens, news, kv, G, page, order, window)
