@@ -7,6 +7,7 @@ error statuses.  The functions carry the C names:
     ebd_evict            Poisson tail sampler (Sec. 3.3, eq. (2); Sec. 3.1)
     ebd_attend_certify   Hajek decode attention + Theorem 2 variance + eq. (4) radius
     ebd_append_certain   append a decode token with pi = 1
+    ebd_rope, ebd_append_paged, ebd_attend_paged, ebd_gather_paged   the paged cache before eviction (paged.py)
     ebd_workspace_size, ebd_status_string, ebd_version, ebd_timing_enable, ebd_timing_read
 
 The library must be built (``python paper_2607_21475_amd/build.py``); importing this package
@@ -377,6 +378,6 @@ def workspace(nbytes: int, device="cuda") -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
-from .paged import (EBD_ROPE_HALF, EBD_ROPE_INVERSE, EBD_ROPE_PAIRS, append_paged_params,  # noqa: E402
-                    attend_paged_params, ebd_append_paged, ebd_attend_paged, ebd_gather_paged, ebd_pages, ebd_rope,
-                    ebd_rotary, gather_paged_params, pages, rope_params, rotary)
+from .paged import (EBD_ROPE_HALF, EBD_ROPE_INVERSE, EBD_ROPE_PAIRS, PagedCache,  # noqa: E402
+                    append_paged_params, attend_paged_params, ebd_append_paged, ebd_attend_paged, ebd_gather_paged,
+                    ebd_pages, ebd_rope, ebd_rotary, gather_paged_params, pages, rope_frequencies, rope_params, rotary)

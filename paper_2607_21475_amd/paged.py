@@ -8,16 +8,19 @@
 Each call takes a parameter struct (`rope_params`, `append_paged_params`, ...) that a program makes once
 per plan and keeps: it holds the tables' addresses and the rows' strides.  A struct keeps the tensors
 whose addresses it holds alive, and the tensors of a call must have the shapes and strides it was made for.
-`PagedCache` allocates a pool and makes the structs of each call.
+`PagedCache` holds a pool and makes the structs and outputs of each call; `rope_frequencies` gives the
+frequencies of the usual rotary positions.
 """
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+import math
+from dataclasses import dataclass
+from typing import Optional, Sequence
 
 import torch
 
-from . import HEAD_DIM, _check, _lib, _ptr
+from . import EBD_WS_ATTEND_PAGED, HEAD_DIM, _check, _lib, _ptr, ebd_workspace_size, workspace
 
 EBD_ROPE_HALF = 0
 EBD_ROPE_PAIRS = 1
@@ -376,3 +379,106 @@ def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None,
                                  _out(params, "Ku", Ku, _BF, None), _out(params, "Vu", Vu, _BF, None),
                                  _out(params, "status", status, _I32, params.units), _on_stream(params, stream))
     _check("ebd_gather_paged", code)
+
+
+# ---- helpers that allocate ---------------------------------------------------------------------
+
+def rope_frequencies(rot_dim: int = HEAD_DIM, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     original: int = 0, low: Optional[float] = None, high: Optional[float] = None, device="cuda"):
+    """(frequencies [rot_dim / 2] float64, amplitude) of f_i = base^(-2i / rot_dim), scaled for contexts `factor` times
+    as long as the `original` ones:
+
+      none    as they are
+      linear  f / factor (positions interpolated)
+      ntk     base -> base factor^(rot_dim / (rot_dim - 2)): the highest frequency stays, the lowest becomes f / factor
+      bands   by the turns t = original f / 2 pi that a pair makes over the original context: f from `high` turns
+              (default 4) on, f / factor up to `low` (default 1), and between them g f + (1 - g) f / factor with
+              g = (t - low) / (high - low)
+      yarn    as bands, with `high` 32, and the amplitude 0.1 ln(factor) + 1
+    """
+    if rot_dim < 2 or rot_dim > HEAD_DIM or rot_dim % 2:
+        raise ValueError("rot_dim must be even, 2 to %d" % HEAD_DIM)
+    if not (base > 0 and factor > 0 and math.isfinite(base) and math.isfinite(factor)):
+        raise ValueError("base and factor must be positive")
+    amplitude = 1.0
+    if scaling == "ntk":
+        if rot_dim == 2:
+            raise ValueError("ntk scaling needs more than one pair")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = base ** (-2.0 * torch.arange(rot_dim // 2, dtype=torch.float64) / rot_dim)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling in ("bands", "yarn"):
+        low = 1.0 if low is None else low
+        high = (32.0 if scaling == "yarn" else 4.0) if high is None else high
+        if original < 1 or not low < high:
+            raise ValueError("%s scaling needs the original context length, and low < high" % scaling)
+        g = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f = g * f + (1 - g) * f / factor
+        if scaling == "yarn" and factor > 1:
+            amplitude = 0.1 * math.log(factor) + 1.0
+    elif scaling not in ("none", "ntk"):
+        raise ValueError("unknown scaling %r" % (scaling,))
+    return f.to(device), amplitude
+
+
+@dataclass
+class PagedCache:
+    """The pools of one layer and what its sequences hold: K, V [pages, KV heads, rows per page, 128] bf16, page_table
+    [sequences, pages per sequence] int32, len [sequences] int32 (all on the device, the caller's to update)."""
+
+    K: torch.Tensor
+    V: torch.Tensor
+    page_table: torch.Tensor
+    len: torch.Tensor
+
+    @classmethod
+    def allocate(cls, lengths: Sequence[int], kv_heads: int, page_size: int = 64, spare: int = 0, device="cuda"):
+        """A pool with room for `lengths` rows of each sequence (and `spare` pages), tables filled, len zero."""
+        used = [-(-max(int(n), 0) // page_size) for n in lengths]
+        total = max(sum(used) + spare, 1)
+        table = torch.full((len(used), max(used, default=0) or 1), -1, dtype=torch.int32)
+        at = 0
+        for s, n in enumerate(used):
+            table[s, :n] = torch.arange(at, at + n, dtype=torch.int32)
+            at += n
+        shape = (total, kv_heads, page_size, HEAD_DIM)
+        return cls(torch.empty(shape, dtype=_BF, device=device), torch.empty(shape, dtype=_BF, device=device),
+                   table.to(device), torch.zeros(len(used), dtype=torch.int32, device=device))
+
+    @property
+    def pages(self) -> ebd_pages:
+        return pages(self.K, self.V, self.page_table)
+
+    def append(self, k_new, v_new, new_off, rot: Optional[ebd_rotary] = None, pos=None, q=None, status=None):
+        """Append tokens (self.len counts them already); returns the rotated queries, or None without q."""
+        q_out = None if q is None else torch.empty(q.shape, dtype=_BF, device=q.device)
+        p = append_paged_params(self.pages, k_new, v_new, new_off, self.len, rot, pos=pos, q=q, q_out=q_out)
+        ebd_append_paged(p, k_new, v_new, self.K, self.V, q, q_out, status=status)
+        return q_out
+
+    def attend(self, q, new_off, max_new: int, max_rows: int, qpos=None, window: int = 0, scale: float = 0.0,
+               ws: Optional[torch.Tensor] = None, status=None):
+        """Attention of the new tokens: {"y" [tokens, heads, 128] bf16, "lse" [tokens, heads] fp32, "ws"}."""
+        y = torch.empty(q.shape, dtype=_BF, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        p = attend_paged_params(self.pages, q, y, new_off, self.len, max_new, max_rows, qpos=qpos, window=window,
+                                scale=scale)
+        need = ebd_workspace_size(EBD_WS_ATTEND_PAGED, p)
+        if ws is None or ws.numel() < need:
+            ws = workspace(need, q.device)
+        ebd_attend_paged(p, q, self.K, self.V, y, ws, lse=lse, status=status)
+        return {"y": y, "lse": lse, "ws": ws}
+
+    def gather(self, lengths: Sequence[int], status=None):
+        """The first lengths[s] rows of every sequence as units: (K [rows, 128], V, seq_off), as cache.evict takes them
+        with the unit lengths [n for n in lengths for each KV head]."""
+        off = [0]
+        for n in lengths:
+            off += [off[-1] + int(n) * (i + 1) for i in range(self.K.shape[1])]
+        seq_off = torch.tensor(off, dtype=torch.int64, device=self.K.device)
+        K = torch.empty((max(off[-1], 1), HEAD_DIM), dtype=_BF, device=self.K.device)
+        V = torch.empty_like(K)
+        p = gather_paged_params(self.pages, seq_off, max(lengths, default=0))
+        ebd_gather_paged(p, self.K, self.V, K, V, status=status)
+        return K, V, seq_off

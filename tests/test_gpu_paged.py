@@ -516,3 +516,38 @@ def test_the_path_from_a_prompt_to_certified_decoding():
     ref.check(lse, rl, tl, "lse")
     ref.check(res["y"].view(2, kv * G, 128).to(BF), ry, 2 * ty, "certified y")
     ref.check(res["lse"].view(2, kv * G), rl, 2 * tl, "certified lse")
+
+
+def test_the_allocating_helpers():
+    """PagedCache through a prompt in two chunks, a decode step and the eviction of what it holds."""
+    import paper_2607_21475_amd as ebd
+    from paper_2607_21475_amd import cache as ec
+
+    g = _gen(11)
+    lens, kv, G = [150, 61], 2, 3
+    f, amp = ebd.rope_frequencies(96, 1e4, "yarn", 4.0, original=64)
+    rot = ebd.rotary(f, ebd.EBD_ROPE_PAIRS, amp)
+    c = ebd.PagedCache.allocate([n + 1 for n in lens], kv, page_size=32)
+    held = ref.Cache([0, 0], kv, 32, g)
+    held.K, held.V, held.table = c.K, c.V, c.page_table
+    for new in ([100, 61], [50, 0], [1, 1]):
+        T = sum(new)
+        k, v, q = (ref.spaced((T, h, 128), g, True) for h in (kv, kv, kv * G))
+        c.len += torch.tensor(new, dtype=torch.int32, device="cuda")
+        off = torch.tensor([0, new[0], T], device="cuda")
+        qr = c.append(k, v, off, rot, q=q)
+        held.lens = c.len.tolist()
+        row = torch.cat([torch.arange(n - m, n, device="cuda") for n, m in zip(held.lens, new)])
+        want = ref.rotate(q, row, f, amp, 1)
+        ref.check(qr, want, ref.rotate_tolerance(q, want, f, amp, 1), "q")
+        out = c.attend(qr, off, max(new), max(held.lens))
+        ry, rl, ty, tl = ref.attend(held, qr, new, weights_bits=BITS)
+        ref.check(out["y"], ry, ty, "y")
+        ref.check(out["lse"], rl, tl, "lse")
+    K, V, so = c.gather(held.lens)
+    sizes = [n for n in held.lens for _ in range(kv)]
+    qd = ref.spaced((2, kv * G, 128), g, False).view(2 * kv, G, 128)
+    sc, _ = ec.importance_scores(K, so, qd, max(sizes))
+    kept = ec.evict(K, V, sc, so, sizes, budget_frac=0.5, n_sink=4, n_recent=16)
+    res = ec.attend_certify(kept, qd)
+    assert bool((kept.count > 20).all()) and bool(torch.isfinite(res["y"]).all()) and bool((res["r"] >= 0).all())

@@ -193,3 +193,30 @@ def test_binding_refuses_wrong_tensors():
         ebd.pages(K, K.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3), table)
     with pytest.raises(ValueError):
         ebd.pages(K[:1].expand(3, 2, 16, 128), K[:1].expand(3, 2, 16, 128), table)
+
+
+def test_rope_frequencies():
+    f, a = ebd.rope_frequencies(8, 10000.0, device="cpu")
+    assert a == 1.0 and torch.allclose(f, torch.tensor([1.0, 0.1, 0.01, 0.001], dtype=torch.float64), rtol=1e-14)
+    assert torch.equal(ebd.rope_frequencies(8, 1e4, "linear", 4.0, device="cpu")[0], f / 4)
+    n, _ = ebd.rope_frequencies(8, 1e4, "ntk", 4.0, device="cpu")
+    assert n[0] == 1 and abs(float(n[-1] / f[-1]) - 0.25) < 1e-12 and bool((n[1:-1] < f[1:-1]).all())
+    # turns over 6284 positions: about 1000, 100, 10, 1
+    b, a = ebd.rope_frequencies(8, 1e4, "bands", 8.0, original=6284, low=2.0, high=18.0, device="cpu")
+    t = 6284 * 0.01 / (2 * 3.141592653589793)
+    g = (t - 2) / 16
+    assert a == 1.0 and torch.equal(b[:2], f[:2]) and float(b[3]) == float(f[3]) / 8
+    assert abs(float(b[2]) - (g * 0.01 + (1 - g) * 0.01 / 8)) < 1e-15
+    y, a = ebd.rope_frequencies(8, 1e4, "yarn", 8.0, original=6284, device="cpu")
+    assert abs(a - 1.2079441541679836) < 1e-15 and torch.equal(y[:2], f[:2]) and f[2] / 8 < y[2] < f[2]
+    for kw in (dict(rot_dim=7), dict(rot_dim=130), dict(base=-1.0), dict(factor=0.0), dict(scaling="other"),
+               dict(scaling="bands", factor=2.0), dict(scaling="yarn", factor=2.0, original=10, low=5.0, high=5.0),
+               dict(scaling="ntk", rot_dim=2)):
+        with pytest.raises(ValueError):
+            ebd.rope_frequencies(**{"rot_dim": 8, **kw}, device="cpu")
+
+
+def test_paged_cache_allocates_room():
+    c = ebd.PagedCache.allocate([65, 0, 16], 2, page_size=16, spare=1, device="cpu")
+    assert c.K.shape == (7, 2, 16, 128) and c.V.shape == c.K.shape
+    assert c.page_table.tolist() == [[0, 1, 2, 3, 4], [-1] * 5, [5, -1, -1, -1, -1]] and c.len.tolist() == [0, 0, 0]
