@@ -399,7 +399,8 @@ ebd_status ebd_rope(const ebd_rope_params *p, const uint16_t *x, uint16_t *y, vo
  *   page_table  [num_seqs, max_pages] device int32; entries past a sequence's rows are not used.
  *   strides     positive multiples of 8; row_stride below 2^26, the others below 2^40.
  * Limits of the calls on it (beyond them, and for other page sizes, EBD_ERR_UNSUPPORTED): fewer than 2^24 new
- * tokens, 65536 heads, max_rows up to 2^30, and fewer than 2^24 work-groups in a launch.
+ * tokens, fewer than 2^24 query rows (tokens times the query heads of a KV head) of a sequence, 65536 heads, max_rows up
+ * to 2^30, and launches of fewer than 2^23 work-groups.
  */
 typedef struct ebd_pages {
     int32_t num_seqs;

@@ -48,8 +48,10 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   __shared__ __align__(1024) uint8_t lds[kRowsWaves * kWaveLds];
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
-  const int sp = blockIdx.x % L.nsplit, uh = blockIdx.x / L.nsplit, h = uh % H;
-  const Place at = place_of(L, uh / H);
+  auto token = [&](int row) { return L.by_group.quotient(row); };  // of a query row, in its sequence
+  const int uh = L.by_nsplit.quotient(blockIdx.x), sp = blockIdx.x - uh * L.nsplit;
+  const int u = L.by_heads.quotient(uh), h = uh - u * H;
+  const Place at = place_of(L, u);
   const int s = at.s, rb = at.rb;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -61,8 +63,8 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
 
   Span span[NQ];
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) span[b] = span_of(p, sq, row0 + 16 * b + c);
-  const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, row0 / G, (row0 + nrow - 1) / G);
+  for (int b = 0; b < NQ; ++b) span[b] = span_of(L, sq, row0 + 16 * b + c);
+  const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, token(row0), token(row0 + nrow - 1));
   const Keys split = split_of(L, R.lo, R.hi, kTileKeys, sp);
   const int k_beg = split.beg, k_end = split.end;  // (below 2^30: no sum below overflows)
 
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   for (int b = 0; b < NQ; ++b) {
     const int row = row0 + 16 * b + c;
     const bool ok = span[b].lo < span[b].hi;
-    const int j = ok ? row / G : 0, hq = h * G + (ok ? row % G : 0);
+    const int j = ok ? token(row) : 0, hq = h * G + (ok ? row - j * G : 0);
     const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
@@ -325,7 +327,8 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
       *reinterpret_cast<f32x4 *>(part) = f32x4{o[0], o[1], o[2], o[3]};
       *reinterpret_cast<f32x4 *>(part + 4) = f32x4{o[4], o[5], o[6], o[7]};
     } else {
-      store_row(L, sq.t0 + (row0 + r) / G, h * G + (row0 + r) % G, e, M, Z, o);
+      const int j = token(row0 + r);
+      store_row(L, sq.t0 + j, h * G + row0 + r - j * G, e, M, Z, o);
     }
   }
 }
@@ -336,9 +339,10 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
-  const int sub = blockIdx.x % (L.rows / 4), uh = blockIdx.x / (L.rows / 4), h = uh % H;
+  const int shift = __builtin_ctz(L.rows) - 2, sub = blockIdx.x & ((1 << shift) - 1), uh = blockIdx.x >> shift;
+  const int u = L.by_heads.quotient(uh), h = uh - u * H;
   const int64_t slot0 = (int64_t)uh * L.nsplit;
-  const Place at = place_of(L, uh / H);
+  const Place at = place_of(L, u);
   if (at.s < 0) return;
   const int s = at.s, rb = at.rb;
   const int r = 4 * sub + (threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, e = (lane & 15) * 8;
@@ -382,7 +386,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
   Z = add_xor32(add_xor16(Z * a));
 #pragma unroll
   for (int j = 0; j < 8; ++j) o[j] = add_xor32(add_xor16(a == 0.0f ? 0.0f : o[j] * a));
-  if (g == 0) store_row(L, sq.t0 + row / G, h * G + row % G, e, all, Z, o);
+  const int j = L.by_group.quotient(row);
+  if (g == 0) store_row(L, sq.t0 + j, h * G + row - j * G, e, all, Z, o);
 }
 
 size_t attend_paged_part_bytes(const AttendPagedLaunch &L) {

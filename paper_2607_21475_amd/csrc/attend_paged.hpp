@@ -32,6 +32,10 @@ __device__ __forceinline__ void load_lds16(uint32_t to, const uint8_t *base, uin
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base)
                  : "memory");
 }
+// ... from an address of each lane's own.
+__device__ __forceinline__ void load_lds16_from(uint32_t to, const void *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -90,7 +94,10 @@ struct Place {
   int s, rb;
 };
 __device__ __forceinline__ Place place_of(const AttendPagedLaunch &L, int u) {
-  if (L.blocks > 0) return {u / L.blocks, u % L.blocks};
+  if (L.blocks > 0) {
+    const int s = L.by_blocks.quotient(u);
+    return {s, u - s * L.blocks};
+  }
   const ebd_attend_paged_params &p = L.p;
   const int lane = threadIdx.x & 63;
   for (int base = 0; base < p.pages.num_seqs; base += 64) {
@@ -135,8 +142,9 @@ __device__ __forceinline__ Keys split_of(const AttendPagedLaunch &L, int lo, int
 struct Span {
   int lo, hi;
 };
-__device__ __forceinline__ Span span_of(const ebd_attend_paged_params &p, const Seq &q, int row) {
-  const int j = row / p.group;
+__device__ __forceinline__ Span span_of(const AttendPagedLaunch &L, const Seq &q, int row) {
+  const ebd_attend_paged_params &p = L.p;
+  const int j = L.by_group.quotient(row);
   if (j >= q.tokens) return {0, 0};
   int64_t last = q.first + j;
   if (p.qpos) last = min((int64_t)p.qpos[q.t0 + j], q.len - 1);

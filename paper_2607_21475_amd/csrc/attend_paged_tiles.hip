@@ -90,9 +90,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
   // heads vary fastest (work-groups go round the XCDs: a head's stay together for 8, 4, 2 heads and
-  // share its keys through the XCD's L2), then query blocks, the last (which see most) first
-  const int h = blockIdx.x % H, us = blockIdx.x / H;
-  const int u = (int)L.units - 1 - us % (int)L.units, sp = us / (int)L.units;
+  // share its keys through the XCD's L2), then splits, then query blocks, the last (which see most) first
+  auto token = [&](int row) { return L.by_group.quotient(row); };  // of a query row, in its sequence
+  const int us = L.by_heads.quotient(blockIdx.x), h = blockIdx.x - us * H;
+  const int back = L.by_nsplit.quotient(us), sp = us - back * L.nsplit, u = (int)L.units - 1 - back;
   const Place place = place_of(L, u);
   if (place.s < 0) return;
   const int s = place.s, rb = place.rb;
@@ -108,12 +109,12 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
 
   // what this wave's rows see, and the work-group's
   const int row = row0 + 32 * rw + c;
-  Span span[1] = {span_of(p, sq, row)};
+  Span span[1] = {span_of(L, sq, row)};
   const bool sees = span[0].lo < span[0].hi;
   Range R, all;
   if (!p.qpos) {
-    R = range_of_tokens(p, sq, (row0 + 32 * rw) / G, (row0 + 32 * rw + 31) / G);
-    all = range_of_tokens(p, sq, row0 / G, (row0 + nrow - 1) / G);
+    R = range_of_tokens(p, sq, token(row0 + 32 * rw), token(row0 + 32 * rw + 31));
+    all = range_of_tokens(p, sq, token(row0), token(row0 + nrow - 1));
   } else {
     R = range_of<1>(span);
     if (lane == 0) ranges[wave] = R;
@@ -321,18 +322,23 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     };
     load(k, 0);
     {
-      const int j = sees ? row / G : 0, hq = h * G + (sees ? row % G : 0);
-      const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
+      // the wave's query rows come the same way, into the stage that is still free: whole rows, where operand loads
+      // would gather 16 bytes from each
+      const uint32_t to = tiles_at + kStage + wave * 32 * kRowBytes;
 #pragma unroll
-      for (int kb = 0; kb < 8; ++kb)
-        Q[kb] = __builtin_bit_cast(bf16x8, sees ? reinterpret_cast<const uint4 *>(q)[2 * kb + half] : make_uint4(0u, 0u, 0u, 0u));
+      for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 4), x = min(row0 + 32 * rw + r, row0 + nrow - 1), j = token(x);
+        const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + (h * G + x - j * G) * p.q_rows.head_stride;
+        load_lds16_from(to + i * 4 * kRowBytes, q + ((lane & 15) ^ chunk_turn(r)) * 8);
+      }
       bool bad = false;
       for (int e = (k_beg >> L.shift) + (int)threadIdx.x; e <= (k_end - 1) >> L.shift; e += 64 * kWaves)
         bad |= (uint32_t)p.pages.page_table[(int64_t)s * p.pages.max_pages + e] >= (uint32_t)p.pages.num_pages;
       bad = __any(bad);
       if (lane == 0) bad_pages[wave] = bad;
+      wait_loads<0>();
 #pragma unroll
-      for (int kb = 0; kb < 8; ++kb) asm volatile("" : "+v"(Q[kb]));
+      for (int kb = 0; kb < 8; ++kb) Q[kb] = lds_read<bf16x8>(to + (ka ^ (32 * kb)));
     }
     barrier();
     any_bad = __any(lane < kWaves && bad_pages[lane & (kWaves - 1)]);
@@ -405,14 +411,15 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
         *reinterpret_cast<f32x4 *>(part_of) = f32x4{o[0], o[1], o[2], o[3]};
         *reinterpret_cast<f32x4 *>(part_of + 4) = f32x4{o[4], o[5], o[6], o[7]};
       } else {
-        store_row(L, sq.t0 + (row0 + r) / G, h * G + (row0 + r) % G, e, M, Z, o);
+        const int j = token(row0 + r);
+        store_row(L, sq.t0 + j, h * G + row0 + r - j * G, e, M, Z, o);
       }
     }
     return;
   }
   const int r = 32 * rw + c;
-  if (r >= nrow) return;
   if (L.nsplit > 1) {
+    if (r >= nrow) return;
     if (half == 0) L.stats[slot + r] = sees ? make_float2(m, z) : make_float2(-INFINITY, 0.0f);
     if (!sees || m == -INFINITY) return;
 #pragma unroll
@@ -424,22 +431,33 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     }
     return;
   }
+  // finished rows go through LDS, so that they leave as whole rows
   const bool any = sees && m != -INFINITY;
   const float a = any ? 1.0f / z : 0.0f;
-  const int64_t t = sq.t0 + row / G;
-  const int hq = h * G + row % G;
-  uint16_t *y = L.y + t * p.y_rows.token_stride + hq * p.y_rows.head_stride + 4 * half;
+  const int64_t j = token(row);
+  if (half == 0 && L.lse && r < nrow)
+    L.lse[(sq.t0 + j) * ((int64_t)H * G) + h * G + (row - j * G)] = any ? (m + fast_log2(z)) * kLn2 : -INFINITY;
+  __syncthreads();  // every wave has read its tiles
+  const uint32_t at = tiles_at + wave * 32 * kRowBytes;
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int i = 0; i < 4; ++i) {
       u32x2 v;
-      v[0] = any ? pack_bf16(O[d][4 * j] * a, O[d][4 * j + 1] * a) : 0u;
-      v[1] = any ? pack_bf16(O[d][4 * j + 2] * a, O[d][4 * j + 3] * a) : 0u;
-      *reinterpret_cast<u32x2 *>(y + 32 * d + 8 * j) = v;
+      v[0] = any ? pack_bf16(O[d][4 * i] * a, O[d][4 * i + 1] * a) : 0u;
+      v[1] = any ? pack_bf16(O[d][4 * i + 2] * a, O[d][4 * i + 3] * a) : 0u;
+      lds_write(at + c * kRowBytes + ((4 * d + i) ^ chunk_turn(c)) * 16 + 8 * half, v);
     }
   }
-  if (half == 0 && L.lse) L.lse[t * ((int64_t)H * G) + hq] = any ? (m + fast_log2(z)) * kLn2 : -INFINITY;
+  wave_sync();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int x = 4 * i + (lane >> 4), out = 32 * rw + x;
+    const u32x4 v = lds_read<u32x4>(at + x * kRowBytes + ((lane & 15) ^ chunk_turn(x)) * 16);
+    const int jo = token(row0 + out);
+    if (out < nrow)
+      *reinterpret_cast<u32x4 *>(L.y + (sq.t0 + jo) * p.y_rows.token_stride + (h * G + row0 + out - jo * G) * p.y_rows.head_stride + (lane & 15) * 8) = v;
+  }
 }
 
 hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {

@@ -188,6 +188,20 @@ struct GatherPagedLaunch {
   int32_t chunks;  // work-groups per unit
 };
 
+// Division by d as a multiplication, exact for n d < 2^40 and n < 2^24: with m = (2^40 + e) / d, e < d, the quotient
+// n m / 2^40 = (n + n e / 2^40) / d is off by less than 1 / d.
+struct Divisor {
+  uint64_t m;
+  int32_t d;
+  void set(int64_t by) {
+    d = (int32_t)by;
+    m = (((uint64_t)1 << 40) + (uint64_t)by - 1) / (uint64_t)by;
+  }
+#ifdef __HIPCC__
+  __device__ __forceinline__ int quotient(int n) const { return (int)(((uint64_t)(uint32_t)n * m) >> 40); }
+#endif
+};
+
 struct AttendPagedLaunch {
   ebd_attend_paged_params p;
   const uint16_t *q, *K, *V;
@@ -200,6 +214,7 @@ struct AttendPagedLaunch {
   int32_t blocks;      // blocks set aside for each sequence, or 0: counted on the way
   int64_t units;       // blocks of all sequences
   int64_t more_than, at_most;  // query rows of the sequences that the launch takes
+  Divisor by_group, by_heads, by_blocks, by_nsplit;
   int32_t nsplit;      // splits of the rows a block sees
   int32_t least;       // ... fewest rows of one
   int32_t once;        // keys and values are read once, and more of them than caches hold: non-temporal loads

@@ -63,7 +63,7 @@ bool valid_attend_paged(const ebd_attend_paged_params *p) {
 
 bool supported_attend_paged(const ebd_attend_paged_params *p) {
   return supported_pages(p->pages) && (int64_t)p->group * p->pages.kv_heads <= kHeadsMax &&
-         p->num_tokens <= kGridMax && p->max_rows <= kRowsMax && (int64_t)p->max_new * p->group <= INT32_MAX / 2;
+         p->num_tokens <= kGridMax && p->max_rows <= kRowsMax && (int64_t)p->max_new * p->group <= kGridMax;
 }
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split over the rows they see where that
@@ -121,6 +121,10 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t ro
   // on the same layer (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
   // to 4096 rows 124 / 111, 16 of up to 6144 rows, 8 tokens, 41.5 / 39.1; one of 4096 rows, found in the cache, 14.4 / 15.3
   L.once = aside == 1 && S * H * span * 4 * kHeadDim > kCacheBytes;
+  L.by_group.set(p->group);
+  L.by_heads.set(H);
+  L.by_blocks.set(std::max<int32_t>(L.blocks, 1));
+  L.by_nsplit.set(L.nsplit);
   L.shift = log2_of(p->pages.page_size);
   L.scale = p->scale > 0.0f ? p->scale : 1.0f / std::sqrt((float)kHeadDim);
   return L;
