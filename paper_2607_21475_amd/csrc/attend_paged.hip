@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
       int pg = b ? pg1 : pg0;
       if ((uint32_t)pg >= (uint32_t)p.pages.num_pages) {
         pg = 0;
-        bad |= 1u << b;
+        if (k + 16 * b + 16 > R.lo) bad |= 1u << b;  // (rows before the first that is seen may have no page any more)
       }
       const int slot = (k + 16 * b) & slots;
       const int64_t at = 2 * ((int64_t)pg * p.pages.page_stride + head) + (int64_t)slot * rs;

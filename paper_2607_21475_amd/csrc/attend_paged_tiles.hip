@@ -331,8 +331,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
         const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + (h * G + x - j * G) * p.q_rows.head_stride;
         load_lds16_from(to + i * 4 * kRowBytes, q + ((lane & 15) ^ chunk_turn(r)) * 8);
       }
-      bool bad = false;
-      for (int e = (k_beg >> L.shift) + (int)threadIdx.x; e <= (k_end - 1) >> L.shift; e += 64 * kWaves)
+      bool bad = false;  // (rows before the first that is seen may have no page any more)
+      for (int e = (max(k_beg, all.lo) >> L.shift) + (int)threadIdx.x; e <= (k_end - 1) >> L.shift; e += 64 * kWaves)
         bad |= (uint32_t)p.pages.page_table[(int64_t)s * p.pages.max_pages + e] >= (uint32_t)p.pages.num_pages;
       bad = __any(bad);
       if (lane == 0) bad_pages[wave] = bad;

@@ -83,15 +83,16 @@ constexpr int64_t kSplitsMost = 256;
 constexpr int64_t kCacheBytes = (int64_t)64 << 20;
 
 int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start) {
+  const int64_t most = std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least));
   int64_t best = 1;
   double cost = 0.0;
-  for (int64_t ns = 1; ns <= std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least)); ++ns) {
+  for (int i = 0; i < 16; ++i) {  // one to eight splits, and as many as fill one to eight rounds
+    const int64_t ns = std::min(most, i < 8 ? i + 1 : std::max<int64_t>(1, (i - 7) * slots / units));
     const int64_t rows = ((span + ns - 1) / ns + 127) / 128 * 128;
     const int64_t groups = units * ((span + rows - 1) / rows);  // (rounded up, the size may leave fewer splits)
     const double rounds = groups <= 2 * slots ? (double)((groups + slots - 1) / slots) : (double)groups / (double)slots + 0.5;
     const double c = rounds * (double)(rows + start);
-    if (ns == 1 || c < cost) best = ns, cost = c;
-    if (groups >= 16 * slots) break;
+    if (i == 0 || c < cost) best = ns, cost = c;
   }
   return best;
 }
@@ -158,6 +159,11 @@ AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
 }
 
 size_t part_bytes(const AttendPagedLaunch &L) { return (attend_paged_part_bytes(L) + 255) / 256 * 256; }
+size_t plan_bytes(const AttendPagedPlan &plan) {
+  size_t bytes = 256;
+  for (int i = 0; i < plan.parts; ++i) bytes += part_bytes(plan.part[i]);
+  return bytes;
+}
 
 }  // namespace
 
@@ -165,10 +171,7 @@ namespace ebd {
 
 size_t attend_paged_workspace(const ebd_attend_paged_params *p) {
   if (!valid_attend_paged(p) || !supported_attend_paged(p)) return 0;
-  const AttendPagedPlan plan = attend_paged_plan(p);
-  size_t bytes = 256;
-  for (int i = 0; i < plan.parts; ++i) bytes += part_bytes(plan.part[i]);
-  return bytes;
+  return plan_bytes(attend_paged_plan(p));
 }
 
 }  // namespace ebd
@@ -230,13 +233,13 @@ ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q,
   if (!valid_attend_paged(p)) return EBD_ERR_INVALID_ARG;
   if (!supported_attend_paged(p)) return EBD_ERR_UNSUPPORTED;
   if (p->num_tokens == 0 || p->pages.num_seqs == 0) return EBD_OK;
-  if (!q || !K || !V || !y || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
+  if (p->max_new == 0 || !q || !K || !V || !y || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(y) || ((uintptr_t)lse & 3))
     return EBD_ERR_INVALID_ARG;
   AttendPagedPlan plan = attend_paged_plan(p);
   for (int i = 0; i < plan.parts; ++i)
     if (attend_paged_groups(plan.part[i]) > kGridMax / 2) return EBD_ERR_UNSUPPORTED;
-  if (!workspace || ws_bytes < attend_paged_workspace(p) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
+  if (!workspace || ws_bytes < plan_bytes(plan) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
   const ebd_status ds = device_ok();
   if (ds != EBD_OK) return ds;
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -169,9 +169,12 @@ def _rows_of(t):
 
 
 def _distinct(t, name):
-    """Refuse outputs whose rows share memory (expanded tensors)."""
-    if t.numel() and any(n > 1 and s < HEAD_DIM for n, s in zip(t.shape[:-1], t.stride()[:-1])):
-        raise ValueError("the rows of %s must not share memory" % name)
+    """Refuse outputs whose rows may share memory: each stride has to pass over all that the smaller ones span."""
+    span = HEAD_DIM
+    for stride, n in sorted((s, n) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1):
+        if t.numel() and stride < span:
+            raise ValueError("the rows of %s must not share memory" % name)
+        span = max(span, stride * n)
 
 
 def _plan(p, device, keep, **tensors):

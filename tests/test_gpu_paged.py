@@ -335,6 +335,33 @@ def test_attend_rows_without_a_page():
     assert st.tolist() == [ebd.EBD_ST_BAD_PAGE]
 
 
+@pytest.mark.parametrize("news", [[1, 1], [9, 2], [13, 5], [60, 33]])
+def test_attend_pages_given_back_before_the_window(news):
+    """Pages that lie before every window may be anyone's: no effect and no flag."""
+    c = ref.Cache([500, 333], 2, 16, _gen(8), fill=math.nan)
+    window = 70
+    for s, (n, m) in enumerate(zip(c.lens, news)):
+        first = n - m - window + 1  # of the rows that are seen
+        c.table[s, :first // 16] = torch.tensor([-1, 10 ** 6] * 20, dtype=torch.int32, device="cuda")[:first // 16]
+    q, y, lse, st = _attend(c, news, 4, window=window)
+    assert st.tolist() == [0, 0]
+    ry, rl, ty, tl = ref.attend(Held(c), q, news, window=window, weights_bits=BITS)
+    ref.check(y, ry, ty, "y")
+    ref.check(lse, rl, tl, "lse")
+
+
+class Held:
+    """A cache whose rows are gathered from the pages that its table still names."""
+
+    def __init__(self, c):
+        self.c, self.kv, self.lens, self.K, self.V = c, c.kv, c.lens, c.K, c.V
+
+    def rows(self, pool, s, h):
+        p = self.c.table[s, :-(-self.lens[s] // self.c.page)].long()
+        p = torch.where((p >= 0) & (p < pool.shape[0]), p, 0)
+        return pool[p, h].reshape(-1, 128)[:self.lens[s]]
+
+
 @pytest.mark.parametrize("news", [[3, 5], [16, 20], [25, 30], [60, 90]])
 def test_attend_beyond_the_bounds(news):
     """Sequences with more rows or new tokens than the host said: flagged, the rest as asked."""

@@ -119,7 +119,7 @@ def test_attend_refusals():
         assert _attend(pages=_pages(**kw)) == code, kw
         n = LIB.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, ctypes.byref(_attend_params(pages=_pages(**kw))))
         assert n == 0, kw
-    for kw in (dict(group=0), dict(max_new=-1), dict(num_tokens=-1), dict(max_rows=-1), dict(window=-1),
+    for kw in (dict(group=0), dict(max_new=-1), dict(max_new=0), dict(num_tokens=-1), dict(max_rows=-1), dict(window=-1),
                dict(scale=-1.0), dict(scale=float("inf")), dict(new_off=None), dict(len=None),
                dict(q_rows=paged.ebd_rows(-8, 128)), dict(y_rows=paged.ebd_rows(128, 4))):
         assert _attend(**kw) == BAD, kw
@@ -181,6 +181,8 @@ def test_binding_refuses_wrong_tensors():
         ebd.rope_params(cpu, cpu[:3], pos, ebd.rotary(None))
     with pytest.raises(ValueError):  # rows that share memory
         ebd.rope_params(cpu, cpu[:1].expand(4, 2, 128), pos, ebd.rotary(None))
+    with pytest.raises(ValueError):  # ... though no stride is below a row's length
+        ebd.rope_params(cpu, torch.as_strided(cpu, (4, 2, 128), (128, 128, 1)), pos, ebd.rotary(None))
     K = torch.zeros((3, 2, 16, 128), dtype=bf)
     table = torch.zeros((1, 3), dtype=torch.int32)
     with pytest.raises(ValueError):
