@@ -95,7 +95,11 @@ __device__ __forceinline__ void turn_row(const ebd_rotary &R, const Split &S, ui
   }
 }
 
-__device__ __forceinline__ uint4 load16(const uint16_t *p) { return *reinterpret_cast<const uint4 *>(p); }
+// Rows are read once, so that they leave no trace in the caches (8191 tokens of 32 rows 31.2 -> 28.9 us, append of 13k
+// tokens of 36 rows 53 -> 52); what is written stays there for the attention that reads it next.
+__device__ __forceinline__ uint4 load16(const uint16_t *p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)));
+}
 __device__ __forceinline__ void store16(uint16_t *p, const uint4 &v) { *reinterpret_cast<uint4 *>(p) = v; }
 
 }  // namespace

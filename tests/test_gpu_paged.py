@@ -578,3 +578,19 @@ def test_the_allocating_helpers():
     kept = ec.evict(K, V, sc, so, sizes, budget_frac=0.5, n_sink=4, n_recent=16)
     res = ec.attend_certify(kept, qd)
     assert bool((kept.count > 20).all()) and bool(torch.isfinite(res["y"]).all()) and bool((res["r"] >= 0).all())
+
+
+def test_gather_of_more_than_the_caches_hold():
+    import paper_2607_21475_amd as ebd
+
+    lens, kv = [131072, 9999], 2
+    c = ref.Cache(lens, kv, 64, _gen(12))
+    sizes = [n for n in lens for _ in range(kv)]
+    so = torch.tensor([0, 131072, 262144, 272143, 282142], device="cuda")
+    Ku = torch.full((so[-1] + 3, 128), 7.0, dtype=BF, device="cuda")
+    Vu = Ku.clone()
+    p = ebd.gather_paged_params(ebd.pages(c.K, c.V, c.table), so, 131072)
+    ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu)
+    for out, pool in ((Ku, c.K), (Vu, c.V)):
+        want = torch.cat([c.rows(pool, s, h) for s in range(2) for h in range(kv)])
+        assert len(want) == sum(sizes) and torch.equal(out[:-3], want) and bool((out[-3:] == 7).all())
