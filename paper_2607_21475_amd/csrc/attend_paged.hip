@@ -6,7 +6,7 @@
 //   m = max l,  w = 2^(l - m),  y = sum w v / sum w,  lse = m ln 2 + ln sum w
 // in one pass, m running (what was summed is scaled down when it grows).
 //
-// attend_rows (few query rows): one work-group per (sequence, KV head, block of 16 or 32 query rows, split of
+// attend_rows (up to 32 query rows): one work-group per (sequence, KV head, block of 16 or 32 query rows, split of
 //   the rows they see), four waves that take its tiles of 32 keys in turn, each on its own.  A wave keeps the
 //   next tile's keys and values on their way into its share of LDS (loads that write LDS directly, 16 bytes a
 //   lane) while it computes the present one; nothing in the loop waits for another wave.
@@ -17,7 +17,9 @@
 //   The 16-byte chunks of a tile's row r are stored at chunk ^ (r mod 16): without that, the rows a
 //   read gathers from would all lie in the same banks.
 //   Weights enter as a bf16 head and a bf16 tail (16 bits of each): the memory bounds these launches, and
-//   the second product costs nothing beside it.
+//   the second product costs nothing beside it.  A decode step of 32 sequences of 16384 rows, 8 KV heads of 4 query
+//   heads: 317 us, 6.8 TB/s, its keys and values read exactly once; of one of 4096 rows, 8 heads: 6.3 us and the join
+//   3.5, a chain of loads (lengths, pages, the tile) of half a microsecond each.
 // attend_join: the splits of each row, combined in order.
 #include "attend_paged.hpp"
 

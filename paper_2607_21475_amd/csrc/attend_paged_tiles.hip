@@ -1,18 +1,25 @@
-// attend_paged_tiles.hip -- attention of many query rows over a paged cache on gfx950 (prompts, long chunks).
+// attend_paged_tiles.hip -- attention of many query rows over a paged cache on gfx950 (prompts, chunks).
 //
-// attend_tiles: one work-group per (sequence, KV head, block of 256 query rows, split of the rows they see), eight
-//   waves of 32 query rows each.  Tiles of 64 keys and values pass through LDS, the next one on its way (loads
-//   that write LDS directly) while the waves compute the present one; one barrier a tile.
-//   S^T = K Q^T on MFMA 32x32x16 bf16 (exact products, fp32 sums): a lane holds half of the 64 scores of
-//   one query row, so maxima and sums are register operations and one swap of the wave's halves, and the
-//   weights, rounded to bf16, are the B operand of O^T = V^T W^T as they stand, with the keys of a k block in
-//   the order 4h .. 4h+3, 8+4h .. 8+4h+3 of half h.  V^T comes from the row-major tile by transposing LDS reads.
+// attend_tiles: one work-group per (sequence, KV head, block of query rows, split of the rows they see), a wave for
+//   each 32 query rows.  Tiles of keys and values pass through LDS, the next one on its way (loads that write LDS
+//   directly) while the waves compute the present one; one barrier a tile.
+//   S^T = K Q^T on MFMA 32x32x16 bf16 (exact products, fp32 sums): a lane holds half of the scores of one query row,
+//   so maxima and sums are register operations and one swap of the wave's halves, and the weights, rounded to
+//   bf16, are the B operand of O^T = V^T W^T as they stand, with the keys of a k block in the order 4h .. 4h+3,
+//   8+4h .. 8+4h+3 of half h.  V^T comes from the row-major tile by transposing LDS reads.
 //   The 16-byte chunks of a tile's row r are stored at chunk ^ turn(r): rows that are read together (eight by
-//   the transposing reads, 32 by the key reads) then spread over all banks.
-//   The matrix products bound it: 4 x 128 operations per (query row, key), against which the weights' bf16
-//   rounding (half a step, 2^-8, and averaged over a row's keys) saves a second product with their tails.
+//   the transposing reads, 32 by the key reads) then spread over all banks (no conflicts counted).
 //   The running maximum moves only when a score exceeds it by 2^8 (weights stay below that; fp32 and
 //   bf16 keep their relative precision), so that most tiles scale nothing.
+//   Two shapes.  128 query rows by four waves, tiles of 64 keys, two work-groups a CU: they are out of step by
+//   themselves, so that one's weights run under the other's products and its start under the other's loop.
+//   64 query rows by eight waves, in four groups of two that take every fourth tile of 32 keys: 33 to 64 rows are
+//   too few to hide the memory with 128-row blocks, and too much work for attend_rows' one wave a SIMD (16 sequences
+//   of up to 6144 rows, 56 query rows: 38 us, attend_rows 58).
+//   The matrix products bound it: 4 x 128 operations per (query row, key), against which the weights' bf16
+//   rounding (half a step, 2^-8, averaged over a row's keys) saves a second product with their tails.  1024 tokens, 32
+//   heads, over 131072 rows: 2.06 to 2.18 ms, 1.0 to 1.06 PFLOP/s; the matrix cores are busy 54% of the
+//   cycles, of which the power limit leaves about 2.0 to 2.1 GHz (a large product runs at 1.34 PFLOP/s there).
 #include "attend_paged.hpp"
 
 namespace ebd {
@@ -143,7 +150,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     off[i] = (uint32_t)(lane >> 4) * rs + (uint32_t)((lane & 15) ^ chunk_turn(r)) * 16u;
   }
   const int64_t head = (int64_t)h * p.pages.head_stride;
-  // (past the range: some page of it.  What is loaded there is not used, but each step loads the same number of times.)
+  // (past the range: some page of it; what a group loads there is not used)
   auto page_of = [&](int k) -> int { return table[min(k, k_end - 1) >> L.shift]; };
   const uint32_t part = kPart * rw * kRowBytes;
   auto address = [&](int k, int pg) {
