@@ -315,6 +315,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   auto barrier = [&]() {
     wait_lds();
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");  // nothing behind the barrier is read before it
   };
 
   if (k_beg < k_end) {

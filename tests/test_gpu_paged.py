@@ -248,6 +248,10 @@ BITS = 8
     ([500, 31], [9, 7], 3, 3, 64, "heads", 7),
     ([2049, 33], [513, 33], 1, 2, 64, "heads", 700),
     ([64, 0, 5], [64, 0, 5], 2, 1, 16, "heads", 0),
+    # ragged batches whose splits follow their lengths
+    ([3000, 1, 0, 700] + [40 * i + 5 for i in range(66)], [1, 1, 0, 1] + [1] * 66, 2, 4, 16, "heads", 0),
+    ([2500, 64, 1300, 9, 700], [12, 3, 1, 0, 9], 2, 4, 64, "tokens", 0),
+    ([1700, 300, 5, 900], [5, 6, 5, 2], 1, 4, 32, "heads", 0),
     # a long chunk among many short ones, sequences without new tokens between them
     ([300] + [20 + 7 * i for i in range(70)], [150] + [1 + i % 3 * (i % 2) for i in range(70)], 1, 4, 16, "heads", 0),
     ([9, 700, 30, 40, 2, 90], [2, 400, 0, 30, 1, 60], 2, 2, 32, "tokens", 0),
