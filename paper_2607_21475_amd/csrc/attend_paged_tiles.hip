@@ -11,8 +11,9 @@
 //   the transposing reads, 32 by the key reads) then spread over all banks (no conflicts counted).
 //   The running maximum moves only when a score exceeds it by 2^8 (weights stay below that; fp32 and
 //   bf16 keep their relative precision), so that most tiles scale nothing.
-//   Two shapes.  128 query rows by four waves, tiles of 64 keys, two work-groups a CU: they are out of step by
-//   themselves, so that one's weights run under the other's products and its start under the other's loop.
+//   Three shapes.  128 query rows by four waves, tiles of 64 keys, two work-groups a CU: they are out of step by
+//   themselves, so that one's weights run under the other's products and its start under the other's loop.  256 query
+//   rows by eight waves, one work-group a CU, for one sequence's long chunks: each tile is loaded half as often.
 //   64 query rows by eight waves, in four groups of two that take every fourth tile of 32 keys: 33 to 64 rows are
 //   too few to hide the memory with 128-row blocks, and too much work for attend_rows' one wave a SIMD (16 sequences
 //   of up to 6144 rows, 56 query rows: 38 us, attend_rows 58).
@@ -87,7 +88,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   constexpr int kStage = KG * 2 * kTile;
   constexpr int kMergeRow = 132;              // floats of a row's sums in LDS, padded
   constexpr int kMerge = KG > 1 ? KG * kRows * kMergeRow * 4 : 0;
-  __shared__ __align__(1024) uint8_t tiles[2 * kStage > kMerge ? 2 * kStage : kMerge];
+  // two stages; the query rows pass through the second, and past its end where they are more than it holds
+  constexpr int kThrough = kStage + kWaves * 32 * kRowBytes, kHeld = 2 * kStage > kThrough ? 2 * kStage : kThrough;
+  __shared__ __align__(1024) uint8_t tiles[kHeld > kMerge ? kHeld : kMerge];
+  static_assert(kThrough <= sizeof(tiles) && kWaves * 32 * kRowBytes <= sizeof(tiles), "query rows, finished rows");
   __shared__ uint32_t poisons[kWaves][32][8];   // of each query row, two bits an element
   __shared__ uint16_t notes[2][KG][KEYS][16];   // of a tile's values, 16 bits a chunk
   __shared__ int noted[2][KG][RW];              // ... whether a wave noted any
@@ -472,7 +476,8 @@ hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {
   const dim3 grid((unsigned)attend_paged_groups(L));
   if (L.rows == kFewRows && L.once) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, true>), grid, dim3(512), 0, s, L);
   else if (L.rows == kFewRows) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, false>), grid, dim3(512), 0, s, L);
-  else hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64, false>), grid, dim3(256), 0, s, L);
+  else if (L.rows == kTileRows) hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64, false>), grid, dim3(256), 0, s, L);
+  else hipLaunchKernelGGL((attend_tiles_kernel<8, 1, 64, false>), grid, dim3(512), 0, s, L);
   return hipGetLastError();
 }
 

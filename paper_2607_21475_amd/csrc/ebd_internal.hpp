@@ -226,6 +226,7 @@ constexpr int kRowsWaves = 4;      // waves of an attend_rows work-group
 constexpr int kRowsKernelMax = 32;  // query rows of a KV head up to which a launch takes attend_rows
 constexpr int kFewRows = 64;       // query rows of an attend_tiles work-group that splits the keys, too
 constexpr int kTileRows = 128;     // ... of one that does not
+constexpr int kLongRows = 256;     // ... of one alone on its CU
 
 constexpr int64_t kMaxBlocks = 8192;  // blocks per unit of ebd_block_contributions (LDS bins)
 constexpr int kBlockWaves = 8;        // most waves of its work-groups

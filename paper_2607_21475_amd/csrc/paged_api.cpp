@@ -103,7 +103,7 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t ro
   L.p = *p;
   L.rows = rows;
   L.at_most = INT64_MAX;
-  const bool tiles = rows == kTileRows;
+  const bool tiles = rows >= kTileRows;
   const int64_t S = p->pages.num_seqs, H = p->pages.kv_heads;
   // Every sequence has at most a block that is not full; blocks set aside for the longest sequence cost an
   // empty work-group each where there are none (64 sequences, one of 2048 tokens: 32768 of them, about 130 us).
@@ -116,7 +116,7 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t ro
   span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
   const int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
   L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
-  L.nsplit = (int32_t)(tiles ? splits(full * H, span, 2 * kCus, kTilesLeast, kTilesStartRows)
+  L.nsplit = (int32_t)(tiles ? splits(full * H, span, rows == kTileRows ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows)
                              : splits(full * H, span, kCus, kRowsLeast, kStartRows));
   // keys and values that one work-group alone reads, and too many to stay in the last-level cache until the next call
   // on the same layer (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
@@ -139,6 +139,19 @@ struct AttendPagedPlan {
   AttendPagedLaunch part[2];
   int parts;
 };
+// Whether blocks of 256 query rows, one work-group a CU, serve a call: they load every tile half as often, and have
+// nothing to run under a start, an end or another's shorter block.  So only where the work-groups fill the chip once,
+// the blocks are full and see about the same rows, which a call knows of one sequence.  us by 128 rows / by 256, 8 KV
+// heads of 4 query heads, taken: 1024 tokens over 131072 rows 2197 / 2053, 32768 558 / 540, under a window of 2048 71 / 68,
+// 2048 over 16384 513 / 504, 512 over 4096 61 / 60; not taken: 8192 over 8192 571 / 567, 2048 over 8192 257 / 265, 1500
+// over 6000 167 / 180, 256 over 1024 30 / 35, 160 (a block half empty) over 32768 122 / 130; 8 ragged sequences of up to
+// 256 over up to 16384 320 / 420.
+bool long_blocks(const ebd_attend_paged_params *p, int64_t most) {
+  if (p->pages.num_seqs != 1 || most < kLongRows || (int64_t)p->max_new * 8 > p->max_rows) return false;
+  const AttendPagedLaunch L = attend_paged_part(p, kLongRows, most, std::min<int64_t>(p->num_tokens * p->group, most));
+  const int64_t groups = attend_paged_groups(L), rows = (most + kLongRows - 1) / kLongRows * kLongRows;
+  return groups <= kCus && 8 * groups >= 7 * kCus && 8 * most >= 7 * rows;
+}
 AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
   const int64_t S = p->pages.num_seqs, G = p->group, most = (int64_t)p->max_new * G;
   const int64_t sum = std::min<int64_t>(p->num_tokens * G, S * most);
@@ -152,6 +165,8 @@ AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
     plan.part[1].at_most = small;
     plan.part[0] = attend_paged_part(p, rows, most, sum);
     plan.part[0].more_than = small;
+  } else if (long_blocks(p, most)) {
+    plan.part[0] = attend_paged_part(p, kLongRows, most, sum);
   } else {
     plan.part[0] = attend_paged_part(p, rows, most, sum);
   }

@@ -434,6 +434,35 @@ def test_offsets_past_32_bits():
         ref.check(y, ry, ty, "y")
 
 
+# one sequence whose blocks of 256 query rows fill the chip once: in splits, with explicit positions, under a window,
+# without splits
+@pytest.mark.parametrize("n,m,G,qpos,window", [(9001, 500, 4, False, 0), (9001, 500, 4, True, 0),
+                                               (9001, 500, 4, False, 5000), (4224, 510, 16, False, 0)])
+def test_attend_long_blocks(n, m, G, qpos, window):
+    """Every 37th token and the last against the formula; an infinity that some rows see."""
+    _say("attend long", n, m, G, qpos, window)
+    hold = 197 if not window else n - m - window + 200  # (some rows' window begins behind it)
+    gen = _gen(n + m + G + qpos)
+    c = ref.Cache([n], 8, 64, gen, fill=math.nan)
+    c.V[int(c.table[0, hold // 64]), 0, hold % 64, 7] = INF
+    hi = torch.arange(n - m, n, device="cuda", dtype=torch.int32)
+    if qpos:
+        hi = torch.randint(-1, n, (m,), generator=gen, device="cuda").to(torch.int32)
+    q, y, lse, st = _attend(c, [m], G, hi=hi if qpos else None, window=window)
+    assert not bool(st.any())
+    pick = torch.zeros(m, dtype=torch.bool, device="cuda")
+    pick[::37] = True
+    pick[-1] = True
+    # the reference's other tokens see nothing
+    ry, rl, ty, tl = ref.attend(c, q, [m], hi=torch.where(pick, hi, -1), window=window, weights_bits=BITS)
+    inf = torch.zeros_like(y, dtype=torch.bool)
+    inf[:, :G, 7] = ((hi >= hold) & ((hi - window < hold) if window else True))[:, None]
+    assert bool((y[inf] == INF).all()) and bool(y[~inf].isfinite().all())
+    zero = torch.zeros((), dtype=torch.float64, device="cuda")
+    ref.check(torch.where(inf, zero, y.double())[pick], torch.where(inf, zero, ry)[pick], torch.where(inf, zero, ty)[pick], "y")
+    ref.check(lse[pick], rl[pick], tl[pick], "lse")
+
+
 def test_two_streams_and_a_graph():
     """Calls on two side streams at once, and a captured step replayed with the program's own work between."""
     import paper_2607_21475_amd as ebd
