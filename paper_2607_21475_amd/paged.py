@@ -236,9 +236,9 @@ def rotary(freq: Optional[torch.Tensor], layout: int = EBD_ROPE_HALF, amplitude:
     r.layout, r.amplitude = int(layout), float(amplitude)
     r.flags = EBD_ROPE_INVERSE if inverse else 0
     if freq is not None:
+        r.freq = _ptr(freq, torch.float64, "freq")
         if freq.dim() != 1 or not 1 <= freq.numel() <= HEAD_DIM // 2:
             raise ValueError("freq must be [rot_dim / 2], 1 to %d of them" % (HEAD_DIM // 2))
-        r.freq = _ptr(freq, torch.float64, "freq")
         r.rot_dim = 2 * freq.numel()
     r.keep = freq
     return r
@@ -272,12 +272,13 @@ def pages(K, V, page_table) -> ebd_pages:
     if K.shape != V.shape or K.stride() != V.stride():
         raise ValueError("K and V must have the same shape and strides")
     _distinct(K, "K")
-    if page_table.dim() != 2:
+    table = _ptr(page_table, torch.int32, "page_table")
+    if page_table is None or page_table.dim() != 2:
         raise ValueError("page_table must be [sequences, pages per sequence]")
     P = ebd_pages()
     P.num_pages, P.kv_heads, P.page_size, P.head_dim = *K.shape[:3], HEAD_DIM
     P.num_seqs, P.max_pages = page_table.shape
-    P.page_table = _ptr(page_table, torch.int32, "page_table")
+    P.page_table = table
     # strides over one page, head or row are never used, and may be anything
     P.page_stride, P.head_stride, P.row_stride = (s if n > 1 else HEAD_DIM
                                                   for n, s in zip(K.shape[:3], K.stride()[:3]))
@@ -368,6 +369,8 @@ def ebd_append_paged(params: ebd_append_paged_params, k_new, v_new, K, V, q=None
 def ebd_attend_paged(params: ebd_attend_paged_params, q, K, V, y, workspace, lse=None, status=None,
                      stream=None) -> None:
     """Attention of the new tokens over the paged cache (asynchronous)."""
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
     code = _lib.ebd_attend_paged(params.at, _arg(params, "q", q), _arg(params, "K", K), _arg(params, "V", V),
                                  _arg(params, "y", y), _out(params, "lse", lse, torch.float32, params.heads),
                                  _out(params, "status", status, _I32, params.seqs),

@@ -197,6 +197,18 @@ def test_binding_refuses_wrong_tensors():
         ebd.pages(K[:1].expand(3, 2, 16, 128), K[:1].expand(3, 2, 16, 128), table)
 
 
+def test_binding_names_what_is_not_a_tensor():
+    K = torch.zeros(2, 1, 16, 128, dtype=torch.bfloat16)
+    with pytest.raises(TypeError, match="page_table"):
+        ebd.pages(K, K, [[0, 1]])
+    with pytest.raises(ValueError, match="page_table"):
+        ebd.pages(K, K, None)
+    with pytest.raises(TypeError, match="freq"):
+        ebd.rotary([1.0, 0.1])
+    with pytest.raises(TypeError, match="workspace"):
+        ebd.ebd_attend_paged(_attend_params(), K, K, K, K, None)
+
+
 def test_rope_frequencies():
     f, a = ebd.rope_frequencies(8, 10000.0, device="cpu")
     assert a == 1.0 and torch.allclose(f, torch.tensor([1.0, 0.1, 0.01, 0.001], dtype=torch.float64), rtol=1e-14)
