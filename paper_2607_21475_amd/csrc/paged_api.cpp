@@ -67,22 +67,27 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
 }
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split over the rows they see where that
-// ends the launch sooner.  A work-group takes its split's rows and what a start, an end and a share of the join
-// cost, about as long as kStartRows more; as many run at once as the chip holds (one a CU, or two of attend_tiles
+// ends the launch sooner.  A work-group takes its split's rows and what a start and an end cost, about as long
+// as kStartRows more; as many run at once as the chip holds (one a CU, or two of attend_tiles
 // with 128 query rows).  Up to two rounds of them the launch ends with its last round, however full; past that the
-// work-groups are out of step and end about half of one after each other.  us, without splits beyond 256 work-groups / by
-// this rule: 33 sequences of up to 15000 rows (264 units) 218 / 193; by rounds alone, 32 chunks of up to 512 tokens over
+// work-groups are out of step and end about half of one after each other.  Splits also cost the join: its launch, and
+// the partial sums (us without that / with it, 8 KV heads of 4 query heads: 1024 tokens over 1024 rows 49.0 / 33.0, 4 of 256
+// over 1024 51.0 / 34.5, one token over 300 rows 13.4 / 11.5; with it not split, 512 over 512 28.1 / 20.9).
+// us, without splits beyond 256 work-groups / by this rule: 33 sequences of up to 15000 rows (264 units) 218 / 193; by rounds alone, 32 chunks of up to 512 tokens over
 // up to 8192 rows 939, by this rule 770.  Units that fill the first round: 384, 512, 768 or 1024 work-groups / 256: 8
 // sequences of 16384 rows 95, 94, 93, 97 / 90, 16 of up to 6144 rows 40, 36, 38, 40 / 32.
 constexpr int64_t kCus = 256;
 constexpr int64_t kRowsLeast = 128;  // fewest rows of a split: a tile for each wave, or eight tiles
-constexpr int64_t kTilesLeast = 512;
+// us by 512 / 256 / 128: 64 tokens over 1024 rows 24.5 / 21.1 / 21.0, 128 over 2048 28.4 / 24.7 / 27.6
+constexpr int64_t kTilesLeast = 256;
 constexpr int64_t kStartRows = 320;
 constexpr int64_t kTilesStartRows = 640;
+constexpr double kTilesJoin = 250.0;  // (and a row for each 128 query rows' sums, 135 KB written and read)
+constexpr double kRowsJoin = 300.0;
 constexpr int64_t kSplitsMost = 256;
 constexpr int64_t kCacheBytes = (int64_t)64 << 20;
 
-int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start) {
+int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start, double join, double join_each) {
   const int64_t most = std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least));
   int64_t best = 1;
   double cost = 0.0;
@@ -91,7 +96,7 @@ int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_
     const int64_t rows = ((span + ns - 1) / ns + 127) / 128 * 128;
     const int64_t groups = units * ((span + rows - 1) / rows);  // (rounded up, the size may leave fewer splits)
     const double rounds = groups <= 2 * slots ? (double)((groups + slots - 1) / slots) : (double)groups / (double)slots + 0.5;
-    const double c = rounds * (double)(rows + start);
+    const double c = rounds * (double)(rows + start) + (ns > 1 ? join + join_each * (double)groups : 0.0);
     if (i == 0 || c < cost) best = ns, cost = c;
   }
   return best;
@@ -116,8 +121,12 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t ro
   span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
   const int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
   L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
-  L.nsplit = (int32_t)(tiles ? splits(full * H, span, rows == kTileRows ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows)
-                             : splits(full * H, span, kCus, kRowsLeast, kStartRows));
+  if (tiles) {
+    L.nsplit = (int32_t)splits(full * H, span, rows == kTileRows ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows,
+                               kTilesJoin, (double)rows / kTileRows);
+  } else {
+    L.nsplit = (int32_t)splits(full * H, span, kCus, kRowsLeast, kStartRows, kRowsJoin, 0.0);
+  }
   // keys and values that one work-group alone reads, and too many to stay in the last-level cache until the next call
   // on the same layer (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
   // to 4096 rows 124 / 111, 16 of up to 6144 rows, 8 tokens, 41.5 / 39.1; one of 4096 rows, found in the cache, 14.4 / 15.3

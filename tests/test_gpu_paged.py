@@ -240,6 +240,9 @@ BITS = 8
     ([700, 20, 64, 9], [8, 3, 1, 0], 4, 7, 32, "tokens", 0),
     ([130, 64], [130, 7], 2, 3, 16, "heads", 0),
     ([257], [257], 1, 8, 128, "heads", 0),
+    ([1024], [64], 2, 4, 16, "heads", 0),  # short splits of few blocks
+    ([777, 520, 300], [80, 40, 300], 2, 4, 64, "tokens", 0),
+    ([300, 1], [1, 1], 2, 4, 16, "heads", 0),
     ([600, 511, 90], [300, 1, 90], 2, 4, 64, "tokens", 100),
     ([1000, 40], [1, 1], 2, 16, 256, "heads", 33),
     ([300], [64], 1, 17, 16, "heads", 1),
