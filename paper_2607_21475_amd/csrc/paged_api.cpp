@@ -67,15 +67,15 @@ bool supported_attend_paged(const ebd_attend_paged_params *p) {
 }
 
 // How a launch is cut.  Units (sequence, KV head, block of query rows) are split over the rows they see where that
-// ends the launch sooner.  A work-group takes its split's rows and what a start and an end cost, about as long
-// as kStartRows more; as many run at once as the chip holds (one a CU, or two of attend_tiles
-// with 128 query rows).  Up to two rounds of them the launch ends with its last round, however full; past that the
-// work-groups are out of step and end about half of one after each other.  Splits also cost the join: its launch, and
-// the partial sums (us without that / with it, 8 KV heads of 4 query heads: 1024 tokens over 1024 rows 49.0 / 33.0, 4 of 256
-// over 1024 51.0 / 34.5, one token over 300 rows 13.4 / 11.5; with it not split, 512 over 512 28.1 / 20.9).
-// us, without splits beyond 256 work-groups / by this rule: 33 sequences of up to 15000 rows (264 units) 218 / 193; by rounds alone, 32 chunks of up to 512 tokens over
-// up to 8192 rows 939, by this rule 770.  Units that fill the first round: 384, 512, 768 or 1024 work-groups / 256: 8
-// sequences of 16384 rows 95, 94, 93, 97 / 90, 16 of up to 6144 rows 40, 36, 38, 40 / 32.
+// ends the launch sooner.  A work-group takes its split's rows and what a start and an end cost, about as long as
+// kStartRows more; as many run at once as the chip holds (one a CU, or two of attend_tiles with 128 query rows).  Up
+// to two rounds of them the launch ends with its last round, however full; past that the work-groups are out of step
+// and end about half of one after each other.  Splits also cost the join: its launch, and the partial sums.  us, 8 KV
+// heads of 4 query heads, without the join's cost / with it: 1024 tokens over 1024 rows 44.8 / 33.0, 4 of 256 over
+// 1024 51.2 / 34.5, 512 over 512 28.1 / 20.9, one token over 300 rows 13.4 / 11.5; without splits beyond 256
+// work-groups / by this rule: 33 sequences of up to 15000 rows (264 units) 218 / 193; by rounds alone / by this rule:
+// 32 chunks of up to 512 tokens over up to 8192 rows 939 / 770.  Units that fill the first round, 384, 512, 768 or
+// 1024 work-groups / 256: 8 sequences of 16384 rows 95, 94, 93, 97 / 90, 16 of up to 6144 rows 40, 36, 38, 40 / 32.
 constexpr int64_t kCus = 256;
 constexpr int64_t kRowsLeast = 128;  // fewest rows of a split: a tile for each wave, or eight tiles
 // us by 512 / 256 / 128: 64 tokens over 1024 rows 24.5 / 21.1 / 21.0, 128 over 2048 28.4 / 24.7 / 27.6
