@@ -315,7 +315,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     for (int v = 0; v < kRowsWaves; ++v) {
       const float *Ov = reinterpret_cast<const float *>(lds + v * kWaveLds);
       const float2 t = reinterpret_cast<const float2 *>(Ov + kRows * kMergeRow)[r];
-      if (t.x == -INFINITY) continue;  // this wave saw nothing of the row
+      if (t.y == 0.0f) continue;  // this wave saw nothing of the row
       const float a = fast_exp2(t.x - M);
       Z += a * t.y;
 #pragma unroll
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     if (L.nsplit > 1) {
       float *part = L.part + (slot * kRows + r) * kHeadDim + e;
       if (e == 0) L.stats[slot * kRows + r] = make_float2(M, Z);
-      if (M == -INFINITY) continue;
+      if (Z == 0.0f) continue;
       *reinterpret_cast<f32x4 *>(part) = f32x4{o[0], o[1], o[2], o[3]};
       *reinterpret_cast<f32x4 *>(part + 4) = f32x4{o[4], o[5], o[6], o[7]};
     } else {
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
     M = mn;
 #pragma unroll
     for (int i = 0; i < kMany; ++i) {
-      if (t[i].x == -INFINITY) continue;  // nothing seen: its sums were not written
+      if (t[i].y == 0.0f) continue;  // nothing seen: its sums were not written
       const float w = fast_exp2(t[i].x - M);
       Z += w * t[i].y;
 #pragma unroll
@@ -394,9 +394,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendPagedLaunch L) {
   // the quarters, in a fixed order
   const float all = max_xor16_32(M);
   const float a = M == -INFINITY ? 0.0f : fast_exp2(M - all);
+  const bool seen = Z != 0.0f;
   Z = add_xor32(add_xor16(Z * a));
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = add_xor32(add_xor16(a == 0.0f ? 0.0f : o[j] * a));
+  for (int j = 0; j < 8; ++j) o[j] = add_xor32(add_xor16(seen ? o[j] * a : 0.0f));
   const int j = L.by_group.quotient(row);
   if (g == 0) store_row(L, sq.t0 + j, h * G + row - j * G, e, all, Z, o);
 }

@@ -191,10 +191,11 @@ __device__ __forceinline__ Range range_of_tokens(const ebd_attend_paged_params &
 }
 
 // Elements e .. e+7 of a finished row: token t, query head hq, sums o over weights that total Z with the
-// maximum M (-inf: the row saw nothing).
+// maximum M.  A row, or a part of one, that saw nothing has Z = 0, and no other: the key at the maximum weighs 1, and a
+// logit that is NaN makes Z NaN, though no maximum shows it (M stays -inf where there are no others).
 __device__ __forceinline__ void store_row(const AttendPagedLaunch &L, int64_t t, int hq, int e, float M, float Z,
                                           const float (&o)[8]) {
-  const bool any = M != -INFINITY;
+  const bool any = Z != 0.0f;
   const float a = any ? 1.0f / Z : 0.0f;
   uint4 v;
   v.x = any ? pack_bf16(o[0] * a, o[1] * a) : 0u;

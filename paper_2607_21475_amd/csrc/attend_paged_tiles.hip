@@ -410,7 +410,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
 #pragma unroll
       for (int v = 0; v < KG; ++v) {
         const float2 t = merged[v][r];
-        if (t.x == -INFINITY) continue;  // this group saw nothing of the row
+        if (t.y == 0.0f) continue;  // this group saw nothing of the row
         const float a = fast_exp2(t.x - M);
         Z += a * t.y;
 #pragma unroll
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       }
       if (L.nsplit > 1) {
         if (e == 0) L.stats[slot + r] = make_float2(M, Z);
-        if (M == -INFINITY) continue;
+        if (Z == 0.0f) continue;
         float *part_of = L.part + (slot + r) * kHeadDim + e;
         *reinterpret_cast<f32x4 *>(part_of) = f32x4{o[0], o[1], o[2], o[3]};
         *reinterpret_cast<f32x4 *>(part_of + 4) = f32x4{o[4], o[5], o[6], o[7]};
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   if (L.nsplit > 1) {
     if (r >= nrow) return;
     if (half == 0) L.stats[slot + r] = sees ? make_float2(m, z) : make_float2(-INFINITY, 0.0f);
-    if (!sees || m == -INFINITY) return;
+    if (!sees || z == 0.0f) return;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
 #pragma unroll
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     return;
   }
   // finished rows go through LDS, so that they leave as whole rows
-  const bool any = sees && m != -INFINITY;
+  const bool any = sees && z != 0.0f;
   const float a = any ? 1.0f / z : 0.0f;
   const int64_t j = token(row);
   if (half == 0 && L.lse && r < nrow)

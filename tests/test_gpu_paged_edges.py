@@ -1,0 +1,97 @@
+"""Paged-cache operators on the GPU where values are not finite, bounds are wrong or tokens are padding."""
+import math
+
+import pytest
+import torch
+
+import paged_ref as ref
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+INF = float("inf")
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _attend(c, news, G, q=None, seed=0, hi=None, window=0, max_rows=None):
+    import paper_2607_21475_amd as ebd
+
+    T = sum(news)
+    if q is None:
+        q = ref.spaced((T, c.kv * G, 128), _gen(seed + 1), False)
+    y = torch.full((T, c.kv * G, 128), 7.0, dtype=BF, device="cuda")
+    lse = torch.full((T, c.kv * G), 7.0, dtype=torch.float32, device="cuda")
+    off = torch.tensor([0] + [sum(news[:i + 1]) for i in range(len(news))], device="cuda")
+    st = torch.zeros(len(news), dtype=torch.int32, device="cuda")
+    p = ebd.attend_paged_params(ebd.pages(c.K, c.V, c.table), q, y, off, c.len, max(news),
+                                max(c.lens) if max_rows is None else max_rows, qpos=hi, window=window)
+    ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, p))
+    ws.fill_(255)
+    ebd.ebd_attend_paged(p, q, c.K, c.V, y, ws, lse=lse, status=st)
+    return q, y, lse, st
+
+
+def _agree(got, want, tol, what):
+    """As ref.check, with NaN where the formula has NaN and nowhere else."""
+    got, want = got.double(), want.double()
+    assert torch.equal(got.isnan(), want.isnan()), "%s: %d NaN, the formula has %d" % (
+        what, int(got.isnan().sum()), int(want.isnan().sum()))
+    zero = torch.zeros((), dtype=torch.float64, device=got.device)
+    nan = want.isnan()
+    ref.check(torch.where(nan, zero, got), torch.where(nan, zero, want), torch.where(nan, zero, tol), what)
+
+
+# Query rows of a KV head and rows of the sequence: each kernel and shape, with the rows split and not.
+SHAPES = [([1], 4, 33), ([1], 4, 4097), ([2], 3, 20001), ([3], 4, 20), ([5], 4, 130), ([6], 4, 3000), ([14], 4, 200),
+          ([14], 4, 5000), ([70], 2, 150), ([40], 4, 2500), ([500], 4, 9001)]
+
+
+def _picked(m):
+    """Tokens that are compared with the formula: all of a few, every 41st and the last of many."""
+    return torch.tensor(sorted(set(range(0, m, 1 if m < 100 else 41)) | {m - 1}), device="cuda")
+
+
+def _against(c, q, y, lse, m, n, what, window=0):
+    """The picked tokens against the formula (the others see nothing in the reference and are left out)."""
+    pick = _picked(m)
+    hi = torch.full((m,), -1, dtype=torch.int32, device="cuda")
+    hi[pick] = (n - m + pick).to(torch.int32)
+    ry, rl, ty, tl = ref.attend(c, q, [m], hi=hi, window=window, weights_bits=8)
+    _agree(y[pick], ry[pick], ty[pick], what + ", y")
+    _agree(lse[pick], rl[pick], tl[pick], what + ", lse")
+    return ry[pick]
+
+
+@pytest.mark.parametrize("news,G,n", SHAPES)
+def test_a_query_that_holds_nan_gives_nan(news, G, n):
+    """... and only there: the other rows of its block are what they were."""
+    m, kv = news[0], 8 if n == 9001 else 2
+    print("nan query", m, G, n, flush=True)
+    c = ref.Cache([n], kv, 16, _gen(n + m))
+    q = ref.spaced((m, kv * G, 128), _gen(1), False)
+    for t, h in {(0, 0), (m - 1, kv * G - 1), (m // 2 // 41 * 41, G)}:
+        q[t, h, 5] = math.nan
+    _, y, lse, st = _attend(c, news, G, q=q)
+    assert not bool(st.any())
+    want = _against(c, q, y, lse, m, n, "nan query")
+    assert bool(want.isnan().any()) and not bool(want.isnan().all())
+
+
+@pytest.mark.parametrize("news,G,n", SHAPES)
+def test_keys_that_hold_nan_give_nan_to_all_that_see_them(news, G, n):
+    """One key, the last of all, a tile of 32, all: whichever wave, group or split they fall to."""
+    m, kv = news[0], 8 if n == 9001 else 1
+    print("nan keys", m, G, n, flush=True)
+    c = ref.Cache([n], kv, 16, _gen(n + m))
+    K0 = c.K.clone()
+    for first, last in ((0, 1), (n - 1, n), (n // 2, n // 2 + 1), (n // 64 * 32, min(n, n // 64 * 32 + 32)), (0, n)):
+        for r in range(first, last):
+            c.K[int(c.table[0, r // 16]), 0, r % 16, 3] = math.nan
+        q, y, lse, _ = _attend(c, news, G)
+        want = _against(c, q, y, lse, m, n, "nan keys %d to %d" % (first, last))
+        assert bool(want.isnan().any())
+        c.K.copy_(K0)
