@@ -495,14 +495,16 @@ ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q,
  * ebd_gather_paged -- read the paged cache out as units: unit u = s * kv_heads + h receives rows
  * 0 .. seq_off[u+1]-seq_off[u]-1 of sequence s and head h, contiguous, as ebd_scores and ebd_evict take them.
  *   seq_off [num_seqs * kv_heads + 1] device int64, non-decreasing; max_rows >= the longest unit (sizes the
- *   grid; rows of a longer unit past it are not written, and flagged EBD_ST_BAD_LAYOUT).
- *   Ku, Vu [rows, 128] bf16.  status [units] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a row has no page
+ *   grid; rows of a longer unit past it are not written, and flagged EBD_ST_BAD_LAYOUT; 0: the call does nothing).
+ *   Ku, Vu [num_rows, 128] bf16: rows that seq_off places outside them are not written, and flagged
+ *   EBD_ST_BAD_LAYOUT.  status [units] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a row has no page
  *   (it is written as zeros).
  */
 typedef struct ebd_gather_paged_params {
     ebd_pages pages;
     int64_t max_rows;
     const int64_t *seq_off;
+    int64_t num_rows;
 } ebd_gather_paged_params;
 
 ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K, const uint16_t *V,

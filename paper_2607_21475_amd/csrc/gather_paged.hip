@@ -35,7 +35,9 @@ __global__ __launch_bounds__(kGatherPagedThreads) void gather_paged_kernel(Gathe
   const int s = u / P.kv_heads, h = u % P.kv_heads;
   const int64_t u0 = L.p.seq_off[u], n = L.p.seq_off[u + 1] - u0;
   const int64_t seen = min(n, L.p.max_rows);
-  if (c == 0 && threadIdx.x == 0 && n > L.p.max_rows && L.status) atomicOr(&L.status[u], EBD_ST_BAD_LAYOUT);
+  const bool outside = seen > 0 && (u0 < 0 || u0 > L.p.num_rows - seen);  // some rows have no place in Ku and Vu
+  if (c == 0 && threadIdx.x == 0 && (n > L.p.max_rows || outside) && L.status)
+    atomicOr(&L.status[u], EBD_ST_BAD_LAYOUT);
   const int64_t r0 = (int64_t)c * kGatherPagedRows + threadIdx.x / 16;
   if (r0 - threadIdx.x / 16 >= seen) return;
   const int e = threadIdx.x % 16 * 8;
@@ -55,7 +57,7 @@ __global__ __launch_bounds__(kGatherPagedThreads) void gather_paged_kernel(Gathe
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t r = r0 + 16 * j;
-    if (r < seen) {
+    if (r < seen && (uint64_t)(u0 + r) < (uint64_t)L.p.num_rows) {
       store<NT>(L.Ku + (u0 + r) * kHeadDim + e, k[j]);
       store<NT>(L.Vu + (u0 + r) * kHeadDim + e, v[j]);
     }

@@ -289,7 +289,7 @@ ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q,
 
 ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K, const uint16_t *V,
                             uint16_t *Ku, uint16_t *Vu, uint32_t *status, void *stream) {
-  if (!p || !valid_pages(p->pages) || p->max_rows < 0) return EBD_ERR_INVALID_ARG;
+  if (!p || !valid_pages(p->pages) || p->max_rows < 0 || p->num_rows < 0) return EBD_ERR_INVALID_ARG;
   if (!supported_pages(p->pages) || p->max_rows > kRowsMax || gather_paged_groups(*p) > kGridMax) return EBD_ERR_UNSUPPORTED;
   if (p->pages.num_seqs == 0 || p->max_rows == 0) return EBD_OK;
   if (!K || !V || !Ku || !Vu || !p->seq_off) return EBD_ERR_INVALID_ARG;

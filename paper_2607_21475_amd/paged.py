@@ -112,6 +112,7 @@ class ebd_gather_paged_params(ctypes.Structure):
         ("pages", ebd_pages),
         ("max_rows", ctypes.c_int64),
         ("seq_off", ctypes.c_void_p),
+        ("num_rows", ctypes.c_int64),
     ]
 
 
@@ -339,7 +340,8 @@ def attend_paged_params(pgs: ebd_pages, q, y, new_off, len, max_new: int, max_ro
 
 
 def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_paged_params:
-    """Units seq_off [sequences * KV heads + 1] int64, the longest at most max_rows."""
+    """Units seq_off [sequences * KV heads + 1] int64, the longest at most max_rows.  The rows that there is room for
+    are those of each call's outputs."""
     p = ebd_gather_paged_params()
     p.pages, p.max_rows = pgs, int(max_rows)
     p.seq_off = _table(seq_off, torch.int64, (pgs.num_seqs * pgs.kv_heads + 1,), "seq_off")
@@ -380,9 +382,14 @@ def ebd_attend_paged(params: ebd_attend_paged_params, q, K, V, y, workspace, lse
 
 
 def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None, stream=None) -> None:
-    """Read the pages out as units Ku, Vu [rows, 128] (asynchronous)."""
-    code = _lib.ebd_gather_paged(params.at, _arg(params, "K", K), _arg(params, "V", V),
-                                 _out(params, "Ku", Ku, _BF, None), _out(params, "Vu", Vu, _BF, None),
+    """Read the pages out as units Ku, Vu [rows, 128], of the same size (asynchronous)."""
+    ku, vu = _out(params, "Ku", Ku, _BF, None), _out(params, "Vu", Vu, _BF, None)
+    shape = None if Ku is None else Ku.shape
+    if shape is None or Vu is None or len(shape) != 2 or shape[1] != HEAD_DIM or Vu.shape != shape:
+        raise ValueError("Ku and Vu must both be [rows, %d]" % HEAD_DIM)
+    p = ebd_gather_paged_params.from_buffer_copy(params)  # (of this call: calls on the same parameters may overlap)
+    p.num_rows = shape[0]
+    code = _lib.ebd_gather_paged(ctypes.addressof(p), _arg(params, "K", K), _arg(params, "V", V), ku, vu,
                                  _out(params, "status", status, _I32, params.units), _on_stream(params, stream))
     _check("ebd_gather_paged", code)
 

@@ -95,3 +95,57 @@ def test_keys_that_hold_nan_give_nan_to_all_that_see_them(news, G, n):
         want = _against(c, q, y, lse, m, n, "nan keys %d to %d" % (first, last))
         assert bool(want.isnan().any())
         c.K.copy_(K0)
+
+
+def _gather_params(c, off, max_rows):
+    import paper_2607_21475_amd as ebd
+
+    return ebd.gather_paged_params(ebd.pages(c.K, c.V, c.table), torch.tensor(off, device="cuda"), max_rows)
+
+
+@pytest.mark.parametrize("first,short", [(0, 0), (0, 1), (0, 70), (0, 171), (0, 300), (-1, 0), (-70, 0), (-130, 5), (10, 0),
+                                         (1 << 40, 0), (-(1 << 40), 0)])
+def test_gather_writes_no_row_outside_its_outputs(first, short):
+    """Units that seq_off places before, across and behind the ends of Ku and Vu, which lie between guard rows."""
+    import paper_2607_21475_amd as ebd
+
+    print("gather bounds", first, short, flush=True)
+    lens, kv = [100, 50], 2
+    c = ref.Cache(lens, kv, 16, _gen(6))
+    off = [0, 100, 200, 250, 300]
+    rows, guard = 300 - short, 400
+    big = torch.full((2, guard + rows + guard, 128), 7.0, dtype=BF, device="cuda")
+    Ku, Vu = big[0, guard:guard + rows], big[1, guard:guard + rows]
+    st = torch.zeros(4, dtype=torch.int32, device="cuda")
+    p = _gather_params(c, [o + first for o in off], 100)
+    if rows == 0:  # outputs without memory, which the entry point refuses
+        with pytest.raises(ebd.EbdError):
+            ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu, status=st)
+        return
+    ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu, status=st)
+    want = torch.full_like(big, 7.0)
+    flags = []
+    for u, (a, b) in enumerate(zip(off, off[1:])):
+        lo, hi = max(a + first, 0), min(b + first, rows)
+        flags.append(0 if (lo, hi) == (a + first, b + first) else ebd.EBD_ST_BAD_LAYOUT)
+        if lo < hi:
+            for x, pool in zip(want, (c.K, c.V)):
+                x[guard + lo:guard + hi] = c.rows(pool, u // kv, u % kv)[lo - a - first:hi - a - first]
+    assert torch.equal(big, want) and st.tolist() == flags
+
+
+def test_gather_refuses_outputs_of_other_shapes():
+    import paper_2607_21475_amd as ebd
+
+    c = ref.Cache([20], 2, 16, _gen(6))
+    p = _gather_params(c, [0, 20, 40], 20)
+    x = torch.zeros((40, 128), dtype=BF, device="cuda")
+    for Ku, Vu in ((x, x[:39]), (x[:39], x), (x.view(80, 64), x.view(80, 64)), (x.view(-1), x.view(-1)),
+                   (x.view(20, 2, 128), x.view(20, 2, 128)), (x, None), (None, x)):
+        with pytest.raises(ValueError):
+            ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu)
+    # the same parameters serve outputs of other sizes
+    for rows in (40, 43, 40):
+        Ku, Vu = (torch.full((rows, 128), 7.0, dtype=BF, device="cuda") for _ in range(2))
+        ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu)
+        assert torch.equal(Ku[:40], torch.cat([c.rows(c.K, 0, h) for h in range(2)])) and bool((Ku[40:] == 7).all())
