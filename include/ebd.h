@@ -459,7 +459,8 @@ ebd_status ebd_append_paged(const ebd_append_paged_params *p, const uint16_t *k_
  *     lse = ln sum_{r = lo..hi} exp(scale q.k_r)            [tokens, q_heads] fp32, or NULL
  *   A token that sees no row (hi < 0, every row on a bad page) gets y = 0 and lse = -inf.  A row that a
  *   token does not see has no effect on it, whatever its key and value hold, infinities and NaN included.
- *   A logit that is NaN (of a query or a key that holds one) makes y and lse of the rows that see it NaN.
+ *   A logit that is NaN (of a query or a key that holds one) makes y and lse of the rows that see it NaN; an infinite
+ *   value makes its element of y infinite (NaN with one of the other sign, and perhaps where its weight is below 2^-126).
  *   new_off, len as for ebd_append_paged; num_tokens: tokens in q and y.  y and lse of padding tokens
  *   (before new_off[0], from new_off[num_seqs] on) are left as they were.
  *   max_new, max_rows: host bounds on the new tokens and on the rows of a sequence (they size the grid).  Of

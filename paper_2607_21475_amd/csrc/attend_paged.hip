@@ -122,6 +122,29 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   // what a row got from values that are not finite, a byte per element (1: +inf, 2: -inf, 3: NaN)
   uint8_t *poison = my + kPoison;
   bool poisoned = false;
+  auto start_notes = [&]() {
+    if (!poisoned) {
+#pragma unroll 1
+      for (int i = lane; i < kRows * kHeadDim / 4; i += 64) reinterpret_cast<uint32_t *>(poison)[i] = 0u;
+      poisoned = true;
+    }
+    wave_sync();
+  };
+  // dims 2 lane .. 2 lane + 1 of a key's value: the rows that see it note what they get; whether any lane noted
+  auto note = [&](int key, uint32_t v) {
+    const uint32_t v0 = v << 16, v1 = v & 0xffff0000u;
+    if (!__any(not_finite(v0) | not_finite(v1))) return false;
+    const uint32_t what = poison_of(v0) | poison_of(v1) << 8;
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+#pragma unroll 1
+      for (int j = 0; j < 16; ++j) {
+        const bool sees = (key >= __shfl(span[b].lo, j)) & (key < __shfl(span[b].hi, j));
+        if (sees) reinterpret_cast<uint16_t *>(poison)[(16 * b + j) * 64 + lane] |= (uint16_t)what;
+      }
+    }
+    return true;
+  };
 
   const float sc2 = L.scale * kLog2e;
   const int stride = kRowsWaves * kTileKeys;
@@ -190,29 +213,12 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
         for (int e = 0; e < 4; ++e) top |= not_finite(v[e]) | not_finite(v[e] << 16);
       }
       if (__any(top)) {
-        if (!poisoned) {
+        start_notes();
 #pragma unroll 1
-          for (int i = lane; i < kRows * kHeadDim / 4; i += 64) reinterpret_cast<uint32_t *>(poison)[i] = 0u;
-          poisoned = true;
-        }
-        wave_sync();
-#pragma unroll 1
-        for (int r = 0; r < kTileKeys; ++r) {
-          // dims 2 x .. 2 x + 1 of key r: the rows that see it note what they get, and it counts as zero
-          const int x = lane, key = k + r;
-          uint32_t *at = reinterpret_cast<uint32_t *>(Vt + r * kRowBytes + (((x >> 2) ^ (r & 15)) * 16) + 4 * (x & 3));
-          const uint32_t v = *at, v0 = v << 16, v1 = v & 0xffff0000u;
-          if (!__any(not_finite(v0) | not_finite(v1))) continue;
-          const uint32_t note = poison_of(v0) | poison_of(v1) << 8;
-#pragma unroll
-          for (int b = 0; b < NQ; ++b) {
-#pragma unroll 1
-            for (int j = 0; j < 16; ++j) {
-              const bool sees = (key >= __shfl(span[b].lo, j)) & (key < __shfl(span[b].hi, j));
-              if (sees & !((bad >> (r / 16)) & 1u)) reinterpret_cast<uint16_t *>(poison)[(16 * b + j) * 64 + x] |= (uint16_t)note;
-            }
-          }
-          *at = (not_finite(v0) ? 0u : v0 >> 16) | (not_finite(v1) ? 0u : v1);
+        for (int r = 0; r < kTileKeys; ++r) {  // (rows of bad pages are zeros here)
+          uint32_t *at = reinterpret_cast<uint32_t *>(Vt + r * kRowBytes + (((lane >> 2) ^ (r & 15)) * 16) + 4 * (lane & 3));
+          const uint32_t v = *at;
+          if (note(k + r, v)) *at = (not_finite(v << 16) ? 0u : v & 0xffffu) | (not_finite(v) ? 0u : v & 0xffff0000u);
         }
         wave_sync();
       }
@@ -279,14 +285,44 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     bad = next_bad;
   }
   if (bad_any && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  // Where every row sees all keys of a tile, values enter the products as they are.  A NaN stays one, but an infinity's
+  // products with a weight's head and tail differ in sign, or are infinity times zero: the sum is NaN where it should be
+  // infinite.  So if a sum is NaN over weights that are not, the wave looks through its values once more, and notes what
+  // its rows got of them.
+  bool nan = false;
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    z[b] = add_xor32(add_xor16(z[b]));
+    f32x4 all = O[b][0];
+#pragma unroll
+    for (int d = 1; d < 8; ++d) all += O[b][d];
+    const float sum = (all[0] + all[1]) + (all[2] + all[3]);
+    nan |= (sum != sum) & (z[b] == z[b]);
+  }
+  if (__any(nan)) {
+    start_notes();
+#pragma unroll 1
+    for (int k0 = k_beg + wave * kTileKeys; k0 < k_end; k0 += stride) {
+#pragma unroll 1
+      for (int key = k0; key < min(k0 + kTileKeys, k_end); ++key) {
+        const int64_t at = page_row(p.pages, L.shift, s, key);
+        if (at >= 0) note(key, reinterpret_cast<const uint32_t *>(L.V + at + head)[lane]);
+      }
+    }
+    wave_sync();
+  }
+  // (a NaN weight makes the row's total NaN, and with it what is noted)
   if (poisoned) {
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
-        const uint32_t note = *reinterpret_cast<const uint32_t *>(poison + (16 * b + c) * kHeadDim + 16 * d + 4 * g);
+        const uint32_t got = *reinterpret_cast<const uint32_t *>(poison + (16 * b + c) * kHeadDim + 16 * d + 4 * g);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) O[b][d][i] += poison_value((note >> (8 * i)) & 3u);
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = (got >> (8 * i)) & 3u;
+          if (x) O[b][d][i] = poison_value(x);
+        }
       }
     }
   }
@@ -297,7 +333,6 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   float2 *mz = reinterpret_cast<float2 *>(Ow + kRows * kMergeRow);  // [kRows]
 #pragma unroll
   for (int b = 0; b < NQ; ++b) {
-    z[b] = add_xor32(add_xor16(z[b]));
     if (g == 0) mz[16 * b + c] = span[b].lo < span[b].hi ? make_float2(m[b], z[b]) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
     for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4 *>(Ow + (16 * b + c) * kMergeRow + 16 * d + 4 * g) = O[b][d];

@@ -97,6 +97,20 @@ def test_keys_that_hold_nan_give_nan_to_all_that_see_them(news, G, n):
         c.K.copy_(K0)
 
 
+@pytest.mark.parametrize("news,G,n", SHAPES)
+def test_infinite_values_that_all_see(news, G, n):
+    """An infinity times a positive weight is that infinity; of both signs, NaN."""
+    m = news[0]
+    kv = 8 if n == 9001 else 1
+    print("infinite values", m, G, n, flush=True)
+    c = ref.Cache([n], kv, 16, _gen(n + m))
+    for r, e, x in ((0, 1, INF), (n // 3, 2, -INF), (0, 9, INF), (n // 5 + 1, 9, -INF)):
+        c.V[int(c.table[0, r // 16]), 0, r % 16, e] = x
+    q, y, lse, _ = _attend(c, news, G)
+    want = _against(c, q, y, lse, m, n, "infinite values")
+    assert bool((want == INF).any()) and bool((want == -INF).any()) and bool(want.isnan().any())
+
+
 def _gather_params(c, off, max_rows):
     import paper_2607_21475_amd as ebd
 
