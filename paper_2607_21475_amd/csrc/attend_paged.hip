@@ -66,6 +66,11 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   Span span[NQ];
 #pragma unroll
   for (int b = 0; b < NQ; ++b) span[b] = span_of(L, sq, row0 + 16 * b + c);
+  if (sq.held > sq.seen && L.status && sp == 0 && wave == 0) {
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+      if (__any(past_table(L, sq, row0 + 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  }
   const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, token(row0), token(row0 + nrow - 1));
   const Keys split = split_of(L, R.lo, R.hi, kTileKeys, sp);
   const int k_beg = split.beg, k_end = split.end;  // (below 2^30: no sum below overflows)
@@ -95,7 +100,6 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     if (k >= k_end) return 0;  // past the range: never loaded, or masked
     return table[k >> L.shift];
   };
-  uint32_t bad_any = 0;
   auto issue = [&](int k, int pg0, int pg1, int stage) -> uint32_t {
     uint32_t bad = 0;
 #pragma unroll
@@ -118,6 +122,8 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     }
     return bad;
   };
+
+  bool gone = false;  // whether a row sees one on a bad page
 
   // what a row got from values that are not finite, a byte per element (1: +inf, 2: -inf, 3: NaN)
   uint8_t *poison = my + kPoison;
@@ -281,10 +287,16 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
         o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, hi[b], o, 0, 0, 0);
       }
     }
-    bad_any |= bad;
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < 2 * NQ; ++i) {
+        const int at = k + 16 * (i / NQ);
+        if ((bad >> (i / NQ)) & 1u) gone |= __any((span[i % NQ].lo < at + 16) & (span[i % NQ].hi > at));
+      }
+    }
     bad = next_bad;
   }
-  if (bad_any && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  if (gone && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   // Where every row sees all keys of a tile, values enter the products as they are.  A NaN stays one, but an infinity's
   // products with a weight's head and tail differ in sign, or are infinity times zero: the sum is NaN where it should be
   // infinite.  So if a sum is NaN over weights that are not, the wave looks through its values once more, and notes what

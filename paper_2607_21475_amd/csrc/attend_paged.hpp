@@ -55,7 +55,8 @@ struct Seq {
   int tokens;       // new tokens that get an output
   int64_t first;    // row of its first new token
   int64_t len;      // rows it holds
-  int64_t seen;     // ... of which the launch can see
+  int64_t held;     // ... of which the host's bound lets the launch see
+  int64_t seen;     // ... and the page table holds
   uint32_t status;
 };
 // New tokens of a sequence that get an output: tokens t0 .. t1 - 1, as far as the bounds allow.
@@ -71,12 +72,8 @@ __device__ __forceinline__ Seq sequence(const ebd_attend_paged_params &p, int s)
   q.len = ((const const_i32 *)p.len)[s];
   q.first = q.len - n;
   q.status = (n > p.max_new || q.len > p.max_rows) ? EBD_ST_BAD_LAYOUT : 0u;
-  q.seen = min(q.len, p.max_rows);
-  const int64_t room = (int64_t)p.pages.max_pages * p.pages.page_size;
-  if (q.seen > room) {
-    q.status |= EBD_ST_BAD_PAGE;
-    q.seen = room;
-  }
+  q.held = min(q.len, p.max_rows);
+  q.seen = min(q.held, (int64_t)p.pages.max_pages * p.pages.page_size);
   q.tokens = tokens_of(p, q.t0, t1);
   return q;
 }
@@ -151,6 +148,17 @@ __device__ __forceinline__ Span span_of(const AttendPagedLaunch &L, const Seq &q
   const int64_t lo = p.window > 0 ? max((int64_t)0, last - p.window + 1) : 0;
   const int64_t hi = min(last + 1, q.seen);
   return lo < hi ? Span{(int)lo, (int)hi} : Span{0, 0};
+}
+
+// Whether query row `row` would see rows behind the page table's end.
+__device__ __forceinline__ bool past_table(const AttendPagedLaunch &L, const Seq &q, int row) {
+  const ebd_attend_paged_params &p = L.p;
+  const int j = L.by_group.quotient(row);
+  if (j >= q.tokens) return false;
+  int64_t last = q.first + j;
+  if (p.qpos) last = min((int64_t)p.qpos[q.t0 + j], q.len - 1);
+  const int64_t lo = p.window > 0 ? last - p.window + 1 : 0;
+  return min(last + 1, q.held) > max(lo, q.seen);
 }
 
 // The range a block of query rows sees (the same in every lane of a wave that holds them all), and

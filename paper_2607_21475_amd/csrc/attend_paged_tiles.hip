@@ -122,6 +122,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const int row = row0 + 32 * rw + c;
   Span span[1] = {span_of(L, sq, row)};
   const bool sees = span[0].lo < span[0].hi;
+  if (sq.held > sq.seen && __any(past_table(L, sq, row)) && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   Range R, all;
   if (!p.qpos) {
     R = range_of_tokens(p, sq, token(row0 + 32 * rw), token(row0 + 32 * rw + 31));
@@ -354,7 +355,16 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     }
     barrier();
     any_bad = __any(lane < kWaves && bad_pages[lane & (kWaves - 1)]);
-    if (any_bad && threadIdx.x == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+    if (any_bad && L.status) {  // whether one of this wave's rows sees such a page
+      bool gone = false;
+#pragma unroll 1
+      for (int e = max(k_beg, R.lo) >> L.shift; (e << L.shift) < min(k_end, R.hi); ++e) {
+        const int at = e << L.shift;
+        if ((uint32_t)table[e] >= (uint32_t)p.pages.num_pages)
+          gone |= __any((max(span[0].lo, k_beg) < at + p.pages.page_size) & (own_hi > at));
+      }
+      if (gone && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+    }
     int st = 0;
     for (int first = k_beg; first < k_end; first += step, k += step, st ^= 1) {
       wait_loads<0>();

@@ -111,6 +111,31 @@ def test_infinite_values_that_all_see(news, G, n):
     assert bool((want == INF).any()) and bool((want == -INF).any()) and bool(want.isnan().any())
 
 
+@pytest.mark.parametrize("news", [[2], [12], [30], [90]])
+def test_rows_that_no_token_sees_raise_no_flag(news):
+    """Windows apart from each other: the pages between them, and rows past the table, are seen by no token."""
+    c = ref.Cache([700], 2, 16, _gen(8), fill=math.nan)
+    m, window = news[0], 16
+    hi = torch.full((m,), 30, dtype=torch.int32, device="cuda")
+    hi[m // 2:] = 600
+    keep = torch.zeros(c.table.shape[1], dtype=torch.bool, device="cuda")
+    keep[0:2] = keep[36:38] = True
+    held = ref.Cache([700], 2, 16, _gen(8), fill=math.nan)
+    c.table[0, ~keep] = -1
+    c.len[0] = 16 * c.table.shape[1] + 40
+    q, y, lse, st = _attend(c, news, 4, hi=hi, window=window, max_rows=4000)
+    held.K, held.V = c.K, c.V
+    ry, rl, ty, tl = ref.attend(held, q, news, hi=hi, window=window, weights_bits=8)
+    ref.check(y, ry, ty, "y")
+    ref.check(lse, rl, tl, "lse")
+    assert st.tolist() == [0]
+    # one token that sees such a row is enough
+    import paper_2607_21475_amd as ebd
+    for at in (40, 592 + 16, 16 * c.table.shape[1] + 30):
+        hi[m - 1] = at
+        assert _attend(c, news, 4, hi=hi, window=window, max_rows=4000)[3].tolist() == [ebd.EBD_ST_BAD_PAGE], at
+
+
 def _gather_params(c, off, max_rows):
     import paper_2607_21475_amd as ebd
 
