@@ -464,17 +464,19 @@ class PagedCache:
         return pages(self.K, self.V, self.page_table)
 
     def append(self, k_new, v_new, new_off, rot: Optional[ebd_rotary] = None, pos=None, q=None, status=None):
-        """Append tokens (self.len counts them already); returns the rotated queries, or None without q."""
-        q_out = None if q is None else torch.empty(q.shape, dtype=_BF, device=q.device)
+        """Append tokens (self.len counts them already); returns the rotated queries (zeros for padding tokens), or None
+        without q."""
+        q_out = None if q is None else torch.zeros(q.shape, dtype=_BF, device=q.device)
         p = append_paged_params(self.pages, k_new, v_new, new_off, self.len, rot, pos=pos, q=q, q_out=q_out)
         ebd_append_paged(p, k_new, v_new, self.K, self.V, q, q_out, status=status)
         return q_out
 
     def attend(self, q, new_off, max_new: int, max_rows: int, qpos=None, window: int = 0, scale: float = 0.0,
                ws: Optional[torch.Tensor] = None, status=None):
-        """Attention of the new tokens: {"y" [tokens, heads, 128] bf16, "lse" [tokens, heads] fp32, "ws"}."""
-        y = torch.empty(q.shape, dtype=_BF, device=q.device)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        """Attention of the new tokens: {"y" [tokens, heads, 128] bf16, "lse" [tokens, heads] fp32, "ws"}; zeros and -inf
+        for padding tokens and those past max_new."""
+        y = torch.zeros(q.shape, dtype=_BF, device=q.device)
+        lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device)
         p = attend_paged_params(self.pages, q, y, new_off, self.len, max_new, max_rows, qpos=qpos, window=window,
                                 scale=scale)
         need = ebd_workspace_size(EBD_WS_ATTEND_PAGED, p)

@@ -188,3 +188,35 @@ def test_gather_refuses_outputs_of_other_shapes():
         Ku, Vu = (torch.full((rows, 128), 7.0, dtype=BF, device="cuda") for _ in range(2))
         ebd.ebd_gather_paged(p, c.K, c.V, Ku, Vu)
         assert torch.equal(Ku[:40], torch.cat([c.rows(c.K, 0, h) for h in range(2)])) and bool((Ku[40:] == 7).all())
+
+
+def test_helpers_give_padding_tokens_zeros():
+    """Outputs that the helpers allocate hold nothing of what that memory held before."""
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(3)
+    new, kv, G, T = [5, 0, 3], 2, 3, 14
+    c = ebd.PagedCache.allocate([40, 8, 40], kv, page_size=16)
+    c.K.normal_(generator=g), c.V.normal_(generator=g)
+    c.len += torch.tensor([30, 0, 12], dtype=torch.int32, device="cuda")
+    off = torch.tensor([2, 7, 7, 10], device="cuda")  # two tokens before the sequences and four behind
+    k, v, q = (ref.spaced((T, h, 128), g, False) for h in (kv, kv, kv * G))
+    freq, _ = ebd.rope_frequencies(128)
+    pad = torch.ones(T, dtype=torch.bool, device="cuda")
+    pad[2:10] = False
+
+    def dirty():
+        x = [torch.full(s, math.nan, dtype=t, device="cuda") for s, t in (((T, kv * G, 128), BF), ((T, kv * G), torch.float32))]
+        del x
+
+    dirty()
+    qr = c.append(k, v, off, ebd.rotary(freq), q=q)
+    assert not bool(qr[pad].any()) and bool(qr[~pad].any(-1).all())
+    dirty()
+    out = c.attend(qr, off, 5, 30)
+    assert not bool(out["y"][pad].any()) and bool((out["lse"][pad] == -INF).all())
+    assert bool(torch.isfinite(out["lse"][~pad]).all())
+    dirty()
+    short = c.attend(qr, off, 3, 30)  # new tokens past max_new get no output
+    assert not bool(short["y"][5:7].any()) and bool((short["lse"][5:7] == -INF).all())
+    assert torch.equal(short["lse"][7:10], out["lse"][7:10])
