@@ -14,7 +14,7 @@ using namespace ebd;
 
 constexpr int64_t kStrideMax = (int64_t)1 << 40;
 constexpr int64_t kRowStrideMax = (int64_t)1 << 26;  // a lane's offset inside 16 rows stays below 32 bits
-constexpr int64_t kGridMax = ((int64_t)1 << 24) - 1;  // work-groups of 256 threads in a launch
+constexpr int64_t kGridMax = ((int64_t)1 << 24) - 1;  // tokens of a call, query rows of a sequence; groups of 256 threads
 constexpr int64_t kRowsMax = (int64_t)1 << 30;         // rows of a sequence
 constexpr int32_t kHeadsMax = 65536;
 

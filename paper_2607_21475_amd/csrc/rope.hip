@@ -104,7 +104,10 @@ __device__ __forceinline__ void store16(uint16_t *p, const uint4 &v) { *reinterp
 
 }  // namespace
 
-// Work-group (token group, block of rows): `per` threads, whole waves, for each of up to four tokens.
+// Work-group (token group, block of rows): `per` threads, whole waves, for each of up to four tokens.  A dimension of the
+// grid holds fewer than 2^32 threads, which 2^24 tokens of up to 1024 pass, so token groups fill x and go on in z.
+constexpr int kAcross = 1 << 21;
+__device__ __forceinline__ int64_t token_group(int x, int z) { return (int64_t)z * kAcross + x; }
 __device__ __forceinline__ int token_slot(int per) {
   const int t = threadIdx.x;
   return (t >= per) + (t >= 2 * per) + (t >= 3 * per);
@@ -114,7 +117,7 @@ __global__ __launch_bounds__(8 * kRopeRows) void rope_kernel(RopeLaunch L) {
   __shared__ float2 cs[4][kHeadDim / 2];
   const ebd_rope_params &p = L.p;
   const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per;
-  const int64_t t = (int64_t)blockIdx.x * L.tpb + slot;
+  const int64_t t = token_group(blockIdx.x, blockIdx.z) * L.tpb + slot;
   const int h = blockIdx.y * kRopeRows + i / 8;
   const bool live = t < p.num_tokens && h < p.num_heads;
   const Split sp = split_row(p.rot, i % 8, true);
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(8 * kRopeRows) void append_paged_kernel(AppendPaged
   __shared__ float2 cs[4][kHeadDim / 2];
   const ebd_append_paged_params &p = L.p;
   const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per;
-  const int64_t t = (int64_t)blockIdx.x * L.tpb + slot;
+  const int64_t t = token_group(blockIdx.x, blockIdx.z) * L.tpb + slot;
   const int row = blockIdx.y * kRopeRows + i / 8;
   const int kv = p.pages.kv_heads, S = p.pages.num_seqs;
   const bool isk = row < kv, isq = !isk && row < kv + p.q_heads;
@@ -186,7 +189,9 @@ void cut(int64_t rows, int32_t *per, int32_t *tpb) {
   *tpb = std::max(1, std::min(4, 256 / *per));
 }
 dim3 rope_grid(int64_t tokens, int64_t rows, int tpb) {
-  return dim3((unsigned)((tokens + tpb - 1) / tpb), (unsigned)((rows + kRopeRows - 1) / kRopeRows));
+  const int64_t groups = (tokens + tpb - 1) / tpb;
+  return dim3((unsigned)std::min<int64_t>(groups, kAcross), (unsigned)((rows + kRopeRows - 1) / kRopeRows),
+              (unsigned)((groups + kAcross - 1) / kAcross));
 }
 }  // namespace
 

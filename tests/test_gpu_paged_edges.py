@@ -220,3 +220,24 @@ def test_helpers_give_padding_tokens_zeros():
     short = c.attend(qr, off, 3, 30)  # new tokens past max_new get no output
     assert not bool(short["y"][5:7].any()) and bool((short["lse"][5:7] == -INF).all())
     assert torch.equal(short["lse"][7:10], out["lse"][7:10])
+
+
+def test_append_of_the_most_tokens():
+    """2^24 - 1 tokens of 128 rows, 2^34 threads; the tokens before the last three are padding, which reads one token."""
+    import paper_2607_21475_amd as ebd
+
+    T, kv = (1 << 24) - 1, 64
+    g = _gen(2)
+    c = ref.Cache([20], kv, 16, g)
+    k, v = (ref.spaced((1, kv, 128), g, False).expand(T, kv, 128) for _ in range(2))
+    K0, V0 = c.K.clone(), c.V.clone()
+    for n in (3, 0):
+        off = torch.tensor([T - n, T], device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        ebd.ebd_append_paged(ebd.append_paged_params(ebd.pages(c.K, c.V, c.table), k, v, off, c.len), k, v, c.K, c.V, status=st)
+        torch.cuda.synchronize()
+        print("appended", n, flush=True)
+        for r in range(17, 20) if n else ():
+            for x, new in ((K0, k), (V0, v)):
+                x[int(c.table[0, r // 16]), :, r % 16] = new[0]
+        assert torch.equal(c.K, K0) and torch.equal(c.V, V0) and not bool(st.any())
