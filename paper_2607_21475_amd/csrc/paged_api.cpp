@@ -102,18 +102,24 @@ int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_
   return best;
 }
 
-// A launch for blocks of `rows` query rows; `sum` query rows in all, the sequences' most `rows_max` each.
-AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t rows, int64_t rows_max, int64_t sum) {
+// A launch for blocks of `rows` query rows; `sum` query rows in all, the sequences' most `rows_max` each, and each of those
+// that it takes more than `more_than`.
+AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t rows, int64_t rows_max, int64_t sum,
+                                    int64_t more_than = 0) {
   AttendPagedLaunch L{};
   L.p = *p;
   L.rows = rows;
+  L.more_than = more_than;
   L.at_most = INT64_MAX;
   const bool tiles = rows >= kTileRows;
   const int64_t S = p->pages.num_seqs, H = p->pages.kv_heads;
-  // Every sequence has at most a block that is not full; blocks set aside for the longest sequence cost an
-  // empty work-group each where there are none (64 sequences, one of 2048 tokens: 32768 of them, about 130 us).
-  const int64_t aside = std::max<int64_t>(1, (rows_max + rows - 1) / rows), counted = sum / rows + S;
-  L.blocks = S * aside > counted + counted / 2 ? 0 : (int32_t)aside;
+  // Every sequence that the launch takes has at most a block that is not full, and some new tokens: a thousand without
+  // any, beside a chunk of 64 tokens over 10000 rows, are no blocks (17 with the chunk's: 0.3 GB of partial sums;
+  // were they, 17 GB).  Blocks set aside for the longest sequence cost an empty work-group each where there are none (64
+  // sequences, one of 2048 tokens: 32768 of them, about 130 us).
+  const int64_t aside = std::max<int64_t>(1, (rows_max + rows - 1) / rows);
+  const int64_t counted = sum / rows + std::min<int64_t>(S, sum / std::max<int64_t>(p->group, more_than + 1));
+  L.blocks = aside > 1 && S * aside > counted + counted / 2 ? 0 : (int32_t)aside;
   L.units = L.blocks ? S * aside : counted;
   // the most rows a block of query rows sees, under a window from a tile's border on
   int64_t span = p->max_rows;
@@ -172,8 +178,7 @@ AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
     plan.parts = 2;
     plan.part[1] = attend_paged_part(p, small, small, S * small);
     plan.part[1].at_most = small;
-    plan.part[0] = attend_paged_part(p, rows, most, sum);
-    plan.part[0].more_than = small;
+    plan.part[0] = attend_paged_part(p, rows, most, sum, small);
   } else if (long_blocks(p, most)) {
     plan.part[0] = attend_paged_part(p, kLongRows, most, sum);
   } else {

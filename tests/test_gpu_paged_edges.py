@@ -241,3 +241,18 @@ def test_append_of_the_most_tokens():
             for x, new in ((K0, k), (V0, v)):
                 x[int(c.table[0, r // 16]), :, r % 16] = new[0]
         assert torch.equal(c.K, K0) and torch.equal(c.V, V0) and not bool(st.any())
+
+
+@pytest.mark.parametrize("news", [[130] + [17] * 12 + [16] * 5 + [0] * 230, [0] * 70 + [129, 0, 17, 16, 33] + [0] * 40 + [17, 140],
+                                  [300] + [0] * 90])
+def test_attend_chunks_among_sequences_without_new_tokens(news):
+    """As many blocks of query rows as their tokens may make, and none for the sequences that have none."""
+    print("attend idle", len(news), sum(news), flush=True)
+    lens = [n + 40 + 13 * (i % 7) for i, n in enumerate(news)]
+    c = ref.Cache(lens, 1, 16, _gen(5), fill=math.nan)
+    for G in (1, 5):
+        q, y, lse, st = _attend(c, news, G)
+        assert not bool(st.any())
+        ry, rl, ty, tl = ref.attend(c, q, news, weights_bits=8)
+        ref.check(y, ry, ty, "y")
+        ref.check(lse, rl, tl, "lse")

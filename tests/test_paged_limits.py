@@ -23,3 +23,26 @@ def test_gather_needs_a_row_count_that_is_none_below_zero():
     p = paged.ebd_gather_paged_params()
     p.pages, p.max_rows, p.seq_off, p.num_rows = _pages(), 100, FAKE, -1
     assert LIB.ebd_gather_paged(ctypes.byref(p), FAKE, FAKE, FAKE, FAKE, None, None) == BAD
+
+
+def _attend_params(seqs, **kw):
+    p = paged.ebd_attend_paged_params()
+    p.pages = _pages(num_seqs=seqs, kv_heads=8, page_stride=8 * 16 * 128)
+    p.group, p.max_new, p.num_tokens, p.max_rows, p.new_off, p.len = 4, 64, 64, 600, FAKE, FAKE
+    p.q_rows = p.y_rows = paged.ebd_rows(32 * 128, 128)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def test_sequences_without_new_tokens_need_no_workspace():
+    """One chunk of 256 query rows among many idle sequences: partial sums (a block's 128 query rows take 520 bytes each) for
+    its own splits, at most 32 for each of the 17 blocks that 256 rows may lie in, and 8 heads."""
+    size = lambda seqs, **kw: ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, _attend_params(seqs, **kw))  # noqa: E731
+    most = 512 + 17 * 32 * 8 * 128 * 520
+    for rows in (600, 10000):
+        n = size(64, max_rows=rows)
+        assert n <= most and all(size(seqs, max_rows=rows) == n for seqs in (256, 1000, 70000)), rows
+    assert size(64, max_rows=10000) > most // 2
+    wide = dict(group=40, max_new=8, num_tokens=8)  # more query heads than the launch of short sequences serves
+    assert size(64, max_rows=1 << 20, **wide) == size(10000, max_rows=1 << 20, **wide) <= 512 + (320 // 128 + 8) * 32 * 8 * 128 * 520
