@@ -400,7 +400,7 @@ ebd_status ebd_rope(const ebd_rope_params *p, const uint16_t *x, uint16_t *y, vo
  *   strides     positive multiples of 8; row_stride below 2^26, the others below 2^40.
  * Limits of the calls on it (beyond them, and for other page sizes, EBD_ERR_UNSUPPORTED): fewer than 2^24 new
  * tokens, fewer than 2^24 query rows (tokens times the query heads of a KV head) of a sequence, 65536 heads, max_rows up
- * to 2^30, and launches of fewer than 2^23 work-groups.
+ * to 2^30, and launches of fewer than 2^23 work-groups (2^24 of the gather's and of those that join splits).
  */
 typedef struct ebd_pages {
     int32_t num_seqs;

@@ -457,6 +457,10 @@ int64_t attend_paged_groups(const AttendPagedLaunch &L) {
   return L.units * L.p.pages.kv_heads * L.nsplit;
 }
 
+int64_t attend_paged_join_groups(const AttendPagedLaunch &L) {
+  return L.nsplit > 1 ? L.units * L.p.pages.kv_heads * (L.rows / 4) : 0;
+}
+
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
   if (L.rows > kRowsKernelMax) return launch_attend_tiles(L, s);
   const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
@@ -468,8 +472,7 @@ hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
 }
 
 hipError_t launch_attend_paged_join(const AttendPagedLaunch &L, hipStream_t s) {
-  const int64_t groups = attend_paged_groups(L) / L.nsplit * (L.rows / 4);
-  hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)groups), dim3(256), 0, s, L);
+  hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)attend_paged_join_groups(L)), dim3(256), 0, s, L);
   return hipGetLastError();
 }
 

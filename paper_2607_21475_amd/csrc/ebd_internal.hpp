@@ -257,6 +257,7 @@ hipError_t launch_append_paged(AppendPagedLaunch L, hipStream_t s);
 int64_t gather_paged_groups(const ebd_gather_paged_params &p);
 hipError_t launch_gather_paged(GatherPagedLaunch L, hipStream_t s);
 int64_t attend_paged_groups(const AttendPagedLaunch &L);
+int64_t attend_paged_join_groups(const AttendPagedLaunch &L);  // 0: no join
 size_t attend_paged_part_bytes(const AttendPagedLaunch &L);
 size_t attend_paged_workspace(const ebd_attend_paged_params *p);  // 0: invalid parameters
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s);

@@ -267,7 +267,8 @@ ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q,
     return EBD_ERR_INVALID_ARG;
   AttendPagedPlan plan = attend_paged_plan(p);
   for (int i = 0; i < plan.parts; ++i)
-    if (attend_paged_groups(plan.part[i]) > kGridMax / 2) return EBD_ERR_UNSUPPORTED;
+    if (attend_paged_groups(plan.part[i]) > kGridMax / 2 || attend_paged_join_groups(plan.part[i]) > kGridMax)
+      return EBD_ERR_UNSUPPORTED;
   if (!workspace || ws_bytes < plan_bytes(plan) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
   const ebd_status ds = device_ok();
   if (ds != EBD_OK) return ds;

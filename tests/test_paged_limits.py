@@ -46,3 +46,16 @@ def test_sequences_without_new_tokens_need_no_workspace():
     assert size(64, max_rows=10000) > most // 2
     wide = dict(group=40, max_new=8, num_tokens=8)  # more query heads than the launch of short sequences serves
     assert size(64, max_rows=1 << 20, **wide) == size(10000, max_rows=1 << 20, **wide) <= 512 + (320 // 128 + 8) * 32 * 8 * 128 * 520
+
+
+def test_attend_refuses_launches_of_too_many_work_groups():
+    def call(seqs, **kw):
+        return LIB.ebd_attend_paged(ctypes.byref(_attend_params(seqs, **kw)), FAKE, FAKE, FAKE, FAKE, None, None, FAKE, 0, None)
+
+    assert call(1000) == ebd.EBD_ERR_WORKSPACE  # the launches are in bounds, the workspace is not
+    assert call((1 << 20) + 1, max_new=1) == UNSUPPORTED
+    # five tokens of each sequence, over so many rows that a block's are split: the splits' launch is in bounds, the one
+    # that joins them, a work-group for four query rows of every block, is not
+    assert call(80000, num_tokens=400000, max_rows=1 << 22) == UNSUPPORTED
+    assert call(50000, num_tokens=250000, max_rows=1 << 22) == ebd.EBD_ERR_WORKSPACE  # (57812 blocks of 8 heads: 14.8 million)
+    assert call(80000, num_tokens=400000, max_rows=1 << 12) == ebd.EBD_ERR_WORKSPACE
