@@ -175,7 +175,7 @@ def _distinct(t, name):
     for stride, n in sorted((s, n) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1):
         if t.numel() and stride < span:
             raise ValueError("the rows of %s must not share memory" % name)
-        span = max(span, stride * n)
+        span += stride * (n - 1)
 
 
 def _plan(p, device, keep, **tensors):

@@ -256,3 +256,25 @@ def test_attend_chunks_among_sequences_without_new_tokens(news):
         ry, rl, ty, tl = ref.attend(c, q, news, weights_bits=8)
         ref.check(y, ry, ty, "y")
         ref.check(lse, rl, tl, "lse")
+
+
+def test_outputs_of_every_second_head():
+    """Rotated rows and results written to heads 0 and 2 of three: the heads between them stay as they were."""
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(4)
+    c = ref.Cache([40], 2, 16, g)
+    x = ref.spaced((5, 2, 128), g, False)
+    freq, _ = ebd.rope_frequencies(128)
+    pos = torch.arange(5, device="cuda", dtype=torch.int32)
+    off = torch.tensor([0, 5], device="cuda")
+    whole = torch.full((2, 5, 3, 128), 7.0, dtype=BF, device="cuda")
+    r, y = whole[0, :, ::2], whole[1, :, ::2]
+    ebd.ebd_rope(ebd.rope_params(x, r, pos, ebd.rotary(freq)), x, r)
+    p = ebd.attend_paged_params(ebd.pages(c.K, c.V, c.table), r, y, off, c.len, 5, 40)
+    ebd.ebd_attend_paged(p, r, c.K, c.V, y, ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, p)))
+    want = ref.rotate(x, pos, freq)
+    ref.check(r, want, ref.rotate_tolerance(x, want, freq), "rotated")
+    ry, _, ty, _ = ref.attend(c, r, [5], weights_bits=8)
+    ref.check(y, ry, ty, "y")
+    assert bool((whole[:, :, 1] == 7).all())

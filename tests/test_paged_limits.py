@@ -1,6 +1,9 @@
 """CPU checks of the paged-cache entry points' limits and of the layouts that the binding takes."""
 import ctypes
 
+import pytest
+import torch
+
 import paper_2607_21475_amd as ebd
 from paper_2607_21475_amd import paged
 
@@ -59,3 +62,19 @@ def test_attend_refuses_launches_of_too_many_work_groups():
     assert call(80000, num_tokens=400000, max_rows=1 << 22) == UNSUPPORTED
     assert call(50000, num_tokens=250000, max_rows=1 << 22) == ebd.EBD_ERR_WORKSPACE  # (57812 blocks of 8 heads: 14.8 million)
     assert call(80000, num_tokens=400000, max_rows=1 << 12) == ebd.EBD_ERR_WORKSPACE
+
+
+def test_outputs_whose_rows_lie_apart_are_taken():
+    """Every second head of an odd number, heads or tokens outermost, gaps of any size: no two rows share an element."""
+    x = torch.zeros(40000, dtype=torch.bfloat16)
+    for t in (x[:1920].view(5, 3, 128)[:, ::2], x[:1920].view(3, 5, 128)[::2].transpose(0, 1), x[:1920].view(5, 3, 128)[::3],
+              torch.as_strided(x, (4, 2, 128), (392, 264, 1)), torch.as_strided(x, (4, 2, 128), (0, 128, 1))[:1],
+              x[:3840].view(2, 5, 3, 128)[:, ::2, ::2], x[:0].view(0, 3, 128)):
+        seen = (torch.arange(40000)[:, None].new_zeros(40000)).index_add_(
+            0, torch.as_strided(torch.arange(40000), t.shape, t.stride()).reshape(-1), torch.ones(t.numel(), dtype=torch.long))
+        assert int(seen.max()) <= 1
+        paged._distinct(t, "t")
+    for shape, stride in (((4, 2, 128), (391, 264, 1)), ((4, 2, 128), (264, 136, 1)), ((2, 2, 128), (0, 128, 1)),
+                          ((3, 2, 128), (128, 128, 1)), ((2, 4, 2, 128), (1000, 264, 136, 1))):
+        with pytest.raises(ValueError, match="share memory"):
+            paged._distinct(torch.as_strided(x, shape, stride), "t")
