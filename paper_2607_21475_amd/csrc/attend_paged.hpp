@@ -22,7 +22,8 @@ __device__ __forceinline__ uint32_t lds_at(const void *p) {
 
 // 16 bytes per lane from base + off straight into LDS at `to` + 16 lane; NT: the non-temporal hint.  Written as
 // assembly because the compiler would wait for all of them before any read of LDS; it holds no result register, and
-// the waits below order it.
+// the waits below order it.  It writes m0, which cannot be named as clobbered (the register is reserved); nothing else in
+// these kernels uses it, which the build's tests look at.
 template <bool NT>
 __device__ __forceinline__ void load_lds16(uint32_t to, const uint8_t *base, uint32_t off) {
   if constexpr (NT)
