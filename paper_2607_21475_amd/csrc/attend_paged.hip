@@ -6,8 +6,8 @@
 //   m = max l,  w = 2^(l - m),  y = sum w v / sum w,  lse = m ln 2 + ln sum w
 // in one pass, m running (what was summed is scaled down when it grows).
 //
-// attend_rows (up to 32 query rows): one work-group per (sequence, KV head, block of 16 or 32 query rows, split of
-//   the rows they see), four waves that take its tiles of 32 keys in turn, each on its own.  A wave keeps the
+// attend_rows (up to 32 query rows of a sequence): one work-group per (sequence, KV head, split of the rows that its
+//   block of 16 or 32 query rows sees), four waves that take its tiles of 32 keys in turn, each on its own.  A wave keeps the
 //   next tile's keys and values on their way into its share of LDS (loads that write LDS directly, 16 bytes a
 //   lane) while it computes the present one; nothing in the loop waits for another wave.
 //   Scores are formed transposed, S^T = K Q^T (MFMA 16x16x32 bf16: exact products, fp32 sums): lane (g, c) then
@@ -52,26 +52,24 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   const int H = p.pages.kv_heads, G = p.group;
   auto token = [&](int row) { return L.by_group.quotient(row); };  // of a query row, in its sequence
   const int uh = L.by_nsplit.quotient(blockIdx.x), sp = blockIdx.x - uh * L.nsplit;
-  const int u = L.by_heads.quotient(uh), h = uh - u * H;
-  const Place at = place_of(L, u);
-  const int s = at.s, rb = at.rb;
+  const int s = L.by_heads.quotient(uh), h = uh - s * H;  // a block holds all query rows of a sequence
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   const Seq sq = sequence(p, s);
-  const int row0 = rb * kRows, nrow = min(kRows, sq.tokens * G - row0);
+  const int nrow = min(kRows, sq.tokens * G);
   if (nrow <= 0 || !takes(L, (int64_t)sq.tokens * G)) return;
-  if (threadIdx.x == 0 && rb == 0 && sp == 0 && h == 0 && L.status && sq.status) atomicOr(&L.status[s], sq.status);
+  if (threadIdx.x == 0 && sp == 0 && h == 0 && L.status && sq.status) atomicOr(&L.status[s], sq.status);
 
   Span span[NQ];
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) span[b] = span_of(L, sq, row0 + 16 * b + c);
+  for (int b = 0; b < NQ; ++b) span[b] = span_of(L, sq, 16 * b + c);
   if (sq.held > sq.seen && L.status && sp == 0 && wave == 0) {
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
-      if (__any(past_table(L, sq, row0 + 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+      if (__any(past_table(L, sq, 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   }
-  const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, token(row0), token(row0 + nrow - 1));
+  const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, 0, token(nrow - 1));
   const Keys split = split_of(L, R.lo, R.hi, kTileKeys, sp);
   const int k_beg = split.beg, k_end = split.end;  // (below 2^30: no sum below overflows)
 
@@ -164,7 +162,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   bf16x8 Q[NQ][4];  // B operand: column c of block b is query row 16 b + c
 #pragma unroll
   for (int b = 0; b < NQ; ++b) {
-    const int row = row0 + 16 * b + c;
+    const int row = 16 * b + c;
     const bool ok = span[b].lo < span[b].hi;
     const int j = ok ? token(row) : 0, hq = h * G + (ok ? row - j * G : 0);
     const uint16_t *q = L.q + (sq.t0 + j) * p.q_rows.token_stride + hq * p.q_rows.head_stride;
@@ -376,8 +374,8 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
       *reinterpret_cast<f32x4 *>(part) = f32x4{o[0], o[1], o[2], o[3]};
       *reinterpret_cast<f32x4 *>(part + 4) = f32x4{o[4], o[5], o[6], o[7]};
     } else {
-      const int j = token(row0 + r);
-      store_row(L, sq.t0 + j, h * G + row0 + r - j * G, e, M, Z, o);
+      const int j = token(r);
+      store_row(L, sq.t0 + j, h * G + r - j * G, e, M, Z, o);
     }
   }
 }
