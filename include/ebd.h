@@ -470,7 +470,9 @@ ebd_status ebd_append_paged(const ebd_append_paged_params *p, const uint16_t *k_
  *   scale: logit scale (0 means 1/sqrt(head_dim)).
  *   status [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when a row that some token sees has no page
  *   (it is not seen), EBD_ST_BAD_LAYOUT as above.
- *   Logits, softmax statistics and the sums over v are fp32.  workspace: at least
+ *   Logits, softmax statistics and the sums over v are fp32.  A weight enters the sums over v rounded to 16 bits in calls
+ *   of up to 64 query rows of a sequence (max_new times group), and to 8 (bf16) in others, which the matrix products
+ *   bound: there y may be off by 2^-8 of the weighted mean of |v|, beside its own rounding.  workspace: at least
  *   ebd_workspace_size(EBD_WS_ATTEND_PAGED, p) bytes, 256-byte aligned; nothing in it is kept from one
  *   call to the next.
  */

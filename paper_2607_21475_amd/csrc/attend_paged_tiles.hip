@@ -17,8 +17,10 @@
 //   64 query rows by eight waves, in four groups of two that take every fourth tile of 32 keys: 33 to 64 rows are
 //   too few to hide the memory with 128-row blocks, and too much work for attend_rows' one wave a SIMD (16 sequences
 //   of up to 6144 rows, 56 query rows: 38 us, attend_rows 58).
-//   The matrix products bound it: 4 x 128 operations per (query row, key), against which the weights' bf16
-//   rounding (half a step, 2^-8, averaged over a row's keys) saves a second product with their tails.  1024 tokens, 32
+//   The matrix products bound it: 4 x 128 operations per (query row, key).  So the weights of the first two shapes are
+//   rounded to bf16 (half a step, 2^-8, averaged over a row's keys); a second product with their tails, 16 bits in all,
+//   costs 20 to 40% (8192 tokens over 8192 rows 770 us with it, 566 without, 1024 over 131072 2930 / 2070, 1024 over 1024
+//   38.7 / 32.0).  The third shape is bound by memory and has it (the call above with its join 42.0 / 40.9).  1024 tokens, 32
 //   heads, over 131072 rows: 2.06 to 2.18 ms, 1.0 to 1.06 PFLOP/s; the matrix cores are busy 54% of the
 //   cycles, of which the power limit leaves about 2.0 to 2.1 GHz (a large product runs at 1.34 PFLOP/s there).
 #include "attend_paged.hpp"
@@ -31,18 +33,18 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLazy = 8.0f;
 
-// The order of N products and their READS of LDS each: the operands of four products on their way, no more, so
+// The order of N operands from LDS, READS reads each, and the PRODUCTS of each: four operands on their way, no more, so
 // that the registers suffice.
-template <int N, int READS>
+template <int N, int READS, int PRODUCTS = 1>
 __device__ __forceinline__ void feed() {
   constexpr int kRead = 0x100, kProduct = 0x008;
   __builtin_amdgcn_sched_group_barrier(kRead, 4 * READS, 0);
 #pragma unroll
   for (int i = 0; i < N - 4; ++i) {
-    __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kProduct, PRODUCTS, 0);
     __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(kProduct, 4, 0);
+  __builtin_amdgcn_sched_group_barrier(kProduct, 4 * PRODUCTS, 0);
 }
 
 __device__ __forceinline__ Range uniform(const Range &r) {
@@ -83,6 +85,7 @@ template <int RW, int KG, int KEYS, bool NT>
 __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
   constexpr int kWaves = RW * KG, kRows = 32 * RW;
   constexpr int kSub = KEYS / 32;             // blocks of 32 keys of a tile
+  constexpr bool kTails = KG > 1;             // weights as a bf16 head and a bf16 tail, not a head alone
   constexpr int kPart = KEYS / RW;            // rows of a tile that a wave loads
   constexpr int kTile = KEYS * kRowBytes;     // bytes of a tile's K, or of its V
   constexpr int kStage = KG * 2 * kTile;
@@ -193,6 +196,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   f32x16 S[kSub];
   bf16x8 Q[8];  // B operand: column c is this lane's query row, dims 16 kb + 8 half .. + 7
   bf16x8 W[2 * kSub];  // weights, the B operand of the sums
+  bf16x8 X[kTails ? 2 * kSub : 1];  // ... their tails
   bool any_bad = false;
 
   auto keys = [&](uint32_t Kt, int i) {
@@ -211,7 +215,11 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   };
   auto sums = [&](uint32_t Vt) {
 #pragma unroll
-    for (int i = 0; i < 8 * kSub; ++i) O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(Vt, i), W[i / 4], O[i % 4], 0, 0, 0);
+    for (int i = 0; i < 8 * kSub; ++i) {
+      const bf16x8 A = values(Vt, i);
+      if constexpr (kTails) O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, X[i / 4], O[i % 4], 0, 0, 0);
+      O[i % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, W[i / 4], O[i % 4], 0, 0, 0);
+    }
   };
   auto mixed = [&](int k, uint32_t bad) { return bad || k < R.every_lo || k + KEYS > min(R.every_hi, k_end); };
   auto softmax = [&](int k, uint32_t bad) {
@@ -253,6 +261,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
         const float w = fast_exp2(__builtin_fmaf(S[b][i], sc2, -mu));
         part_z[i % 4] += w;
         W[2 * b + i / 8][i % 8] = (__bf16)w;
+        if constexpr (kTails) X[2 * b + i / 8][i % 8] = (__bf16)(w - (float)W[2 * b + i / 8][i % 8]);
       }
     }
     z += (part_z[0] + part_z[1]) + (part_z[2] + part_z[3]);
@@ -297,23 +306,26 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     any = __any(any);
     if (lane == 0) noted[stage][kg][rw] = any;
   };
-  auto keep_notes = [&](int stage, int k, uint32_t bad) {
-    if (!partial(k, bad) || !__any(lane < RW && noted[stage][kg][lane & (RW - 1)])) return;
+  auto start_notes = [&]() {
     if (!poisoned) {
       for (int i = lane; i < 256; i += 64) poison[0][i] = 0u;
       poisoned = true;
     }
     wave_sync();
+  };
+  auto keep_note = [&](int key, uint32_t note) {  // 16 bits in each of the first 16 lanes
+    if (!__any(note)) return;
 #pragma unroll 1
-    for (int r = 0; r < KEYS; ++r) {
-      const uint32_t note = lane < 16 ? notes[stage][kg][r][lane] : 0u;
-      if (!__any(note)) continue;
-#pragma unroll 1
-      for (int j = 0; j < 32; ++j) {
-        const bool hit = (k + r >= __shfl(span[0].lo, j)) & (k + r < __shfl(own_hi, j));
-        if (hit && note) atomicOr(&poison[j][lane >> 1], note << (16 * (lane & 1)));
-      }
+    for (int j = 0; j < 32; ++j) {
+      const bool hit = (key >= __shfl(span[0].lo, j)) & (key < __shfl(own_hi, j));
+      if (hit && note) atomicOr(&poison[j][lane >> 1], note << (16 * (lane & 1)));
     }
+  };
+  auto keep_notes = [&](int stage, int k, uint32_t bad) {
+    if (!partial(k, bad) || !__any(lane < RW && noted[stage][kg][lane & (RW - 1)])) return;
+    start_notes();
+#pragma unroll 1
+    for (int r = 0; r < KEYS; ++r) keep_note(k + r, lane < 16 ? notes[stage][kg][r][lane] : 0u);
     wave_sync();
   };
   auto mine = [&](int k) { return k < min(R.hi, k_end) && k + KEYS > R.lo; };  // whether this wave's rows see the tile
@@ -381,9 +393,39 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       softmax(k, bad);
       __builtin_amdgcn_s_setprio(1);
       sums(T + kTile);
-      feed<8 * kSub, 2>();
+      feed<8 * kSub, 2, kTails ? 2 : 1>();
       __builtin_amdgcn_s_setprio(0);
     }
+    if constexpr (kTails) {
+      // An infinity's products with a weight's head and tail differ in sign, or are infinity times zero: in tiles that
+      // every row sees whole the sum is NaN where it should be infinite.  If a sum is NaN over weights that are not, the
+      // wave looks through its values once more.
+      f32x16 all = (O[0] + O[1]) + (O[2] + O[3]);
+#pragma unroll
+      for (int n = 8; n; n /= 2) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) all[i] += all[i + n];
+      }
+      const float total = add_xor32(z);
+      if (__any((all[0] != all[0]) & (total == total))) {
+        start_notes();
+#pragma unroll 1
+        for (int k0 = k_beg + kg * KEYS; k0 < k_end; k0 += step) {
+#pragma unroll 1
+          for (int key = k0; key < min(k0 + KEYS, k_end); ++key) {
+            const int64_t at = page_row(p.pages, L.shift, s, key);
+            if (at < 0) continue;
+            const u32x4 v = reinterpret_cast<const u32x4 *>(L.V + at + head)[lane & 15];
+            uint32_t note = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) note |= (poison_of(v[e] << 16) | poison_of(v[e] & 0xffff0000u) << 2) << (4 * e);
+            keep_note(key, lane < 16 ? note : 0u);
+          }
+        }
+        wave_sync();
+      }
+    }
+    // (a NaN weight makes the row's total NaN, and with it what is noted)
     if (poisoned) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
@@ -391,7 +433,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
         for (int j = 0; j < 4; ++j) {
           const uint32_t note = poison[c][2 * d + j / 2] >> (16 * (j % 2) + 8 * half);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) O[d][4 * j + i] += poison_value((note >> (2 * i)) & 3u);
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = (note >> (2 * i)) & 3u;
+            if (x) O[d][4 * j + i] = poison_value(x);
+          }
         }
       }
     }
