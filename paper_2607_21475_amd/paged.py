@@ -407,7 +407,10 @@ def rope_frequencies(rot_dim: int = HEAD_DIM, base: float = 10000.0, scaling: st
       bands   by the turns t = original f / 2 pi that a pair makes over the original context: f from `high` turns
               (default 4) on, f / factor up to `low` (default 1), and between them g f + (1 - g) f / factor with
               g = (t - low) / (high - low)
-      yarn    as bands, with `high` 32, and the amplitude 0.1 ln(factor) + 1
+      yarn    as bands, with `high` 32, and the amplitude 0.1 ln(factor) + 1: linear in the turns, as the method is
+              written.  Checkpoints whose frequencies were blended linearly in the pair's index i, between the (perhaps
+              rounded) indices at which the turns are `high` and `low`, were trained with others in that band: give
+              `rotary` those.
     """
     if rot_dim < 2 or rot_dim > HEAD_DIM or rot_dim % 2:
         raise ValueError("rot_dim must be even, 2 to %d" % HEAD_DIM)
