@@ -16,12 +16,12 @@
 //   rows by eight waves, one work-group a CU, for one sequence's long chunks: each tile is loaded half as often.
 //   64 query rows by eight waves, in four groups of two that take every fourth tile of 32 keys: 33 to 64 rows are
 //   too few to hide the memory with 128-row blocks, and too much work for attend_rows' one wave a SIMD (16 sequences
-//   of up to 6144 rows, 56 query rows: 38 us, attend_rows 58).
+//   of up to 6144 rows, 56 query rows: 40 us, attend_rows 58).
 //   The matrix products bound it: 4 x 128 operations per (query row, key).  So the weights of the first two shapes are
 //   rounded to bf16 (half a step, 2^-8, averaged over a row's keys); a second product with their tails, 16 bits in all,
 //   costs 20 to 40% (8192 tokens over 8192 rows 770 us with it, 566 without, 1024 over 131072 2930 / 2070, 1024 over 1024
 //   38.7 / 32.0).  The third shape is bound by memory and has it (the call above with its join 42.0 / 40.9).  1024 tokens, 32
-//   heads, over 131072 rows: 2.06 to 2.18 ms, 1.0 to 1.06 PFLOP/s; the matrix cores are busy 54% of the
+//   heads, over 131072 rows: 1.95 to 2.06 ms, 1.06 to 1.12 PFLOP/s; the matrix cores are busy 54% of the
 //   cycles, of which the power limit leaves about 2.0 to 2.1 GHz (a large product runs at 1.34 PFLOP/s there).
 #include "attend_paged.hpp"
 

@@ -135,7 +135,8 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t ro
   }
   // keys and values that one work-group alone reads, and too many to stay in the last-level cache until the next call
   // on the same layer (us without / with the hint; groups of 4, 8 KV heads): 32 sequences of 16384 rows 356 / 318, 64 of up
-  // to 4096 rows 124 / 111, 16 of up to 6144 rows, 8 tokens, 41.5 / 39.1; one of 4096 rows, found in the cache, 14.4 / 15.3
+  // to 4096 rows 124 / 111, 16 of up to 6144 rows, 8 tokens, eight layers in turn, 46.1 / 42.9; one of 4096 rows,
+  // found in the cache, 14.4 / 15.3
   L.once = aside == 1 && S * H * span * 4 * kHeadDim > kCacheBytes;
   L.by_group.set(p->group);
   L.by_heads.set(H);
