@@ -313,6 +313,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     start_notes();
 #pragma unroll 1
     for (int k0 = k_beg + wave * kTileKeys; k0 < k_end; k0 += stride) {
+      if (!any_not_finite(L, s, head, k0, k_end)) continue;
 #pragma unroll 1
       for (int key = k0; key < min(k0 + kTileKeys, k_end); ++key) {
         const int64_t at = page_row(p.pages, L.shift, s, key);

@@ -189,6 +189,21 @@ __device__ __forceinline__ float poison_value(uint32_t note) {
   return note == 0u ? 0.0f : note == 1u ? INFINITY : note == 2u ? -INFINITY : NAN;
 }
 
+// Whether any value of the rows k .. end - 1 (at most 32) of a sequence's KV head is not finite; `head`: its offset.
+__device__ __forceinline__ bool any_not_finite(const AttendPagedLaunch &L, int s, int64_t head, int k, int end) {
+  const int lane = threadIdx.x & 63;
+  bool found = false;
+#pragma unroll 2
+  for (int r = lane >> 4; r < 32; r += 4) {
+    const int64_t at = k + r < end ? page_row(L.p.pages, L.shift, s, k + r) : -1;
+    if (at < 0) continue;
+    const u32x4 v = reinterpret_cast<const u32x4 *>(L.V + at + head)[lane & 15];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) found |= not_finite(v[e]) | not_finite(v[e] << 16);
+  }
+  return __any(found);
+}
+
 // range_of the query rows of tokens j0 .. j1 without positions of their own (p.qpos is NULL): what they see moves
 // on with the token, so the first and the last that see anything tell.
 __device__ __forceinline__ Range range_of_tokens(const ebd_attend_paged_params &p, const Seq &q, int j0, int j1) {

@@ -397,6 +397,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       __builtin_amdgcn_s_setprio(0);
     }
     if constexpr (kTails) {
+      static_assert(KEYS == 32, "tiles of any_not_finite");
       // An infinity's products with a weight's head and tail differ in sign, or are infinity times zero: in tiles that
       // every row sees whole the sum is NaN where it should be infinite.  If a sum is NaN over weights that are not, the
       // wave looks through its values once more.
@@ -411,6 +412,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
         start_notes();
 #pragma unroll 1
         for (int k0 = k_beg + kg * KEYS; k0 < k_end; k0 += step) {
+          if (!any_not_finite(L, s, head, k0, k_end)) continue;
 #pragma unroll 1
           for (int key = k0; key < min(k0 + KEYS, k_end); ++key) {
             const int64_t at = page_row(p.pages, L.shift, s, key);
