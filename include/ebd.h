@@ -513,16 +513,92 @@ typedef struct ebd_gather_paged_params {
 ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K, const uint16_t *V,
                             uint16_t *Ku, uint16_t *Vu, uint32_t *status, void *stream);
 
+/*
+ * Norms of heads.  A row x of 128 elements becomes r w x with r = 1 / sqrt(mean x^2 + eps), w the weights of its head.
+ *   weight       device float, 16-byte aligned: [128] for all heads (head_stride 0) or a row for each head (head_stride
+ *                elements apart, a multiple of 4, at least 128, below 2^40).
+ *   eps          positive and finite.
+ */
+typedef struct ebd_norm {
+    const float *weight;
+    int64_t head_stride;
+    float eps;
+    int32_t reserved; /* 0 */
+} ebd_norm;
+
+/*
+ * ebd_norm_rope -- norm of num_tokens x num_heads rows and their rotary positions in one pass, y = R (r w x): all steps in
+ * fp32, rounded once.  (A row whose squares' sum passes fp32 is scaled before; an infinite or NaN element gives what the
+ * formula gives.)
+ *   rot.freq  NULL: no rotation (pos is not read and may be NULL; amplitude unused).
+ *   y may be x itself (same address and strides); they may not overlap otherwise.
+ */
+typedef struct ebd_norm_rope_params {
+    int32_t num_tokens;
+    int32_t num_heads;
+    int32_t head_dim;
+    int32_t reserved; /* 0 */
+    ebd_rows x, y;
+    const int32_t *pos;
+    ebd_norm norm;
+    ebd_rotary rot;
+} ebd_norm_rope_params;
+
+ebd_status ebd_norm_rope(const ebd_norm_rope_params *p, const uint16_t *x, uint16_t *y, void *stream);
+
+/*
+ * ebd_norm_rope_backward -- gradients of ebd_norm_rope: from x (its input) and dy, with g = R^T dy and h = g w,
+ *     dx = r (h - x r^2 mean(h x)),     dweight = sum of g r x over the tokens (and the heads that share the weights)
+ *   rot  as given to the forward call (its flags too).  dx may be x or dy (same address and strides).
+ *   dweight  [128] fp32 (norm.head_stride 0) or [num_heads, 128] contiguous, written (zeros without tokens); its sums are
+ *            taken in a fixed order: the same call gives the same bits.
+ *   workspace: ebd_workspace_size(EBD_WS_NORM_ROPE_BACKWARD, p) bytes, 256-byte aligned.
+ */
+typedef struct ebd_norm_rope_backward_params {
+    int32_t num_tokens;
+    int32_t num_heads;
+    int32_t head_dim;
+    int32_t reserved; /* 0 */
+    ebd_rows x, dy, dx;
+    const int32_t *pos;
+    ebd_norm norm;
+    ebd_rotary rot;
+} ebd_norm_rope_backward_params;
+
+ebd_status ebd_norm_rope_backward(const ebd_norm_rope_backward_params *p, const uint16_t *x, const uint16_t *dy,
+                                  uint16_t *dx, float *dweight, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * ebd_append_norm -- ebd_append_paged with norms: the new keys are normalised by k_norm and the queries by q_norm before
+ * their rotation (weight NULL: not normalised), in one pass, all in fp32 and rounded once.
+ *   slots  [num_tokens] device int64 or NULL.  Given (by ebd_plan_step), token t goes to slot slots[t] % page_size of page
+ *          slots[t] / page_size, and append.new_off, append.len and the page table are not read (they may be NULL);
+ *          append.pos is then needed where there is a rotation, and nothing is written, the query included, for a token
+ *          whose slot lies outside the pool (-1: padding); status is not written.  No two tokens may have one slot.
+ *          NULL: as ebd_append_paged.
+ */
+typedef struct ebd_append_norm_params {
+    ebd_append_paged_params append;
+    ebd_norm k_norm, q_norm;
+    const int64_t *slots;
+} ebd_append_norm_params;
+
+ebd_status ebd_append_norm(const ebd_append_norm_params *p, const uint16_t *k_new, const uint16_t *v_new, uint16_t *K,
+                           uint16_t *V, const uint16_t *q, uint16_t *q_out, uint32_t *status, void *stream);
+
 /* which-values for ebd_workspace_size */
 #define EBD_WS_EVICT 0
 #define EBD_WS_ATTEND 1
 #define EBD_WS_SCORES 2
 #define EBD_WS_ATTEND_PAGED 3
+#define EBD_WS_NORM_ROPE_BACKWARD 5
 
 /*
  * Workspace bytes needed by ebd_evict (which = EBD_WS_EVICT, params = ebd_evict_params*),
  * ebd_attend_certify (EBD_WS_ATTEND, ebd_attend_params*), ebd_scores (EBD_WS_SCORES,
- * ebd_scores_params*) or ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*).
+ * ebd_scores_params*) or ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*),
+ * ebd_norm_rope_backward (EBD_WS_NORM_ROPE_BACKWARD,
+ * ebd_norm_rope_backward_params*).
  * Depends only on the host fields of the params.  Returns 0 on invalid arguments.
  */
 size_t ebd_workspace_size(int32_t which, const void *params);
@@ -539,7 +615,9 @@ const char *ebd_version(void);
  * ebd_timing_read() waits for the recorded events, and adds the elapsed times of kernel `name`
  * ("evict_select", "evict_copy", "attend_split", "attend_finalize", "append_certain",
  * "scores_stats", "scores_accum", "block_contrib", "cert_step", "rope", "append_paged",
- * "attend_paged", "attend_paged_join", "gather_paged") to *total_ms and its launch count to
+ * "attend_paged", "attend_paged_join", "gather_paged",
+ * "norm_rope", "norm_rope_backward", "norm_rope_join",
+ * "append_norm") to *total_ms and its launch count to
  * *launches; it then clears that kernel's record.  The switch is an atomic flag and the records
  * are guarded by a lock, so both calls may come from any host thread; while timing is off no
  * event is created and launches take no lock.

@@ -8,6 +8,7 @@ error statuses.  The functions carry the C names:
     ebd_attend_certify   Hajek decode attention + Theorem 2 variance + eq. (4) radius
     ebd_append_certain   append a decode token with pi = 1
     ebd_rope, ebd_append_paged, ebd_attend_paged, ebd_gather_paged   the paged cache before eviction (paged.py)
+    ebd_norm_rope, ebd_norm_rope_backward, ebd_append_norm           ... with norms of queries and keys for each head
     ebd_workspace_size, ebd_status_string, ebd_version, ebd_timing_enable, ebd_timing_read
 
 The library must be built (``python paper_2607_21475_amd/build.py``); importing this package
@@ -52,6 +53,9 @@ EBD_WS_EVICT = 0
 EBD_WS_ATTEND = 1
 EBD_WS_SCORES = 2
 EBD_WS_ATTEND_PAGED = 3
+EBD_WS_ATTEND_TREE = 4
+EBD_WS_NORM_ROPE_BACKWARD = 5
+EBD_WS_PLAN_STEP = 6
 EBD_SCORES_ACCUMULATE = 1
 EBD_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -256,7 +260,10 @@ def scores_params(num_units, num_queries, max_rows, seq_off, qpos=None, split_ro
 
 def ebd_workspace_size(which: int, params) -> int:
     n = _lib.ebd_workspace_size(int(which), ctypes.byref(params))
-    units = params.pages.num_seqs if which == EBD_WS_ATTEND_PAGED else params.num_units
+    if which in (EBD_WS_ATTEND_TREE, EBD_WS_NORM_ROPE_BACKWARD, EBD_WS_PLAN_STEP):
+        units = 1  # (their calls need a workspace of whatever size)
+    else:
+        units = params.pages.num_seqs if which == EBD_WS_ATTEND_PAGED else params.num_units
     if n == 0 and units > 0:
         raise EbdError("ebd_workspace_size", EBD_ERR_INVALID_ARG)
     return int(n)
@@ -379,5 +386,7 @@ def workspace(nbytes: int, device="cuda") -> torch.Tensor:
 
 
 from .paged import (EBD_ROPE_HALF, EBD_ROPE_INVERSE, EBD_ROPE_PAIRS, PagedCache,  # noqa: E402
-                    append_paged_params, attend_paged_params, ebd_append_paged, ebd_attend_paged, ebd_gather_paged,
-                    ebd_pages, ebd_rope, ebd_rotary, gather_paged_params, pages, rope_frequencies, rope_params, rotary)
+                    append_norm_params, append_paged_params, attend_paged_params, ebd_append_norm, ebd_append_paged,
+                    ebd_attend_paged, ebd_gather_paged, ebd_norm, ebd_norm_rope, ebd_norm_rope_backward, ebd_pages,
+                    ebd_rope, ebd_rotary, gather_paged_params, head_norm, norm_rope_backward_params, norm_rope_params,
+                    pages, rope_frequencies, rope_params, rotary)

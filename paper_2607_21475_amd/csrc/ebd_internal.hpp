@@ -179,6 +179,33 @@ struct AppendPagedLaunch {
   int32_t per, tpb;
 };
 
+struct NormRopeLaunch {
+  ebd_norm_rope_params p;  // amplitude resolved
+  const uint16_t *x;
+  uint16_t *y;
+  int32_t per, tpb;
+};
+
+struct NormRopeBackwardLaunch {
+  ebd_norm_rope_backward_params p;
+  const uint16_t *x, *dy;
+  uint16_t *dx;
+  float *dweight;
+  float *part;     // [parts, 128] (weights of each head's own: [parts, heads, 128]) sums of dweight
+  int32_t per, tpb;
+  int32_t groups;  // work-groups a block of heads
+  int32_t parts;
+};
+
+struct AppendNormLaunch {
+  ebd_append_norm_params p;
+  const uint16_t *k_new, *v_new, *q;
+  uint16_t *K, *V, *q_out;
+  uint32_t *status;
+  int32_t shift;
+  int32_t per, tpb;
+};
+
 struct GatherPagedLaunch {
   ebd_gather_paged_params p;
   const uint16_t *K, *V;
@@ -254,6 +281,13 @@ hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hip
 
 hipError_t launch_rope(RopeLaunch L, hipStream_t s);
 hipError_t launch_append_paged(AppendPagedLaunch L, hipStream_t s);
+hipError_t launch_norm_rope(NormRopeLaunch L, hipStream_t s);
+NormRopeBackwardLaunch norm_rope_backward_plan(const ebd_norm_rope_backward_params &p);
+size_t norm_rope_backward_bytes(const NormRopeBackwardLaunch &L);
+size_t norm_rope_backward_workspace(const ebd_norm_rope_backward_params *p);  // 0: invalid parameters
+hipError_t launch_norm_rope_backward(const NormRopeBackwardLaunch &L, hipStream_t s);
+hipError_t launch_norm_rope_join(const NormRopeBackwardLaunch &L, hipStream_t s);
+hipError_t launch_append_norm(AppendNormLaunch L, hipStream_t s);
 int64_t gather_paged_groups(const ebd_gather_paged_params &p);
 hipError_t launch_gather_paged(GatherPagedLaunch L, hipStream_t s);
 int64_t attend_paged_groups(const AttendPagedLaunch &L);

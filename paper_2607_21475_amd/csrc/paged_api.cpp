@@ -54,6 +54,20 @@ bool valid_rotary(const ebd_rotary &R) {
 
 float amplitude_of(const ebd_rotary &R) { return R.amplitude != 0.0f ? R.amplitude : 1.0f; }
 
+bool valid_norm(const ebd_norm &N) {
+  if (((uintptr_t)N.weight & 15) || N.head_stride % 4 || N.head_stride >= kStrideMax || N.reserved != 0) return false;
+  return (N.head_stride == 0 || N.head_stride >= kHeadDim) && std::isnormal(N.eps) && N.eps > 0.0f;
+}
+
+bool valid_norm_rope_backward(const ebd_norm_rope_backward_params *p) {
+  return p && p->num_tokens >= 0 && p->num_heads >= 0 && p->reserved == 0 && valid_norm(p->norm) && p->norm.weight &&
+         (!p->rot.freq || valid_rotary(p->rot)) && valid_rows(p->x) && valid_rows(p->dy) && valid_rows(p->dx);
+}
+bool supported_heads(int32_t head_dim, int32_t tokens, int32_t heads) {
+  return head_dim == kHeadDim && tokens <= kGridMax && heads <= kHeadsMax;
+}
+size_t backward_bytes(const NormRopeBackwardLaunch &L) { return (norm_rope_backward_bytes(L) + 255) / 256 * 256 + 256; }
+
 bool valid_attend_paged(const ebd_attend_paged_params *p) {
   if (!p || !valid_pages(p->pages)) return false;
   if (p->group < 1 || p->max_new < 0 || p->num_tokens < 0 || p->max_rows < 0) return false;
@@ -204,6 +218,11 @@ size_t attend_paged_workspace(const ebd_attend_paged_params *p) {
   return plan_bytes(attend_paged_plan(p));
 }
 
+size_t norm_rope_backward_workspace(const ebd_norm_rope_backward_params *p) {
+  if (!valid_norm_rope_backward(p) || !supported_heads(p->head_dim, p->num_tokens, p->num_heads)) return 0;
+  return backward_bytes(norm_rope_backward_plan(*p));
+}
+
 }  // namespace ebd
 
 extern "C" {
@@ -314,6 +333,87 @@ ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K,
   hipStream_t s = static_cast<hipStream_t>(stream);
   return timed_launch("gather_paged", s, [&] { return launch_gather_paged(L, s); }) == hipSuccess ? EBD_OK
                                                                                                    : EBD_ERR_HIP;
+}
+
+ebd_status ebd_norm_rope(const ebd_norm_rope_params *p, const uint16_t *x, uint16_t *y, void *stream) {
+  if (!p || p->num_tokens < 0 || p->num_heads < 0 || p->reserved != 0) return EBD_ERR_INVALID_ARG;
+  if (!valid_norm(p->norm) || !p->norm.weight || (p->rot.freq && !valid_rotary(p->rot))) return EBD_ERR_INVALID_ARG;
+  if (!valid_rows(p->x) || !valid_rows(p->y)) return EBD_ERR_INVALID_ARG;
+  if (!supported_heads(p->head_dim, p->num_tokens, p->num_heads)) return EBD_ERR_UNSUPPORTED;
+  if (p->num_tokens == 0 || p->num_heads == 0) return EBD_OK;
+  if (!x || !y || (p->rot.freq && !p->pos) || !aligned16(x) || !aligned16(y)) return EBD_ERR_INVALID_ARG;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  NormRopeLaunch L{};
+  L.p = *p;
+  L.p.rot.amplitude = amplitude_of(p->rot);
+  L.x = x;
+  L.y = y;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("norm_rope", s, [&] { return launch_norm_rope(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
+}
+
+ebd_status ebd_norm_rope_backward(const ebd_norm_rope_backward_params *p, const uint16_t *x, const uint16_t *dy,
+                                  uint16_t *dx, float *dweight, void *workspace, size_t ws_bytes, void *stream) {
+  if (!valid_norm_rope_backward(p)) return EBD_ERR_INVALID_ARG;
+  if (!supported_heads(p->head_dim, p->num_tokens, p->num_heads)) return EBD_ERR_UNSUPPORTED;
+  if (!dweight || ((uintptr_t)dweight & 3)) return EBD_ERR_INVALID_ARG;
+  const bool rows = p->num_tokens > 0 && p->num_heads > 0;
+  if (p->num_heads == 0 && p->norm.head_stride) return EBD_OK;
+  if (rows && (!x || !dy || !dx || (p->rot.freq && !p->pos))) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(dy) || !aligned16(dx)) return EBD_ERR_INVALID_ARG;
+  NormRopeBackwardLaunch L = norm_rope_backward_plan(*p);
+  if (!workspace || ws_bytes < backward_bytes(L) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  L.p.rot.amplitude = amplitude_of(p->rot);
+  L.x = x;
+  L.dy = dy;
+  L.dx = dx;
+  L.dweight = dweight;
+  L.part = static_cast<float *>(workspace);
+  if (!rows) L.parts = 0;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (rows && timed_launch("norm_rope_backward", s, [&] { return launch_norm_rope_backward(L, s); }) != hipSuccess)
+    return EBD_ERR_HIP;
+  return timed_launch("norm_rope_join", s, [&] { return launch_norm_rope_join(L, s); }) == hipSuccess ? EBD_OK
+                                                                                                      : EBD_ERR_HIP;
+}
+
+ebd_status ebd_append_norm(const ebd_append_norm_params *n, const uint16_t *k_new, const uint16_t *v_new, uint16_t *K,
+                           uint16_t *V, const uint16_t *q, uint16_t *q_out, uint32_t *status, void *stream) {
+  if (!n) return EBD_ERR_INVALID_ARG;
+  const ebd_append_paged_params *p = &n->append;
+  ebd_pages P = p->pages;
+  if (n->slots) P.num_seqs = 0;  // neither the table nor the sequences are looked at
+  if (!valid_pages(P) || p->num_tokens < 0 || p->q_heads < 0 || p->reserved != 0) return EBD_ERR_INVALID_ARG;
+  if (p->rot.freq && !valid_rotary(p->rot)) return EBD_ERR_INVALID_ARG;
+  if ((n->k_norm.weight && !valid_norm(n->k_norm)) || (n->q_norm.weight && !valid_norm(n->q_norm)))
+    return EBD_ERR_INVALID_ARG;
+  if (!valid_rows(p->k_rows) || !valid_rows(p->v_rows) || !valid_rows(p->q_rows) || !valid_rows(p->q_out_rows))
+    return EBD_ERR_INVALID_ARG;
+  if (!supported_pages(P) || p->num_tokens > kGridMax || p->q_heads > kHeadsMax) return EBD_ERR_UNSUPPORTED;
+  if (p->num_tokens == 0 || (!n->slots && P.num_seqs == 0)) return EBD_OK;
+  if (!k_new || !v_new || !K || !V) return EBD_ERR_INVALID_ARG;
+  if (n->slots ? (p->rot.freq && !p->pos) || ((uintptr_t)n->slots & 7) : !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(K) || !aligned16(V)) return EBD_ERR_INVALID_ARG;
+  if ((p->q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr)) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(q_out)) return EBD_ERR_INVALID_ARG;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  AppendNormLaunch L{};
+  L.p = *n;
+  L.p.append.rot.amplitude = amplitude_of(p->rot);
+  L.k_new = k_new;
+  L.v_new = v_new;
+  L.q = q;
+  L.K = K;
+  L.V = V;
+  L.q_out = q_out;
+  L.status = status;
+  L.shift = log2_of(p->pages.page_size);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("append_norm", s, [&] { return launch_append_norm(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
 }
 
 }  // extern "C"

@@ -13,24 +13,11 @@
 // there; tokens of few rows share a work-group.
 #include "ebd.h"
 #include "ebd_internal.hpp"
-#include "paged_device.hpp"
-
-#include <algorithm>
+#include "rope_device.hpp"
 
 namespace ebd {
 
 namespace {
-
-constexpr int kRopeRows = 128;  // most rows of a work-group: 8 lanes each
-
-// cos and sin (times the amplitude) of pair `i` at position `pos`.
-__device__ __forceinline__ float2 turn(const ebd_rotary &R, int i, int64_t pos) {
-  const double t = (double)pos * R.freq[i] * 0.15915494309189535;  // 1 / 2 pi
-  float s, c;
-  sincospif(2.0f * (float)(t - rint(t)), &s, &c);
-  if (R.flags & EBD_ROPE_INVERSE) s = -s;
-  return make_float2(R.amplitude * c, R.amplitude * s);
-}
 
 // Eight pairs whose first elements are in a and second ones in b.
 __device__ __forceinline__ void rotate8(uint4 &a, uint4 &b, const float2 *cs) {
@@ -54,21 +41,6 @@ __device__ __forceinline__ void rotate_pairs(uint4 &a, const float2 *cs, int n) 
     const uint32_t r = pack_bf16(x * t.x - y * t.y, y * t.x + x * t.y);
     p[w] = w < n ? r : p[w];
   }
-}
-
-// How the eight lanes of a row split it: lane l's two 16-byte chunks (elements), and whether the second
-// elements of the first chunk's pairs are the second chunk (halves), which needs rot_dim / 2 to be whole
-// chunks.  Other halves go element by element (kOdd).
-enum { kCopy, kHalf, kPairs, kOdd };
-struct Split {
-  int how, e0, e1;
-};
-__device__ __forceinline__ Split split_row(const ebd_rotary &R, int l, bool rotated) {
-  if (!rotated || !R.freq) return {kCopy, 16 * l, 16 * l + 8};
-  if (R.layout == EBD_ROPE_PAIRS) return {kPairs, 16 * l, 16 * l + 8};
-  if (R.rot_dim % 16) return {kOdd, 0, 0};
-  if (16 * l < R.rot_dim) return {kHalf, 8 * l, R.rot_dim / 2 + 8 * l};
-  return {kCopy, 16 * l, 16 * l + 8};
 }
 
 // A rotary half that is no multiple of eight elements: lane l takes every eighth pair, then every eighth
@@ -95,23 +67,7 @@ __device__ __forceinline__ void turn_row(const ebd_rotary &R, const Split &S, ui
   }
 }
 
-// Rows are read once, so that they leave no trace in the caches (8191 tokens of 32 rows 31.2 -> 28.9 us, append of 13k
-// tokens of 36 rows 53 -> 52); what is written stays there for the attention that reads it next.
-__device__ __forceinline__ uint4 load16(const uint16_t *p) {
-  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)));
-}
-__device__ __forceinline__ void store16(uint16_t *p, const uint4 &v) { *reinterpret_cast<uint4 *>(p) = v; }
-
 }  // namespace
-
-// Work-group (token group, block of rows): `per` threads, whole waves, for each of up to four tokens.  A dimension of the
-// grid holds fewer than 2^32 threads, which 2^24 tokens of up to 1024 pass, so token groups fill x and go on in z.
-constexpr int kAcross = 1 << 21;
-__device__ __forceinline__ int64_t token_group(int x, int z) { return (int64_t)z * kAcross + x; }
-__device__ __forceinline__ int token_slot(int per) {
-  const int t = threadIdx.x;
-  return (t >= per) + (t >= 2 * per) + (t >= 3 * per);
-}
 
 __global__ __launch_bounds__(8 * kRopeRows) void rope_kernel(RopeLaunch L) {
   __shared__ float2 cs[4][kHeadDim / 2];
@@ -182,28 +138,15 @@ __global__ __launch_bounds__(8 * kRopeRows) void append_paged_kernel(AppendPaged
   store16(y + sp.e1, b);
 }
 
-namespace {
-// Threads of a token and tokens of a work-group.
-void cut(int64_t rows, int32_t *per, int32_t *tpb) {
-  *per = (int32_t)((std::min<int64_t>(rows, kRopeRows) * 8 + 63) / 64 * 64);
-  *tpb = std::max(1, std::min(4, 256 / *per));
-}
-dim3 rope_grid(int64_t tokens, int64_t rows, int tpb) {
-  const int64_t groups = (tokens + tpb - 1) / tpb;
-  return dim3((unsigned)std::min<int64_t>(groups, kAcross), (unsigned)((rows + kRopeRows - 1) / kRopeRows),
-              (unsigned)((groups + kAcross - 1) / kAcross));
-}
-}  // namespace
-
 hipError_t launch_rope(RopeLaunch L, hipStream_t s) {
-  cut(L.p.num_heads, &L.per, &L.tpb);
+  cut_tokens(L.p.num_heads, &L.per, &L.tpb);
   hipLaunchKernelGGL(rope_kernel, rope_grid(L.p.num_tokens, L.p.num_heads, L.tpb), dim3(L.per * L.tpb), 0, s, L);
   return hipGetLastError();
 }
 
 hipError_t launch_append_paged(AppendPagedLaunch L, hipStream_t s) {
   const int64_t rows = 2 * (int64_t)L.p.pages.kv_heads + L.p.q_heads;
-  cut(rows, &L.per, &L.tpb);
+  cut_tokens(rows, &L.per, &L.tpb);
   hipLaunchKernelGGL(append_paged_kernel, rope_grid(L.p.num_tokens, rows, L.tpb), dim3(L.per * L.tpb), 0, s, L);
   return hipGetLastError();
 }

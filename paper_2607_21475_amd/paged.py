@@ -4,6 +4,8 @@
     ebd_append_paged    new tokens into their sequences' pages, keys rotated on the way, queries too
     ebd_attend_paged    attention of a chunk of new tokens, or of a decode step, over the pages
     ebd_gather_paged    the pages read out as units, which ebd_scores and ebd_evict take
+    ebd_norm_rope       norms of heads and rotary positions in one pass; ebd_norm_rope_backward: their gradients
+    ebd_append_norm     ebd_append_paged for models that normalise queries and keys for each head
 
 Each call takes a parameter struct (`rope_params`, `append_paged_params`, ...) that a program makes once
 per plan and keeps: it holds the tables' addresses and the rows' strides.  A struct keeps the tensors
@@ -116,6 +118,53 @@ class ebd_gather_paged_params(ctypes.Structure):
     ]
 
 
+class ebd_norm(ctypes.Structure):
+    _fields_ = [
+        ("weight", ctypes.c_void_p),
+        ("head_stride", ctypes.c_int64),
+        ("eps", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class ebd_norm_rope_params(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("x", ebd_rows),
+        ("y", ebd_rows),
+        ("pos", ctypes.c_void_p),
+        ("norm", ebd_norm),
+        ("rot", ebd_rotary),
+    ]
+
+
+class ebd_norm_rope_backward_params(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("x", ebd_rows),
+        ("dy", ebd_rows),
+        ("dx", ebd_rows),
+        ("pos", ctypes.c_void_p),
+        ("norm", ebd_norm),
+        ("rot", ebd_rotary),
+    ]
+
+
+class ebd_append_norm_params(ctypes.Structure):
+    _fields_ = [
+        ("append", ebd_append_paged_params),
+        ("k_norm", ebd_norm),
+        ("q_norm", ebd_norm),
+        ("slots", ctypes.c_void_p),
+    ]
+
+
 _lib.ebd_rope.argtypes = [_P] * 4
 _lib.ebd_rope.restype = ctypes.c_int
 _lib.ebd_append_paged.argtypes = [_P] * 9
@@ -124,6 +173,12 @@ _lib.ebd_attend_paged.argtypes = [_P] * 8 + [ctypes.c_size_t, _P]
 _lib.ebd_attend_paged.restype = ctypes.c_int
 _lib.ebd_gather_paged.argtypes = [_P] * 7
 _lib.ebd_gather_paged.restype = ctypes.c_int
+_lib.ebd_norm_rope.argtypes = [_P] * 4
+_lib.ebd_norm_rope.restype = ctypes.c_int
+_lib.ebd_norm_rope_backward.argtypes = [_P] * 6 + [ctypes.c_size_t, _P]
+_lib.ebd_norm_rope_backward.restype = ctypes.c_int
+_lib.ebd_append_norm.argtypes = [_P] * 9
+_lib.ebd_append_norm.restype = ctypes.c_int
 
 
 # ---- tensors -> parameters ---------------------------------------------------------------------
@@ -260,6 +315,101 @@ def rope_params(x, y, pos, rot: ebd_rotary) -> ebd_rope_params:
     return _plan(p, _here(x, y, pos, rot.keep), (pos, rot.keep), x=x, y=y)
 
 
+def head_norm(weight, eps: float = 1e-6) -> ebd_norm:
+    """Norms of heads: weights [128] of all heads, or [heads, 128] of each one's own (fp32)."""
+    if not isinstance(weight, torch.Tensor):
+        raise TypeError("weight must be a torch.Tensor")
+    if weight.dtype != torch.float32:
+        raise TypeError("weight must be %s, got %s" % (torch.float32, weight.dtype))
+    if weight.device.type != "cuda":
+        raise ValueError("weight must be on the GPU")
+    if weight.dim() not in (1, 2) or weight.shape[-1] != HEAD_DIM or weight.stride(-1) != 1:
+        raise ValueError("weight must be [%d] or [heads, %d] with contiguous rows" % (HEAD_DIM, HEAD_DIM))
+    n = ebd_norm()
+    n.weight, n.eps = weight.data_ptr(), float(eps)
+    if weight.dim() == 2:  # (a stride over one head is never used, and may be anything)
+        n.head_stride = weight.stride(0) if weight.shape[0] > 1 else HEAD_DIM
+    n.keep = weight
+    return n
+
+
+def _norm_of(norm, heads, name):
+    if not isinstance(norm, ebd_norm):
+        raise TypeError("%s must be made by head_norm" % name)
+    if norm.keep.dim() == 2 and norm.keep.shape[0] != heads:
+        raise ValueError("%s has weights of %d heads, not %d" % (name, norm.keep.shape[0], heads))
+    return norm
+
+
+def _turned(p, rot, pos, tokens):
+    """Note a rotation (or none) and its positions; returns the frequencies."""
+    if rot is None:
+        return None
+    if rot.keep is None:
+        raise ValueError("rot needs frequencies")
+    if pos is None:
+        raise ValueError("a rotation needs positions")
+    p.rot = rot
+    p.pos = _table(pos, torch.int32, (tokens,), "pos")
+    return rot.keep
+
+
+def norm_rope_params(x, y, norm: ebd_norm, rot: Optional[ebd_rotary] = None, pos=None) -> ebd_norm_rope_params:
+    """Rows x [tokens, heads, 128] -> y (may be x), normalised, and with `rot` rotated by pos [tokens] int32."""
+    (tokens, heads, _), _ = _layout(x, "x")
+    _layout(y, "y", heads, tokens)
+    _distinct(y, "y")
+    p = ebd_norm_rope_params()
+    p.num_tokens, p.num_heads, p.head_dim = tokens, heads, HEAD_DIM
+    p.x, p.y = _rows_of(x), _rows_of(y)
+    p.norm = _norm_of(norm, heads, "norm")
+    freq = _turned(p, rot, pos, tokens)
+    return _plan(p, _here(x, y, pos if rot else None, norm.keep, freq), (pos, norm.keep, freq), x=x, y=y)
+
+
+def norm_rope_backward_params(x, dy, dx, norm: ebd_norm, rot: Optional[ebd_rotary] = None,
+                              pos=None) -> ebd_norm_rope_backward_params:
+    """Gradients of norm_rope_params' call with the same norm, rot and pos: dy -> dx (may be dy or x)."""
+    (tokens, heads, _), _ = _layout(x, "x")
+    _layout(dy, "dy", heads, tokens)
+    _layout(dx, "dx", heads, tokens)
+    _distinct(dx, "dx")
+    p = ebd_norm_rope_backward_params()
+    p.num_tokens, p.num_heads, p.head_dim = tokens, heads, HEAD_DIM
+    p.x, p.dy, p.dx = _rows_of(x), _rows_of(dy), _rows_of(dx)
+    p.norm = _norm_of(norm, heads, "norm")
+    freq = _turned(p, rot, pos, tokens)
+    p.weights = norm.keep.shape
+    return _plan(p, _here(x, dy, dx, pos if rot else None, norm.keep, freq), (pos, norm.keep, freq), x=x, dy=dy, dx=dx)
+
+
+def append_norm_params(pgs: ebd_pages, k_new, v_new, new_off=None, len=None, k_norm: Optional[ebd_norm] = None,
+                       q_norm: Optional[ebd_norm] = None, rot: Optional[ebd_rotary] = None, pos=None, q=None, q_out=None,
+                       slots=None) -> ebd_append_norm_params:
+    """As append_paged_params, the keys normalised by k_norm and the queries by q_norm (None: not).  With slots [tokens]
+    int64 (of ebd_plan_step) the tokens go there: new_off and len are not needed, and a rotation needs pos."""
+    (tokens, _, _), _ = _layout(k_new, "k_new", pgs.kv_heads)
+    if slots is not None and rot is not None and pos is None:
+        raise ValueError("with slots, a rotation needs positions")
+    if slots is None and (new_off is None or len is None):
+        raise ValueError("without slots, new_off and len are needed")
+    a = append_paged_params(pgs, k_new, v_new, new_off, len, rot, pos=pos, q=q, q_out=q_out)
+    p = ebd_append_norm_params()
+    p.append = a
+    if k_norm is not None:
+        p.k_norm = _norm_of(k_norm, pgs.kv_heads, "k_norm")
+    if q_norm is not None:
+        if q is None:
+            raise ValueError("q_norm goes with q")
+        p.q_norm = _norm_of(q_norm, q.shape[1], "q_norm")
+    p.slots = _table(slots, torch.int64, (tokens,), "slots")
+    w = [n.keep for n in (k_norm, q_norm) if n is not None]
+    dev = _here(pgs.pools[0], slots, *w)
+    _plan(p, dev, (a.keep, slots, *w))
+    p.expect, p.seqs = a.expect, a.seqs
+    return p
+
+
 def pages(K, V, page_table) -> ebd_pages:
     """The pools K and V [pages, KV heads, rows per page, 128] (any strides over the first three, the same
     for both) and page_table [sequences, pages per sequence] int32."""
@@ -392,6 +542,35 @@ def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None,
     code = _lib.ebd_gather_paged(ctypes.addressof(p), _arg(params, "K", K), _arg(params, "V", V), ku, vu,
                                  _out(params, "status", status, _I32, params.units), _on_stream(params, stream))
     _check("ebd_gather_paged", code)
+
+
+def ebd_norm_rope(params: ebd_norm_rope_params, x, y, stream=None) -> None:
+    """Normalise and rotate rows x into y (asynchronous)."""
+    code = _lib.ebd_norm_rope(params.at, _arg(params, "x", x), _arg(params, "y", y), _on_stream(params, stream))
+    _check("ebd_norm_rope", code)
+
+
+def ebd_norm_rope_backward(params: ebd_norm_rope_backward_params, x, dy, dx, dweight, workspace, stream=None) -> None:
+    """Gradients dx and dweight (fp32, the weights' shape, contiguous) of ebd_norm_rope (asynchronous)."""
+    if not isinstance(dweight, torch.Tensor):
+        raise TypeError("dweight must be a torch.Tensor")
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
+    code = _lib.ebd_norm_rope_backward(params.at, _arg(params, "x", x), _arg(params, "dy", dy), _arg(params, "dx", dx),
+                                       _out(params, "dweight", dweight, torch.float32, params.weights),
+                                       _out(params, "workspace", workspace, workspace.dtype, None), workspace.nbytes,
+                                       _on_stream(params, stream))
+    _check("ebd_norm_rope_backward", code)
+
+
+def ebd_append_norm(params: ebd_append_norm_params, k_new, v_new, K, V, q=None, q_out=None, status=None,
+                    stream=None) -> None:
+    """Write new tokens into their pages, keys and queries normalised and rotated (asynchronous)."""
+    code = _lib.ebd_append_norm(params.at, _arg(params, "k_new", k_new), _arg(params, "v_new", v_new),
+                                _arg(params, "K", K), _arg(params, "V", V), _arg(params, "q", q),
+                                _arg(params, "q_out", q_out), _out(params, "status", status, _I32, params.seqs),
+                                _on_stream(params, stream))
+    _check("ebd_append_norm", code)
 
 
 # ---- helpers that allocate ---------------------------------------------------------------------
