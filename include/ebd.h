@@ -586,19 +586,73 @@ typedef struct ebd_append_norm_params {
 ebd_status ebd_append_norm(const ebd_append_norm_params *p, const uint16_t *k_new, const uint16_t *v_new, uint16_t *K,
                            uint16_t *V, const uint16_t *q, uint16_t *q_out, uint32_t *status, void *stream);
 
+/*
+ * ebd_plan_step -- what a step's calls on the paged cache need, from the sequences' new token counts: pages for the new
+ * rows, offsets, slots, positions, and the masks of drafted trees.  Nothing of it passes through the host.
+ *   count        [num_seqs] device int32: new tokens of each sequence; negative: the sequence has ended.
+ *   len          [num_seqs] device int32, updated: the rows held before the step, then those with its new tokens.
+ *   page_table   [num_seqs, max_pages] device int32, updated.  An entry of the new rows (from the one that row len lies on)
+ *                that names no page of the pool gets one from the free pages, in the order of the sequences and of their
+ *                rows; one that names a page keeps it (a page left behind by a path that was not kept, say).  An ended
+ *                sequence's entries become -1, its len 0, and its pages free from the next call on.
+ *   free_pages   [num_pages] device int32, a ring of the free pages; free_state [2] device int32: where its first one is
+ *                and how many it holds (both updated; entries that are neither taken from nor given back to stay).  A state
+ *                outside the ring is taken for an empty ring.
+ *   new_off      [num_seqs + 1] device int64, written: first new token of each sequence, as the other calls take it.
+ *   slots        [num_tokens] device int64 or NULL, written: page * page_size + row in it of each new token, -1 where it has
+ *                no page and for padding tokens (from new_off[num_seqs] on).
+ *   pos          [num_tokens] device int32 or NULL, written: the token's position, len before the step + its index among
+ *                its sequence's new tokens (or its depth in the tree); -1 for padding tokens.
+ *   parent       [num_tokens] device int32 or NULL: the new tokens of a sequence are trees; a token's parent as an index
+ *                among its sequence's new tokens, below its own, or -1 (it follows the held rows).
+ *   mask         [num_tokens, mask_words] device uint64 (with parent), written: bit i of word w is set where the token
+ *                follows its sequence's new token 64 w + i or is it; 0 for padding.  mask_words 1 .. 64; a token whose index
+ *                does not fit gets an empty mask and position -1.
+ *   num_tokens   room in slots, pos, parent and mask; new_off goes on past it, but nothing else is written there.
+ *   status       [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when new rows are left without a page (the ring is empty,
+ *                the table too short); EBD_ST_BAD_LAYOUT when new tokens have no room in num_tokens or in the mask, a parent
+ *                is out of place (taken for -1), or the sequence would hold more than 2^30 rows (it gets none, and keeps
+ *                what it has; a negative len counts as 0).
+ * Pages that several sequences share must not be given back by ending one of them.  At most 65536 sequences, 2^24 - 1 tokens.
+ * workspace: ebd_workspace_size(EBD_WS_PLAN_STEP, p) bytes, 256-byte aligned; nothing in it is kept.
+ */
+typedef struct ebd_plan_step_params {
+    int32_t num_seqs;
+    int32_t page_size; /* a power of two, 16 .. 65536 */
+    int32_t num_pages;
+    int32_t max_pages;
+    int64_t num_tokens;
+    const int32_t *count;
+    int32_t *len;
+    int32_t *page_table;
+    int32_t *free_pages;
+    int32_t *free_state;
+    int64_t *new_off;
+    int64_t *slots;
+    int32_t *pos;
+    const int32_t *parent;
+    uint64_t *mask;
+    int32_t mask_words;
+    int32_t reserved; /* 0 */
+} ebd_plan_step_params;
+
+ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *workspace, size_t ws_bytes, void *stream);
+
 /* which-values for ebd_workspace_size */
 #define EBD_WS_EVICT 0
 #define EBD_WS_ATTEND 1
 #define EBD_WS_SCORES 2
 #define EBD_WS_ATTEND_PAGED 3
 #define EBD_WS_NORM_ROPE_BACKWARD 5
+#define EBD_WS_PLAN_STEP 6
 
 /*
  * Workspace bytes needed by ebd_evict (which = EBD_WS_EVICT, params = ebd_evict_params*),
  * ebd_attend_certify (EBD_WS_ATTEND, ebd_attend_params*), ebd_scores (EBD_WS_SCORES,
  * ebd_scores_params*) or ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*),
  * ebd_norm_rope_backward (EBD_WS_NORM_ROPE_BACKWARD,
- * ebd_norm_rope_backward_params*).
+ * ebd_norm_rope_backward_params*),
+ * ebd_plan_step (EBD_WS_PLAN_STEP, ebd_plan_step_params*).
  * Depends only on the host fields of the params.  Returns 0 on invalid arguments.
  */
 size_t ebd_workspace_size(int32_t which, const void *params);
@@ -617,7 +671,8 @@ const char *ebd_version(void);
  * "scores_stats", "scores_accum", "block_contrib", "cert_step", "rope", "append_paged",
  * "attend_paged", "attend_paged_join", "gather_paged",
  * "norm_rope", "norm_rope_backward", "norm_rope_join",
- * "append_norm") to *total_ms and its launch count to
+ * "append_norm",
+ * "plan_step") to *total_ms and its launch count to
  * *launches; it then clears that kernel's record.  The switch is an atomic flag and the records
  * are guarded by a lock, so both calls may come from any host thread; while timing is off no
  * event is created and launches take no lock.

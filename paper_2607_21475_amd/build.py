@@ -21,7 +21,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libebd.so")
 
 SOURCES = ["evict.hip", "evict_long.hip", "attend.hip", "append.hip", "scores.hip", "finegrain.hip", "noalloc.hip",
-           "rope.hip", "norm_rope.hip", "gather_paged.hip", "attend_paged.hip",
+           "rope.hip", "norm_rope.hip", "plan_step.hip", "gather_paged.hip", "attend_paged.hip",
            "attend_paged_tiles.hip", "ebd_api.cpp", "paged_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -206,6 +206,14 @@ struct AppendNormLaunch {
   int32_t per, tpb;
 };
 
+struct PlanStepLaunch {
+  ebd_plan_step_params p;
+  uint32_t *status;
+  int2 *state;   // the ring's head and count before the step
+  int4 *info;    // [num_seqs] new tokens (-1: ended), rows held before, pages needed, pages given back
+  int32_t shift;
+};
+
 struct GatherPagedLaunch {
   ebd_gather_paged_params p;
   const uint16_t *K, *V;
@@ -288,6 +296,9 @@ size_t norm_rope_backward_workspace(const ebd_norm_rope_backward_params *p);  //
 hipError_t launch_norm_rope_backward(const NormRopeBackwardLaunch &L, hipStream_t s);
 hipError_t launch_norm_rope_join(const NormRopeBackwardLaunch &L, hipStream_t s);
 hipError_t launch_append_norm(AppendNormLaunch L, hipStream_t s);
+size_t plan_step_bytes(const ebd_plan_step_params &p);
+size_t plan_step_workspace(const ebd_plan_step_params *p);  // 0: invalid parameters
+hipError_t launch_plan_step(const PlanStepLaunch &L, hipStream_t s);
 int64_t gather_paged_groups(const ebd_gather_paged_params &p);
 hipError_t launch_gather_paged(GatherPagedLaunch L, hipStream_t s);
 int64_t attend_paged_groups(const AttendPagedLaunch &L);

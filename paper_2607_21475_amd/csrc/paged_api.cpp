@@ -54,6 +54,21 @@ bool valid_rotary(const ebd_rotary &R) {
 
 float amplitude_of(const ebd_rotary &R) { return R.amplitude != 0.0f ? R.amplitude : 1.0f; }
 
+constexpr int32_t kPlanSeqs = 65536;
+constexpr int32_t kMaskWords = 64;
+
+bool valid_plan_step(const ebd_plan_step_params *p) {
+  if (!p || p->num_seqs < 0 || p->num_pages < 1 || p->max_pages < 1 || p->page_size < 1 || p->num_tokens < 0) return false;
+  if (p->reserved != 0 || (p->parent != nullptr) != (p->mask != nullptr)) return false;
+  if (((uintptr_t)p->new_off & 7) || ((uintptr_t)p->slots & 7) || ((uintptr_t)p->mask & 7)) return false;
+  return !p->mask || (p->mask_words >= 1 && p->mask_words <= kMaskWords);
+}
+bool supported_plan_step(const ebd_plan_step_params *p) {
+  return p->page_size >= 16 && p->page_size <= 65536 && (p->page_size & (p->page_size - 1)) == 0 &&
+         p->num_seqs <= kPlanSeqs && p->num_tokens <= kGridMax && p->num_pages <= kRowsMax && p->max_pages <= kRowsMax;
+}
+size_t plan_bytes(const ebd_plan_step_params &p) { return (plan_step_bytes(p) + 255) / 256 * 256; }
+
 bool valid_norm(const ebd_norm &N) {
   if (((uintptr_t)N.weight & 15) || N.head_stride % 4 || N.head_stride >= kStrideMax || N.reserved != 0) return false;
   return (N.head_stride == 0 || N.head_stride >= kHeadDim) && std::isnormal(N.eps) && N.eps > 0.0f;
@@ -216,6 +231,10 @@ namespace ebd {
 size_t attend_paged_workspace(const ebd_attend_paged_params *p) {
   if (!valid_attend_paged(p) || !supported_attend_paged(p)) return 0;
   return plan_bytes(attend_paged_plan(p));
+}
+
+size_t plan_step_workspace(const ebd_plan_step_params *p) {
+  return valid_plan_step(p) && supported_plan_step(p) ? plan_bytes(*p) : 0;
 }
 
 size_t norm_rope_backward_workspace(const ebd_norm_rope_backward_params *p) {
@@ -414,6 +433,24 @@ ebd_status ebd_append_norm(const ebd_append_norm_params *n, const uint16_t *k_ne
   L.shift = log2_of(p->pages.page_size);
   hipStream_t s = static_cast<hipStream_t>(stream);
   return timed_launch("append_norm", s, [&] { return launch_append_norm(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
+}
+
+ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *workspace, size_t ws_bytes, void *stream) {
+  if (!valid_plan_step(p)) return EBD_ERR_INVALID_ARG;
+  if (!supported_plan_step(p)) return EBD_ERR_UNSUPPORTED;
+  if (p->num_seqs == 0) return EBD_OK;
+  if (!p->count || !p->len || !p->page_table || !p->free_pages || !p->free_state || !p->new_off) return EBD_ERR_INVALID_ARG;
+  if (!workspace || ws_bytes < plan_bytes(*p) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  PlanStepLaunch L{};
+  L.p = *p;
+  L.status = status;
+  L.state = static_cast<int2 *>(workspace);
+  L.info = reinterpret_cast<int4 *>(static_cast<char *>(workspace) + 256);
+  L.shift = log2_of(p->page_size);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("plan_step", s, [&] { return launch_plan_step(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
 }
 
 }  // extern "C"

@@ -6,6 +6,7 @@
     ebd_gather_paged    the pages read out as units, which ebd_scores and ebd_evict take
     ebd_norm_rope       norms of heads and rotary positions in one pass; ebd_norm_rope_backward: their gradients
     ebd_append_norm     ebd_append_paged for models that normalise queries and keys for each head
+    ebd_plan_step       page tables, slots, positions and tree masks of a step, from the new token counts
 
 Each call takes a parameter struct (`rope_params`, `append_paged_params`, ...) that a program makes once
 per plan and keeps: it holds the tables' addresses and the rows' strides.  A struct keeps the tensors
@@ -15,6 +16,7 @@ frequencies of the usual rotary positions.
 """
 from __future__ import annotations
 
+import builtins
 import ctypes
 import math
 from dataclasses import dataclass
@@ -165,6 +167,28 @@ class ebd_append_norm_params(ctypes.Structure):
     ]
 
 
+class ebd_plan_step_params(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("num_tokens", ctypes.c_int64),
+        ("count", ctypes.c_void_p),
+        ("len", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+        ("free_pages", ctypes.c_void_p),
+        ("free_state", ctypes.c_void_p),
+        ("new_off", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+        ("pos", ctypes.c_void_p),
+        ("parent", ctypes.c_void_p),
+        ("mask", ctypes.c_void_p),
+        ("mask_words", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 _lib.ebd_rope.argtypes = [_P] * 4
 _lib.ebd_rope.restype = ctypes.c_int
 _lib.ebd_append_paged.argtypes = [_P] * 9
@@ -179,6 +203,8 @@ _lib.ebd_norm_rope_backward.argtypes = [_P] * 6 + [ctypes.c_size_t, _P]
 _lib.ebd_norm_rope_backward.restype = ctypes.c_int
 _lib.ebd_append_norm.argtypes = [_P] * 9
 _lib.ebd_append_norm.restype = ctypes.c_int
+_lib.ebd_plan_step.argtypes = [_P] * 3 + [ctypes.c_size_t, _P]
+_lib.ebd_plan_step.restype = ctypes.c_int
 
 
 # ---- tensors -> parameters ---------------------------------------------------------------------
@@ -500,6 +526,41 @@ def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_pa
     return _plan(p, _here(K, V, pgs.keep, seq_off), (pgs.keep, seq_off), K=K, V=V)
 
 
+def plan_step_params(count, len, page_table, page_size: int, free_pages, free_state, new_off, slots=None, pos=None,
+                     parent=None, mask=None) -> ebd_plan_step_params:
+    """New tokens count [sequences] int32 (negative: ended) of sequences that hold len [sequences] int32 rows in the pages
+    page_table [sequences, pages per sequence] int32; free_pages [pages of the pool] int32, a ring, and free_state [2] int32.
+    Written: new_off [sequences + 1] int64, slots [tokens] int64, pos [tokens] int32; with the trees parent [tokens] int32
+    also mask [tokens, words] int64.  len, page_table, free_pages and free_state are updated."""
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be [sequences, pages per sequence]")
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1 or free_pages.numel() < 1:
+        raise ValueError("free_pages must be [pages of the pool]")
+    if (parent is None) != (mask is None):
+        raise ValueError("parent and mask go together")
+    S = page_table.shape[0]
+    room = {t.shape[0] for t in (slots, pos, parent, mask) if isinstance(t, torch.Tensor) and t.dim()}
+    if builtins.len(room) > 1:
+        raise ValueError("slots, pos, parent and mask must have the same number of tokens")
+    p = ebd_plan_step_params()
+    p.num_seqs, p.max_pages = page_table.shape
+    p.page_size, p.num_pages, p.num_tokens = int(page_size), free_pages.numel(), room.pop() if room else 0
+    T = (p.num_tokens,)
+    p.count, p.len = _table(count, _I32, (S,), "count"), _table(len, _I32, (S,), "len")
+    p.page_table = _table(page_table, _I32, page_table.shape, "page_table")
+    p.free_pages = _table(free_pages, _I32, free_pages.shape, "free_pages")
+    p.free_state, p.new_off = _table(free_state, _I32, (2,), "free_state"), _table(new_off, torch.int64, (S + 1,), "new_off")
+    p.slots, p.pos = _table(slots, torch.int64, T, "slots"), _table(pos, _I32, T, "pos")
+    if mask is not None:
+        if not isinstance(mask, torch.Tensor) or mask.dim() != 2:
+            raise ValueError("mask must be [tokens, words]")
+        p.parent, p.mask = _table(parent, _I32, T, "parent"), _table(mask, torch.int64, mask.shape, "mask")
+        p.mask_words = mask.shape[1]
+    p.seqs = (S,)
+    held = (count, len, page_table, free_pages, free_state, new_off, slots, pos, parent, mask)
+    return _plan(p, _here(*held), held)
+
+
 # ---- the calls ---------------------------------------------------------------------------------
 
 def ebd_rope(params: ebd_rope_params, x, y, stream=None) -> None:
@@ -571,6 +632,16 @@ def ebd_append_norm(params: ebd_append_norm_params, k_new, v_new, K, V, q=None, 
                                 _arg(params, "q_out", q_out), _out(params, "status", status, _I32, params.seqs),
                                 _on_stream(params, stream))
     _check("ebd_append_norm", code)
+
+
+def ebd_plan_step(params: ebd_plan_step_params, workspace, status=None, stream=None) -> None:
+    """Pages, offsets, slots, positions and masks of a step (asynchronous)."""
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
+    code = _lib.ebd_plan_step(params.at, _out(params, "status", status, _I32, params.seqs),
+                              _out(params, "workspace", workspace, workspace.dtype, None), workspace.nbytes,
+                              _on_stream(params, stream))
+    _check("ebd_plan_step", code)
 
 
 # ---- helpers that allocate ---------------------------------------------------------------------

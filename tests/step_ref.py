@@ -67,3 +67,92 @@ def norm_rope_gradients(x, w, eps, dy, pos, freq, amp=1.0, layout=0, inverse=Fal
 def frequencies(rot, base=5e5, dev="cuda"):
     i = torch.arange(rot // 2, dtype=torch.float64, device=dev)
     return base ** (-2.0 * i / rot)
+
+
+# ---- plans -------------------------------------------------------------------------------------
+
+BAD_LAYOUT, BAD_PAGE = 16, 32
+
+
+def plan(count, lens, table, page, ring, state, room, parent=None, words=0):
+    """What ebd_plan_step makes of these (lists; the table a list of rows): a dict of lists, by the definition."""
+    N, P = len(ring), len(table[0]) if table else 0
+    lens, table, ring = list(lens), [list(r) for r in table], list(ring)
+    head, free = state
+    if not (0 <= head < N and 0 <= free <= N):
+        head = free = 0
+    known = lambda pg: 0 <= pg < N  # noqa: E731
+    taken = back = 0
+    off, slots, pos, masks, status = [0], [], [], [], [0] * len(count)
+    for s, n in enumerate(count):
+        first = max(lens[s], 0)
+        if n < 0:
+            for pg in table[s]:
+                if known(pg):
+                    if free + back < N:
+                        ring[(head + free + back) % N] = pg
+                    back += 1
+            table[s] = [-1] * P
+            lens[s] = 0
+            off.append(off[-1])
+            continue
+        if n > 0 and first + n > 2 ** 30:
+            n, status[s] = 0, BAD_LAYOUT
+        if n > 0:
+            for e in range(first // page, (first + n - 1) // page + 1):
+                if e >= P:
+                    status[s] |= BAD_PAGE
+                    break
+                if known(table[s][e]):
+                    continue
+                if taken < free:
+                    table[s][e] = ring[(head + taken) % N]
+                else:
+                    status[s] |= BAD_PAGE
+                taken += 1
+            lens[s] = first + n
+        off.append(off[-1] + n)
+        bits, depth = [], []
+        for j in range(min(n, room - off[-2]) if n else 0):
+            if j < 0:
+                break
+            row = first + j
+            pg = table[s][row // page] if row // page < P else -1
+            slots.append(pg * page + row % page if known(pg) else -1)
+            if parent is None:
+                pos.append(row)
+                continue
+            if j >= 64 * words:
+                status[s] |= BAD_LAYOUT
+                pos.append(-1)
+                masks.append([0] * words)
+                continue
+            up = parent[off[-2] + j]
+            if not -1 <= up < j:
+                up = -1
+                status[s] |= BAD_LAYOUT
+            depth.append(0 if up < 0 else depth[up] + 1)
+            bits.append((bits[up] if up >= 0 else 0) | 1 << j)
+            pos.append(first + depth[j])
+            masks.append([signed(bits[j] >> (64 * w) & (2 ** 64 - 1)) for w in range(words)])
+        if n > 0 and off[-1] > room:
+            status[s] |= BAD_LAYOUT
+    pad = room - len(slots)
+    got = min(taken, free)
+    return {"len": lens, "table": table, "ring": ring, "state": [(head + got) % N, min(free - got + back, N)], "new_off": off,
+            "slots": slots + [-1] * pad, "pos": pos + [-1] * pad, "mask": masks + [[0] * words for _ in range(pad)],
+            "status": status}
+
+
+def signed(word):
+    return word - 2 ** 64 if word >> 63 else word
+
+
+def tree(n, rng):
+    """Parents of a tree of n drafted tokens."""
+    return [rng.randrange(j + 1) - 1 for j in range(n)]
+
+
+def chains(n, width):
+    """... of `width` chains side by side."""
+    return [j - width if j >= width else -1 for j in range(n)]

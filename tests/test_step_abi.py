@@ -129,3 +129,42 @@ def test_norms_of_the_binding():
         ebd.head_norm(torch.zeros(128))
     with pytest.raises(TypeError, match="head_norm"):
         ebd.norm_rope_params(x, x, None)
+
+
+def _plan(ws=FAKE, ws_bytes=1 << 40, **kw):
+    p = paged.ebd_plan_step_params()
+    _with(p, num_seqs=3, page_size=16, num_pages=40, max_pages=8, num_tokens=20, count=FAKE, len=FAKE, page_table=FAKE,
+          free_pages=FAKE, free_state=FAKE, new_off=FAKE, slots=FAKE, pos=FAKE, parent=FAKE, mask=FAKE, mask_words=1)
+    _with(p, **kw)
+    size = LIB.ebd_workspace_size(ebd.EBD_WS_PLAN_STEP, ctypes.byref(p))
+    return LIB.ebd_plan_step(ctypes.byref(p), None, ws, ws_bytes, None), size
+
+
+def test_plan_refusals():
+    assert LIB.ebd_plan_step(None, None, FAKE, 1 << 40, None) == BAD
+    for kw in (dict(num_seqs=-1), dict(num_pages=0), dict(max_pages=0), dict(page_size=0), dict(num_tokens=-1),
+               dict(reserved=1), dict(parent=None), dict(mask=None), dict(mask_words=0), dict(mask_words=65),
+               dict(new_off=FAKE + 4), dict(slots=FAKE + 4), dict(mask=FAKE + 4)):
+        assert _plan(**kw) == (BAD, 0), kw
+    for kw in (dict(count=None), dict(len=None), dict(page_table=None), dict(free_pages=None), dict(free_state=None),
+               dict(new_off=None)):
+        assert _plan(**kw)[0] == BAD, kw
+    for kw in (dict(page_size=8), dict(page_size=48), dict(page_size=1 << 17), dict(num_seqs=65537),
+               dict(num_tokens=1 << 24), dict(num_pages=(1 << 30) + 1), dict(max_pages=(1 << 30) + 1)):
+        assert _plan(**kw) == (UNSUPPORTED, 0), kw
+    need = _plan()[1]
+    assert _plan(ws=None)[0] == NO_WS and _plan(ws=FAKE + 8)[0] == NO_WS and _plan(ws_bytes=need - 1)[0] == NO_WS
+    assert _plan(num_seqs=0)[0] == OK
+
+
+def test_plans_of_the_binding():
+    i32 = torch.int32
+    z = lambda *shape, dtype=i32: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    args = dict(count=z(2), len=z(2), page_table=z(2, 4), page_size=16, free_pages=z(9), free_state=z(2),
+                new_off=z(3, dtype=torch.int64))
+    for kw, what in ((dict(page_table=z(8)), "page_table"), (dict(free_pages=z(0)), "free_pages"),
+                     (dict(parent=z(5)), "go together"), (dict(mask=z(5, 1, dtype=torch.int64)), "go together"),
+                     (dict(slots=z(4, dtype=torch.int64), pos=z(5)), "same number"),
+                     (dict(), "CUDA|GPU|cuda|device")):
+        with pytest.raises((ValueError, TypeError), match=what):
+            ebd.plan_step_params(**{**args, **kw})
