@@ -638,6 +638,29 @@ typedef struct ebd_plan_step_params {
 
 ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *workspace, size_t ws_bytes, void *stream);
 
+/*
+ * ebd_attend_tree -- ebd_attend_paged for new tokens that see each other by a mask (a tree of drafted tokens, or any other
+ * pattern) instead of in order.  Token j of sequence s (index t = new_off[s] + j) sees, of the rows held before the step
+ * (first = len[s] - (new_off[s+1] - new_off[s]) of them), those from lo on, and the new token i (row first + i) where
+ * bit i % 64 of mask[t * mask_words + i / 64] is set:
+ *     lo = max(0, qpos[t] - window + 1) (qpos NULL: first + j stands for it), or 0 when window is 0
+ *   mask        [num_tokens, mask_words] device uint64; new tokens past 64 * mask_words are seen by none.
+ *   mask_words  1 .. 64.
+ *   attend.qpos positions of the tokens, or NULL; a token with a negative position sees nothing, whatever its mask.  The window
+ *               does not apply to new tokens, which the mask alone chooses.
+ * Everything else is as for ebd_attend_paged (outputs, bounds, status, rounding of weights, values that are not finite).
+ * workspace: ebd_workspace_size(EBD_WS_ATTEND_TREE, p) bytes, 256-byte aligned.
+ */
+typedef struct ebd_attend_tree_params {
+    ebd_attend_paged_params attend;
+    const uint64_t *mask;
+    int32_t mask_words;
+    int32_t reserved; /* 0 */
+} ebd_attend_tree_params;
+
+ebd_status ebd_attend_tree(const ebd_attend_tree_params *p, const uint16_t *q, const uint16_t *K, const uint16_t *V,
+                           uint16_t *y, float *lse, uint32_t *status, void *workspace, size_t ws_bytes, void *stream);
+
 /* which-values for ebd_workspace_size */
 #define EBD_WS_EVICT 0
 #define EBD_WS_ATTEND 1
@@ -645,6 +668,7 @@ ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *
 #define EBD_WS_ATTEND_PAGED 3
 #define EBD_WS_NORM_ROPE_BACKWARD 5
 #define EBD_WS_PLAN_STEP 6
+#define EBD_WS_ATTEND_TREE 4
 
 /*
  * Workspace bytes needed by ebd_evict (which = EBD_WS_EVICT, params = ebd_evict_params*),
@@ -652,7 +676,8 @@ ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *
  * ebd_scores_params*) or ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*),
  * ebd_norm_rope_backward (EBD_WS_NORM_ROPE_BACKWARD,
  * ebd_norm_rope_backward_params*),
- * ebd_plan_step (EBD_WS_PLAN_STEP, ebd_plan_step_params*).
+ * ebd_plan_step (EBD_WS_PLAN_STEP, ebd_plan_step_params*),
+ * ebd_attend_tree (EBD_WS_ATTEND_TREE, ebd_attend_tree_params*).
  * Depends only on the host fields of the params.  Returns 0 on invalid arguments.
  */
 size_t ebd_workspace_size(int32_t which, const void *params);
@@ -672,7 +697,8 @@ const char *ebd_version(void);
  * "attend_paged", "attend_paged_join", "gather_paged",
  * "norm_rope", "norm_rope_backward", "norm_rope_join",
  * "append_norm",
- * "plan_step") to *total_ms and its launch count to
+ * "plan_step",
+ * "attend_tree", "attend_tree_join") to *total_ms and its launch count to
  * *launches; it then clears that kernel's record.  The switch is an atomic flag and the records
  * are guarded by a lock, so both calls may come from any host thread; while timing is off no
  * event is created and launches take no lock.

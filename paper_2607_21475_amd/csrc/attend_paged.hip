@@ -41,7 +41,8 @@ __device__ __forceinline__ float max_xor16_32(float x) {
 
 }  // namespace
 
-template <int NQ, bool NT>
+// TREE: the new tokens see each other by a mask.
+template <int NQ, bool NT, bool TREE>
 __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L) {
   constexpr int kRows = 16 * NQ;
   constexpr int kMerge = kRows * (kMergeRow * 4 + 8);  // a wave's sums and statistics, when the waves combine
@@ -63,13 +64,16 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
 
   Span span[NQ];
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) span[b] = span_of(L, sq, 16 * b + c);
+  for (int b = 0; b < NQ; ++b) span[b] = TREE ? tree_span_of(L, sq, 16 * b + c) : span_of(L, sq, 16 * b + c);
   if (sq.held > sq.seen && L.status && sp == 0 && wave == 0) {
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
-      if (__any(past_table(L, sq, 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+      if (__any(TREE ? tree_past_table(L, sq, 16 * b + c) : past_table(L, sq, 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   }
-  const Range R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, 0, token(nrow - 1));
+  Range R = TREE || p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, 0, token(nrow - 1));
+  if constexpr (TREE) R.every_hi = (int)min((int64_t)R.every_hi, max((int64_t)0, sq.first));
+  // whether this lane's row of a block sees a key inside its span
+  auto masked = [&](int b, int k) { return mask_bits(L, sq, sq.t0 + token(min(16 * b + c, nrow - 1)), k); };
   const Keys split = split_of(L, R.lo, R.hi, kTileKeys, sp);
   const int k_beg = split.beg, k_end = split.end;  // (below 2^30: no sum below overflows)
 
@@ -141,9 +145,12 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     const uint32_t what = poison_of(v0) | poison_of(v1) << 8;
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
+      uint32_t bit = 1u;
+      if constexpr (TREE) bit = masked(b, key) & 1u;
 #pragma unroll 1
       for (int j = 0; j < 16; ++j) {
-        const bool sees = (key >= __shfl(span[b].lo, j)) & (key < __shfl(span[b].hi, j));
+        bool sees = (key >= __shfl(span[b].lo, j)) & (key < __shfl(span[b].hi, j));
+        if constexpr (TREE) sees &= __shfl(bit, j) != 0u;
         if (sees) reinterpret_cast<uint16_t *>(poison)[(16 * b + j) * 64 + lane] |= (uint16_t)what;
       }
     }
@@ -254,6 +261,11 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
       if (mixed) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[b][i] = visible(i) ? w[b][i] : -INFINITY;
+        if (TREE && k + kTileKeys > R.every_hi) {
+          const uint32_t bits = masked(b, k) >> (4 * g);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[b][i] = (bits >> (16 * (i / 4) + i % 4)) & 1u ? w[b][i] : -INFINITY;
+        }
       }
       float t = fmaxf(fmaxf(fmaxf(w[b][0], w[b][1]), fmaxf(w[b][2], w[b][3])),
                       fmaxf(fmaxf(w[b][4], w[b][5]), fmaxf(w[b][6], w[b][7])));
@@ -289,7 +301,14 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
 #pragma unroll
       for (int i = 0; i < 2 * NQ; ++i) {
         const int at = k + 16 * (i / NQ);
-        if ((bad >> (i / NQ)) & 1u) gone |= __any((span[i % NQ].lo < at + 16) & (span[i % NQ].hi > at));
+        if constexpr (TREE) {
+          const int row = 16 * (i % NQ) + c;
+          if ((bad >> (i / NQ)) & 1u)
+            gone |= __any(span[i % NQ].lo < span[i % NQ].hi &&
+                          sees_any(L, sq, sq.t0 + token(row), span[i % NQ].lo, at, min(at + 16, span[i % NQ].hi)));
+        } else if ((bad >> (i / NQ)) & 1u) {
+          gone |= __any((span[i % NQ].lo < at + 16) & (span[i % NQ].hi > at));
+        }
       }
     }
     bad = next_bad;
@@ -460,14 +479,21 @@ int64_t attend_paged_join_groups(const AttendPagedLaunch &L) {
   return L.nsplit > 1 ? L.units * L.p.pages.kv_heads * (L.rows / 4) : 0;
 }
 
+namespace {
+template <bool TREE>
+hipError_t launch_rows(const AttendPagedLaunch &L, hipStream_t s) {
+  const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
+  if (L.rows == 16 && L.once) hipLaunchKernelGGL((attend_rows_kernel<1, true, TREE>), grid, block, 0, s, L);
+  else if (L.rows == 16) hipLaunchKernelGGL((attend_rows_kernel<1, false, TREE>), grid, block, 0, s, L);
+  else if (L.once) hipLaunchKernelGGL((attend_rows_kernel<2, true, TREE>), grid, block, 0, s, L);
+  else hipLaunchKernelGGL((attend_rows_kernel<2, false, TREE>), grid, block, 0, s, L);
+  return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s) {
   if (L.rows > kRowsKernelMax) return launch_attend_tiles(L, s);
-  const dim3 grid((unsigned)attend_paged_groups(L)), block(64 * kRowsWaves);
-  if (L.rows == 16 && L.once) hipLaunchKernelGGL((attend_rows_kernel<1, true>), grid, block, 0, s, L);
-  else if (L.rows == 16) hipLaunchKernelGGL((attend_rows_kernel<1, false>), grid, block, 0, s, L);
-  else if (L.once) hipLaunchKernelGGL((attend_rows_kernel<2, true>), grid, block, 0, s, L);
-  else hipLaunchKernelGGL((attend_rows_kernel<2, false>), grid, block, 0, s, L);
-  return hipGetLastError();
+  return L.mask ? launch_rows<true>(L, s) : launch_rows<false>(L, s);
 }
 
 hipError_t launch_attend_paged_join(const AttendPagedLaunch &L, hipStream_t s) {

@@ -140,6 +140,44 @@ __device__ __forceinline__ Keys split_of(const AttendPagedLaunch &L, int lo, int
 struct Span {
   int lo, hi;
 };
+
+// Under a mask (TREE) a row of span lo .. hi - 1 sees, of those, the rows held before the step, and the new tokens' rows
+// (from sq.first on) whose bit is set in its token's mask.
+
+// Bits of the rows k .. k + 31: set for held ones, and as token t's mask says for new ones.
+__device__ __forceinline__ uint32_t mask_bits(const AttendPagedLaunch &L, const Seq &q, int64_t t, int k) {
+  const int64_t d = k - q.first;
+  if (d + 32 <= 0) return ~0u;
+  const uint64_t *m = L.mask + t * L.mask_words;
+  if (d < 0) return (uint32_t)m[0] << (int)-d | ((1u << (int)-d) - 1u);
+  const int i = (int)min(d >> 6, (int64_t)L.mask_words), s = (int)(d & 63);
+  uint64_t w = i < L.mask_words ? m[i] >> s : 0;
+  if (s > 32 && i + 1 < L.mask_words) w |= m[i + 1] << (64 - s);
+  return (uint32_t)w;
+}
+
+// Whether a row of token t sees any of the rows a .. b - 1; lo: the first of the held rows that it sees.
+__device__ __forceinline__ bool sees_any(const AttendPagedLaunch &L, const Seq &q, int64_t t, int64_t lo, int64_t a, int64_t b) {
+  if (max(a, lo) < min(b, q.first)) return true;
+  const int64_t x = max(a - q.first, (int64_t)0), y = min(b - q.first, (int64_t)64 * L.mask_words);
+  for (int64_t i = x >> 6; i << 6 < y; ++i) {
+    uint64_t w = L.mask[t * L.mask_words + i];
+    if (i == x >> 6) w &= ~0ull << (x & 63);
+    if (y - (i << 6) < 64) w &= (1ull << (y - (i << 6))) - 1;
+    if (w) return true;
+  }
+  return false;
+}
+
+__device__ __forceinline__ Span tree_span_of(const AttendPagedLaunch &L, const Seq &q, int row) {
+  const ebd_attend_paged_params &p = L.p;
+  const int j = L.by_group.quotient(row);
+  if (j >= q.tokens) return {0, 0};
+  const int64_t pos = p.qpos ? (int64_t)p.qpos[q.t0 + j] : q.first + j;
+  if (pos < 0) return {0, 0};
+  const int64_t lo = p.window > 0 ? min(max((int64_t)0, pos - p.window + 1), max((int64_t)0, q.first)) : 0;
+  return lo < q.seen ? Span{(int)lo, (int)q.seen} : Span{0, 0};
+}
 __device__ __forceinline__ Span span_of(const AttendPagedLaunch &L, const Seq &q, int row) {
   const ebd_attend_paged_params &p = L.p;
   const int j = L.by_group.quotient(row);
@@ -160,6 +198,14 @@ __device__ __forceinline__ bool past_table(const AttendPagedLaunch &L, const Seq
   if (p.qpos) last = min((int64_t)p.qpos[q.t0 + j], q.len - 1);
   const int64_t lo = p.window > 0 ? last - p.window + 1 : 0;
   return min(last + 1, q.held) > max(lo, q.seen);
+}
+
+__device__ __forceinline__ bool tree_past_table(const AttendPagedLaunch &L, const Seq &q, int row) {
+  const ebd_attend_paged_params &p = L.p;
+  const int j = L.by_group.quotient(row);
+  if (j >= q.tokens) return false;
+  const int64_t pos = p.qpos ? (int64_t)p.qpos[q.t0 + j] : q.first + j;
+  return pos >= 0 && sees_any(L, q, q.t0 + j, p.window > 0 ? pos - p.window + 1 : 0, q.seen, q.held);
 }
 
 // The range a block of query rows sees (the same in every lane of a wave that holds them all), and

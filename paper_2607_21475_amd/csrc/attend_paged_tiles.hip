@@ -80,8 +80,9 @@ __device__ __forceinline__ float max_halves(float x) {
 
 }  // namespace
 
-// RW waves of 32 query rows each, KG groups of them that take every KG'th tile of KEYS keys.
-template <int RW, int KG, int KEYS, bool NT>
+// RW waves of 32 query rows each, KG groups of them that take every KG'th tile of KEYS keys.  TREE: the new tokens see each
+// other by a mask.
+template <int RW, int KG, int KEYS, bool NT, bool TREE>
 __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
   constexpr int kWaves = RW * KG, kRows = 32 * RW;
   constexpr int kSub = KEYS / 32;             // blocks of 32 keys of a tile
@@ -123,15 +124,16 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
 
   // what this wave's rows see, and the work-group's
   const int row = row0 + 32 * rw + c;
-  Span span[1] = {span_of(L, sq, row)};
+  Span span[1] = {TREE ? tree_span_of(L, sq, row) : span_of(L, sq, row)};
   const bool sees = span[0].lo < span[0].hi;
-  if (sq.held > sq.seen && __any(past_table(L, sq, row)) && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  if (sq.held > sq.seen && __any(TREE ? tree_past_table(L, sq, row) : past_table(L, sq, row)) && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   Range R, all;
-  if (!p.qpos) {
+  if (!TREE && !p.qpos) {
     R = range_of_tokens(p, sq, token(row0 + 32 * rw), token(row0 + 32 * rw + 31));
     all = range_of_tokens(p, sq, token(row0), token(row0 + nrow - 1));
   } else {
     R = range_of<1>(span);
+    if constexpr (TREE) R.every_hi = (int)min((int64_t)R.every_hi, max((int64_t)0, sq.first));
     if (lane == 0) ranges[wave] = R;
     __syncthreads();
     all = ranges[0];
@@ -191,6 +193,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const uint32_t tiles_at = lds_at(tiles);
   auto tile_of = [&](int stage) { return tiles_at + stage * kStage + kg * 2 * kTile; };  // this group's
   const int own_hi = min(span[0].hi, k_end);
+  // of a lane's row: whether it sees the keys k .. k + 31 inside its span
+  auto masked = [&](int k) { return mask_bits(L, sq, sq.t0 + token(min(row, row0 + nrow - 1)), k); };
   uint32_t(*poison)[8] = poisons[wave];
   bool poisoned = false;
   f32x16 S[kSub];
@@ -231,6 +235,11 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
           const int key = k + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
           const bool ok = (key >= span[0].lo) & (key < own_hi) & !((bad >> (2 * b + i / 8)) & 1u);
           S[b][i] = ok ? S[b][i] : -INFINITY;
+        }
+        if (TREE && k + KEYS > R.every_hi) {
+          const uint32_t bits = masked(k + 32 * b) >> (4 * half);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) S[b][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? S[b][i] : -INFINITY;
         }
       }
     }
@@ -315,9 +324,12 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   };
   auto keep_note = [&](int key, uint32_t note) {  // 16 bits in each of the first 16 lanes
     if (!__any(note)) return;
+    uint32_t bit = 1u;
+    if constexpr (TREE) bit = masked(key) & 1u;
 #pragma unroll 1
     for (int j = 0; j < 32; ++j) {
-      const bool hit = (key >= __shfl(span[0].lo, j)) & (key < __shfl(own_hi, j));
+      bool hit = (key >= __shfl(span[0].lo, j)) & (key < __shfl(own_hi, j));
+      if constexpr (TREE) hit &= __shfl(bit, j) != 0u;
       if (hit && note) atomicOr(&poison[j][lane >> 1], note << (16 * (lane & 1)));
     }
   };
@@ -372,8 +384,13 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
 #pragma unroll 1
       for (int e = max(k_beg, R.lo) >> L.shift; (e << L.shift) < min(k_end, R.hi); ++e) {
         const int at = e << L.shift;
-        if ((uint32_t)table[e] >= (uint32_t)p.pages.num_pages)
-          gone |= __any((max(span[0].lo, k_beg) < at + p.pages.page_size) & (own_hi > at));
+        if ((uint32_t)table[e] >= (uint32_t)p.pages.num_pages) {
+          if constexpr (TREE)
+            gone |= __any(sees && sees_any(L, sq, sq.t0 + token(row), span[0].lo, max(at, k_beg),
+                                           min((int64_t)at + p.pages.page_size, (int64_t)own_hi)));
+          else
+            gone |= __any((max(span[0].lo, k_beg) < at + p.pages.page_size) & (own_hi > at));
+        }
       }
       if (gone && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
     }
@@ -529,13 +546,20 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   }
 }
 
-hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {
+namespace {
+template <bool TREE>
+hipError_t launch_tiles(const AttendPagedLaunch &L, hipStream_t s) {
   const dim3 grid((unsigned)attend_paged_groups(L));
-  if (L.rows == kFewRows && L.once) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, true>), grid, dim3(512), 0, s, L);
-  else if (L.rows == kFewRows) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, false>), grid, dim3(512), 0, s, L);
-  else if (L.rows == kTileRows) hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64, false>), grid, dim3(256), 0, s, L);
-  else hipLaunchKernelGGL((attend_tiles_kernel<8, 1, 64, false>), grid, dim3(512), 0, s, L);
+  if (L.rows == kFewRows && L.once) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, true, TREE>), grid, dim3(512), 0, s, L);
+  else if (L.rows == kFewRows) hipLaunchKernelGGL((attend_tiles_kernel<2, 4, 32, false, TREE>), grid, dim3(512), 0, s, L);
+  else if (L.rows == kTileRows) hipLaunchKernelGGL((attend_tiles_kernel<4, 1, 64, false, TREE>), grid, dim3(256), 0, s, L);
+  else hipLaunchKernelGGL((attend_tiles_kernel<8, 1, 64, false, TREE>), grid, dim3(512), 0, s, L);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {
+  return L.mask ? launch_tiles<true>(L, s) : launch_tiles<false>(L, s);
 }
 
 }  // namespace ebd

@@ -438,6 +438,7 @@ size_t ebd_workspace_size(int32_t which, const void *params) {
   }
   if (which == EBD_WS_ATTEND_PAGED)
     return attend_paged_workspace(static_cast<const ebd_attend_paged_params *>(params));
+  if (which == EBD_WS_ATTEND_TREE) return attend_tree_workspace(static_cast<const ebd_attend_tree_params *>(params));
   if (which == EBD_WS_PLAN_STEP) return plan_step_workspace(static_cast<const ebd_plan_step_params *>(params));
   if (which == EBD_WS_NORM_ROPE_BACKWARD)
     return norm_rope_backward_workspace(static_cast<const ebd_norm_rope_backward_params *>(params));

@@ -255,6 +255,8 @@ struct AttendPagedLaunch {
   int32_t once;        // keys and values are read once, and more of them than caches hold: non-temporal loads
   float *part;         // [groups, rows, 128] sums of the splits, then
   float2 *stats;       // [groups, rows] their maximum and total weight
+  const uint64_t *mask;  // [tokens, mask_words] which new tokens a token sees (NULL: all up to it)
+  int32_t mask_words;
 };
 
 constexpr int kRowsWaves = 4;      // waves of an attend_rows work-group
@@ -304,6 +306,7 @@ hipError_t launch_gather_paged(GatherPagedLaunch L, hipStream_t s);
 int64_t attend_paged_groups(const AttendPagedLaunch &L);
 int64_t attend_paged_join_groups(const AttendPagedLaunch &L);  // 0: no join
 size_t attend_paged_part_bytes(const AttendPagedLaunch &L);
+size_t attend_tree_workspace(const ebd_attend_tree_params *p);    // 0: invalid parameters
 size_t attend_paged_workspace(const ebd_attend_paged_params *p);  // 0: invalid parameters
 hipError_t launch_attend_paged(const AttendPagedLaunch &L, hipStream_t s);
 hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s);

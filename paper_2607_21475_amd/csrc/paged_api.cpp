@@ -133,8 +133,8 @@ int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_
 
 // A launch for blocks of `rows` query rows; `sum` query rows in all, the sequences' most `rows_max` each, and each of those
 // that it takes more than `more_than`.
-AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t rows, int64_t rows_max, int64_t sum,
-                                    int64_t more_than = 0) {
+AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, bool tree, int32_t rows, int64_t rows_max,
+                                    int64_t sum, int64_t more_than = 0) {
   AttendPagedLaunch L{};
   L.p = *p;
   L.rows = rows;
@@ -152,7 +152,7 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, int32_t ro
   L.units = L.blocks ? S * aside : counted;
   // the most rows a block of query rows sees, under a window from a tile's border on
   int64_t span = p->max_rows;
-  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + rows / p->group + 1);
+  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + (tree ? p->max_new : rows / p->group) + 1);
   span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
   const int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
   L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
@@ -191,13 +191,13 @@ struct AttendPagedPlan {
 // 2048 over 16384 513 / 504, 512 over 4096 61 / 60; not taken: 8192 over 8192 571 / 567, 2048 over 8192 257 / 265, 1500
 // over 6000 167 / 180, 256 over 1024 30 / 35, 160 (a block half empty) over 32768 122 / 130; 8 ragged sequences of up to
 // 256 over up to 16384 320 / 420.
-bool long_blocks(const ebd_attend_paged_params *p, int64_t most) {
+bool long_blocks(const ebd_attend_paged_params *p, bool tree, int64_t most) {
   if (p->pages.num_seqs != 1 || most < kLongRows || (int64_t)p->max_new * 8 > p->max_rows) return false;
-  const AttendPagedLaunch L = attend_paged_part(p, kLongRows, most, std::min<int64_t>(p->num_tokens * p->group, most));
+  const AttendPagedLaunch L = attend_paged_part(p, tree, kLongRows, most, std::min<int64_t>(p->num_tokens * p->group, most));
   const int64_t groups = attend_paged_groups(L), rows = (most + kLongRows - 1) / kLongRows * kLongRows;
   return groups <= kCus && 8 * groups >= 7 * kCus && 8 * most >= 7 * rows;
 }
-AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
+AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p, bool tree = false) {
   const int64_t S = p->pages.num_seqs, G = p->group, most = (int64_t)p->max_new * G;
   const int64_t sum = std::min<int64_t>(p->num_tokens * G, S * most);
   const int32_t rows = most <= 16 ? 16 : most <= kRowsKernelMax ? 32 : most <= kFewRows ? kFewRows : kTileRows;
@@ -206,15 +206,19 @@ AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p) {
   if (rows == kTileRows && S > 1 && G <= kRowsKernelMax && 4 * (sum - most) <= (S - 1) * most) {
     const int32_t small = G <= 16 ? 16 : kRowsKernelMax;
     plan.parts = 2;
-    plan.part[1] = attend_paged_part(p, small, small, S * small);
+    plan.part[1] = attend_paged_part(p, tree, small, small, S * small);
     plan.part[1].at_most = small;
-    plan.part[0] = attend_paged_part(p, rows, most, sum, small);
-  } else if (long_blocks(p, most)) {
-    plan.part[0] = attend_paged_part(p, kLongRows, most, sum);
+    plan.part[0] = attend_paged_part(p, tree, rows, most, sum, small);
+  } else if (long_blocks(p, tree, most)) {
+    plan.part[0] = attend_paged_part(p, tree, kLongRows, most, sum);
   } else {
-    plan.part[0] = attend_paged_part(p, rows, most, sum);
+    plan.part[0] = attend_paged_part(p, tree, rows, most, sum);
   }
   return plan;
+}
+
+bool valid_attend_tree(const ebd_attend_tree_params *p) {
+  return p && valid_attend_paged(&p->attend) && p->mask_words >= 1 && p->mask_words <= kMaskWords && p->reserved == 0;
 }
 
 size_t part_bytes(const AttendPagedLaunch &L) { return (attend_paged_part_bytes(L) + 255) / 256 * 256; }
@@ -224,6 +228,46 @@ size_t plan_bytes(const AttendPagedPlan &plan) {
   return bytes;
 }
 
+// Attention of the new tokens, which see each other in order (mask NULL) or by a mask.
+ebd_status attend(const ebd_attend_paged_params *p, const uint64_t *mask, int32_t mask_words, const uint16_t *q,
+                  const uint16_t *K, const uint16_t *V, uint16_t *y, float *lse, uint32_t *status, void *workspace,
+                  size_t ws_bytes, void *stream) {
+  if (!supported_attend_paged(p)) return EBD_ERR_UNSUPPORTED;
+  if (p->num_tokens == 0 || p->pages.num_seqs == 0) return EBD_OK;
+  if (p->max_new == 0 || !q || !K || !V || !y || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(y) || ((uintptr_t)lse & 3))
+    return EBD_ERR_INVALID_ARG;
+  AttendPagedPlan plan = attend_paged_plan(p, mask != nullptr);
+  for (int i = 0; i < plan.parts; ++i)
+    if (attend_paged_groups(plan.part[i]) > kGridMax / 2 || attend_paged_join_groups(plan.part[i]) > kGridMax)
+      return EBD_ERR_UNSUPPORTED;
+  if (!workspace || ws_bytes < plan_bytes(plan) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char *ws = static_cast<char *>(workspace);
+  for (int i = 0; i < plan.parts; ++i) {
+    AttendPagedLaunch &L = plan.part[i];
+    L.q = q;
+    L.K = K;
+    L.V = V;
+    L.y = y;
+    L.lse = lse;
+    L.status = status;
+    L.mask = mask;
+    L.mask_words = mask_words;
+    L.part = reinterpret_cast<float *>(ws);
+    L.stats = reinterpret_cast<float2 *>(L.part + attend_paged_groups(L) * L.rows * kHeadDim);
+    ws += part_bytes(L);
+    if (timed_launch(mask ? "attend_tree" : "attend_paged", s, [&] { return launch_attend_paged(L, s); }) != hipSuccess) return EBD_ERR_HIP;
+    if (L.nsplit > 1 &&
+        timed_launch(mask ? "attend_tree_join" : "attend_paged_join", s,
+                     [&] { return launch_attend_paged_join(L, s); }) != hipSuccess)
+      return EBD_ERR_HIP;
+  }
+  return EBD_OK;
+}
+
 }  // namespace
 
 namespace ebd {
@@ -231,6 +275,11 @@ namespace ebd {
 size_t attend_paged_workspace(const ebd_attend_paged_params *p) {
   if (!valid_attend_paged(p) || !supported_attend_paged(p)) return 0;
   return plan_bytes(attend_paged_plan(p));
+}
+
+size_t attend_tree_workspace(const ebd_attend_tree_params *p) {
+  if (!valid_attend_tree(p) || !supported_attend_paged(&p->attend)) return 0;
+  return plan_bytes(attend_paged_plan(&p->attend, true));
 }
 
 size_t plan_step_workspace(const ebd_plan_step_params *p) {
@@ -299,37 +348,14 @@ ebd_status ebd_attend_paged(const ebd_attend_paged_params *p, const uint16_t *q,
                             const uint16_t *V, uint16_t *y, float *lse, uint32_t *status,
                             void *workspace, size_t ws_bytes, void *stream) {
   if (!valid_attend_paged(p)) return EBD_ERR_INVALID_ARG;
-  if (!supported_attend_paged(p)) return EBD_ERR_UNSUPPORTED;
-  if (p->num_tokens == 0 || p->pages.num_seqs == 0) return EBD_OK;
-  if (p->max_new == 0 || !q || !K || !V || !y || !p->new_off || !p->len) return EBD_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(y) || ((uintptr_t)lse & 3))
-    return EBD_ERR_INVALID_ARG;
-  AttendPagedPlan plan = attend_paged_plan(p);
-  for (int i = 0; i < plan.parts; ++i)
-    if (attend_paged_groups(plan.part[i]) > kGridMax / 2 || attend_paged_join_groups(plan.part[i]) > kGridMax)
-      return EBD_ERR_UNSUPPORTED;
-  if (!workspace || ws_bytes < plan_bytes(plan) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
-  const ebd_status ds = device_ok();
-  if (ds != EBD_OK) return ds;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  char *ws = static_cast<char *>(workspace);
-  for (int i = 0; i < plan.parts; ++i) {
-    AttendPagedLaunch &L = plan.part[i];
-    L.q = q;
-    L.K = K;
-    L.V = V;
-    L.y = y;
-    L.lse = lse;
-    L.status = status;
-    L.part = reinterpret_cast<float *>(ws);
-    L.stats = reinterpret_cast<float2 *>(L.part + attend_paged_groups(L) * L.rows * kHeadDim);
-    ws += part_bytes(L);
-    if (timed_launch("attend_paged", s, [&] { return launch_attend_paged(L, s); }) != hipSuccess) return EBD_ERR_HIP;
-    if (L.nsplit > 1 &&
-        timed_launch("attend_paged_join", s, [&] { return launch_attend_paged_join(L, s); }) != hipSuccess)
-      return EBD_ERR_HIP;
-  }
-  return EBD_OK;
+  return attend(p, nullptr, 0, q, K, V, y, lse, status, workspace, ws_bytes, stream);
+}
+
+ebd_status ebd_attend_tree(const ebd_attend_tree_params *p, const uint16_t *q, const uint16_t *K, const uint16_t *V,
+                           uint16_t *y, float *lse, uint32_t *status, void *workspace, size_t ws_bytes, void *stream) {
+  if (!valid_attend_tree(p)) return EBD_ERR_INVALID_ARG;
+  if (p->attend.num_tokens > 0 && (!p->mask || ((uintptr_t)p->mask & 7))) return EBD_ERR_INVALID_ARG;
+  return attend(&p->attend, p->mask, p->mask_words, q, K, V, y, lse, status, workspace, ws_bytes, stream);
 }
 
 ebd_status ebd_gather_paged(const ebd_gather_paged_params *p, const uint16_t *K, const uint16_t *V,

@@ -6,6 +6,7 @@
     ebd_gather_paged    the pages read out as units, which ebd_scores and ebd_evict take
     ebd_norm_rope       norms of heads and rotary positions in one pass; ebd_norm_rope_backward: their gradients
     ebd_append_norm     ebd_append_paged for models that normalise queries and keys for each head
+    ebd_attend_tree     attention of trees of drafted tokens over the pages
     ebd_plan_step       page tables, slots, positions and tree masks of a step, from the new token counts
 
 Each call takes a parameter struct (`rope_params`, `append_paged_params`, ...) that a program makes once
@@ -120,6 +121,15 @@ class ebd_gather_paged_params(ctypes.Structure):
     ]
 
 
+class ebd_attend_tree_params(ctypes.Structure):
+    _fields_ = [
+        ("attend", ebd_attend_paged_params),
+        ("mask", ctypes.c_void_p),
+        ("mask_words", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 class ebd_norm(ctypes.Structure):
     _fields_ = [
         ("weight", ctypes.c_void_p),
@@ -197,6 +207,8 @@ _lib.ebd_attend_paged.argtypes = [_P] * 8 + [ctypes.c_size_t, _P]
 _lib.ebd_attend_paged.restype = ctypes.c_int
 _lib.ebd_gather_paged.argtypes = [_P] * 7
 _lib.ebd_gather_paged.restype = ctypes.c_int
+_lib.ebd_attend_tree.argtypes = [_P] * 8 + [ctypes.c_size_t, _P]
+_lib.ebd_attend_tree.restype = ctypes.c_int
 _lib.ebd_norm_rope.argtypes = [_P] * 4
 _lib.ebd_norm_rope.restype = ctypes.c_int
 _lib.ebd_norm_rope_backward.argtypes = [_P] * 6 + [ctypes.c_size_t, _P]
@@ -515,6 +527,21 @@ def attend_paged_params(pgs: ebd_pages, q, y, new_off, len, max_new: int, max_ro
                  K=K, V=V, q=q, y=y)
 
 
+def attend_tree_params(pgs: ebd_pages, q, y, new_off, len, max_new: int, max_rows: int, mask, qpos=None,
+                       window: int = 0, scale: float = 0.0) -> ebd_attend_tree_params:
+    """As attend_paged_params, but new tokens see each other by mask [tokens, words] int64: bit i of word w is the
+    sequence's new token 64 w + i.  qpos (positions) then serve the window alone, over the rows held before."""
+    a = attend_paged_params(pgs, q, y, new_off, len, max_new, max_rows, qpos=qpos, window=window, scale=scale)
+    if not isinstance(mask, torch.Tensor) or mask.dim() != 2:
+        raise ValueError("mask must be [tokens, words]")
+    p = ebd_attend_tree_params()
+    p.attend = a
+    p.mask, p.mask_words = _table(mask, torch.int64, (q.shape[0], mask.shape[1]), "mask"), mask.shape[1]
+    _plan(p, _here(q, mask), (a.keep, mask))
+    p.expect, p.seqs, p.heads = a.expect, a.seqs, a.heads
+    return p
+
+
 def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_paged_params:
     """Units seq_off [sequences * KV heads + 1] int64, the longest at most max_rows.  The rows that there is room for
     are those of each call's outputs."""
@@ -590,6 +617,18 @@ def ebd_attend_paged(params: ebd_attend_paged_params, q, K, V, y, workspace, lse
                                  _out(params, "workspace", workspace, workspace.dtype, None), workspace.nbytes,
                                  _on_stream(params, stream))
     _check("ebd_attend_paged", code)
+
+
+def ebd_attend_tree(params: ebd_attend_tree_params, q, K, V, y, workspace, lse=None, status=None, stream=None) -> None:
+    """Attention of trees of drafted tokens over the paged cache (asynchronous)."""
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
+    code = _lib.ebd_attend_tree(params.at, _arg(params, "q", q), _arg(params, "K", K), _arg(params, "V", V),
+                                _arg(params, "y", y), _out(params, "lse", lse, torch.float32, params.heads),
+                                _out(params, "status", status, _I32, params.seqs),
+                                _out(params, "workspace", workspace, workspace.dtype, None), workspace.nbytes,
+                                _on_stream(params, stream))
+    _check("ebd_attend_tree", code)
 
 
 def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None, stream=None) -> None:

@@ -156,3 +156,46 @@ def tree(n, rng):
 def chains(n, width):
     """... of `width` chains side by side."""
     return [j - width if j >= width else -1 for j in range(n)]
+
+
+# ---- trees -------------------------------------------------------------------------------------
+
+def masks_of(parents, words):
+    """Mask words (signed) of a tree's tokens, and their depths."""
+    bits, depth, out = [], [], []
+    for j, up in enumerate(parents):
+        bits.append((bits[up] if up >= 0 else 0) | 1 << j)
+        depth.append(0 if up < 0 else depth[up] + 1)
+        out.append([signed(bits[j] >> (64 * w) & (2 ** 64 - 1)) for w in range(words)])
+    return out, depth
+
+
+def sees(first, n, held, word_row, pos, window, limit=None):
+    """Rows that a token sees by the definition: word_row its mask words, pos its position, n the rows of the sequence."""
+    if pos < 0:
+        return []
+    lo = max(0, pos - window + 1) if window else 0
+    rows = list(range(min(lo, max(first, 0)), max(first, 0)))
+    for w, word in enumerate(word_row):
+        rows += [first + 64 * w + i for i in range(64) if word >> i & 1]
+    return [r for r in rows if 0 <= r < n and (limit is None or r < limit) and (held is None or held(r))]
+
+
+def attend_row(cache, s, h, q, rows, scale=None, weights_bits=16):
+    """(y, lse, tolerance of y, tolerance of lse) of query rows q [heads, 128] of KV head h of sequence s over these rows of
+    it, in float64 (the tolerances of paged_ref.attend)."""
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    q = q.double()
+    if not rows:
+        z = torch.zeros(q.shape[0], dtype=torch.float64, device=q.device)
+        return torch.zeros_like(q), z - math.inf, torch.zeros_like(q), z
+    i = torch.tensor(rows, device=q.device)
+    pg = cache.table[s][i // cache.page].long()
+    k, v = (x[pg, h, i % cache.page].double() for x in (cache.K, cache.V))
+    l = scale * q @ k.t()
+    z = torch.logsumexp(l, 1)
+    w = torch.exp(l - z[:, None])
+    e = 2 * 128 * U * (scale * q.abs() @ k.abs().t()).amax(1) + 2.0 ** -22 + len(rows) * U
+    y = w @ v
+    ty = HALF_STEP * y.abs() + (1 + HALF_STEP) * ((2 * e + 2.0 ** -weights_bits)[:, None] * (w @ v.abs()))
+    return y, z, ty, e + 2.0 ** -22 * (z.abs() + 1)

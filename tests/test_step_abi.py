@@ -168,3 +168,40 @@ def test_plans_of_the_binding():
                      (dict(), "CUDA|GPU|cuda|device")):
         with pytest.raises((ValueError, TypeError), match=what):
             ebd.plan_step_params(**{**args, **kw})
+
+
+def _tree_params(mask=FAKE, words=1, reserved=0, **kw):
+    from test_paged_abi import _attend_params
+
+    p = paged.ebd_attend_tree_params()
+    p.attend, p.mask, p.mask_words, p.reserved = _attend_params(**kw), mask, words, reserved
+    return p
+
+
+def _tree(args=None, ws=FAKE, ws_bytes=1 << 40, **kw):
+    a = [FAKE] * 4 + [None, None]
+    for i, v in (args or {}).items():
+        a[i] = v
+    p = _tree_params(**kw)
+    size = LIB.ebd_workspace_size(ebd.EBD_WS_ATTEND_TREE, ctypes.byref(p))
+    return LIB.ebd_attend_tree(ctypes.byref(p), *a, ws, ws_bytes, None), size
+
+
+def test_tree_refusals():
+    assert LIB.ebd_attend_tree(None, *[FAKE] * 4, None, None, FAKE, 1 << 40, None) == BAD
+    assert LIB.ebd_workspace_size(ebd.EBD_WS_ATTEND_TREE, None) == 0
+    for kw, code in BAD_PAGES:
+        assert _tree(pages=_pages(**kw)) == (code, 0), kw
+    for kw in (dict(words=0), dict(words=65), dict(reserved=1), dict(group=0), dict(max_new=-1), dict(num_tokens=-1),
+               dict(max_rows=-1), dict(window=-1), dict(scale=-1.0), dict(q_rows=paged.ebd_rows(-8, 128))):
+        assert _tree(**kw) == (BAD, 0), kw
+    for kw in (dict(mask=None), dict(mask=FAKE + 4), dict(max_new=0), dict(new_off=None), dict(len=None)):
+        assert _tree(**kw)[0] == BAD, kw
+    for i in range(4):
+        assert _tree({i: None})[0] == BAD and _tree({i: FAKE + 8})[0] == BAD, i
+    for kw in (dict(max_rows=(1 << 30) + 1), dict(num_tokens=1 << 24), dict(max_new=1 << 29)):
+        assert _tree(**kw) == (UNSUPPORTED, 0), kw
+    need = _tree(max_rows=1 << 20)[1]
+    assert need > 256 and _tree(max_rows=1 << 20, ws_bytes=need - 1)[0] == NO_WS
+    assert _tree(ws=None)[0] == NO_WS and _tree(ws=FAKE + 64)[0] == NO_WS
+    assert _tree(num_tokens=0, mask=None)[0] == OK and _tree(pages=_pages(num_seqs=0))[0] == OK
