@@ -661,6 +661,30 @@ typedef struct ebd_attend_tree_params {
 ebd_status ebd_attend_tree(const ebd_attend_tree_params *p, const uint16_t *q, const uint16_t *K, const uint16_t *V,
                            uint16_t *y, float *lse, uint32_t *status, void *workspace, size_t ws_bytes, void *stream);
 
+/*
+ * ebd_keep_rows -- after a tree was verified: the rows of its accepted path move together.  Of sequence s, whose last
+ * new_off[s+1] - new_off[s] rows of len[s] are the new tokens', the row of new token path[s, i] moves to the place of new
+ * token i for i < kept[s], in K and V and all heads; what lies behind them counts no more.
+ *   path     [num_seqs, max_kept] device int32, increasing in each sequence's first kept[s] entries.
+ *   kept     [num_seqs] device int32, 0 .. min(max_kept, new tokens).
+ *   len_out  [num_seqs] device int32 or NULL, written: first + kept[s].  May be len (of the last layer's call).
+ *   status   [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_LAYOUT when kept or path is out of place (nothing moves,
+ *            len_out = len), EBD_ST_BAD_PAGE when a row to move, or its new place, has no page (that row is not moved).
+ * The sequences' new rows must not share pages.  Limits as for the other calls on the paged cache; at most 2^24 - 1 sequences.
+ */
+typedef struct ebd_keep_rows_params {
+    ebd_pages pages;
+    const int64_t *new_off;
+    const int32_t *len;
+    const int32_t *path;
+    const int32_t *kept;
+    int32_t *len_out;
+    int32_t max_kept;
+    int32_t reserved; /* 0 */
+} ebd_keep_rows_params;
+
+ebd_status ebd_keep_rows(const ebd_keep_rows_params *p, uint16_t *K, uint16_t *V, uint32_t *status, void *stream);
+
 /* which-values for ebd_workspace_size */
 #define EBD_WS_EVICT 0
 #define EBD_WS_ATTEND 1
@@ -698,7 +722,8 @@ const char *ebd_version(void);
  * "norm_rope", "norm_rope_backward", "norm_rope_join",
  * "append_norm",
  * "plan_step",
- * "attend_tree", "attend_tree_join") to *total_ms and its launch count to
+ * "attend_tree", "attend_tree_join",
+ * "keep_rows") to *total_ms and its launch count to
  * *launches; it then clears that kernel's record.  The switch is an atomic flag and the records
  * are guarded by a lock, so both calls may come from any host thread; while timing is off no
  * event is created and launches take no lock.

@@ -9,7 +9,7 @@ error statuses.  The functions carry the C names:
     ebd_append_certain   append a decode token with pi = 1
     ebd_rope, ebd_append_paged, ebd_attend_paged, ebd_gather_paged   the paged cache before eviction (paged.py)
     ebd_norm_rope, ebd_norm_rope_backward, ebd_append_norm           ... with norms of queries and keys for each head
-    ebd_attend_tree      attention of trees of drafted tokens
+    ebd_attend_tree, ebd_keep_rows   attention of trees of drafted tokens, and the accepted path's rows moved together
     ebd_plan_step        page tables, slots, positions and tree masks of a serving step
     ebd_workspace_size, ebd_status_string, ebd_version, ebd_timing_enable, ebd_timing_read
 
@@ -389,6 +389,7 @@ def workspace(nbytes: int, device="cuda") -> torch.Tensor:
 
 from .paged import (EBD_ROPE_HALF, EBD_ROPE_INVERSE, EBD_ROPE_PAIRS, PagedCache,  # noqa: E402
                     append_norm_params, append_paged_params, attend_paged_params, attend_tree_params, ebd_append_norm,
-                    ebd_append_paged, ebd_attend_paged, ebd_attend_tree, ebd_gather_paged, ebd_norm, ebd_norm_rope, ebd_norm_rope_backward, ebd_pages,
-                    ebd_plan_step, ebd_rope, ebd_rotary, gather_paged_params, head_norm, norm_rope_backward_params,
-                    norm_rope_params, pages, plan_step_params, rope_frequencies, rope_params, rotary)
+                    ebd_append_paged, ebd_attend_paged, ebd_attend_tree, ebd_gather_paged, ebd_keep_rows, ebd_norm,
+                    ebd_norm_rope, ebd_norm_rope_backward, ebd_pages, ebd_plan_step, ebd_rope, ebd_rotary,
+                    gather_paged_params, head_norm, keep_rows_params, norm_rope_backward_params, norm_rope_params, pages,
+                    plan_step_params, rope_frequencies, rope_params, rotary)

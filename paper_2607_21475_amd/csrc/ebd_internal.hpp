@@ -214,6 +214,13 @@ struct PlanStepLaunch {
   int32_t shift;
 };
 
+struct KeepRowsLaunch {
+  ebd_keep_rows_params p;
+  uint16_t *K, *V;
+  uint32_t *status;
+  int32_t shift;
+};
+
 struct GatherPagedLaunch {
   ebd_gather_paged_params p;
   const uint16_t *K, *V;
@@ -301,6 +308,7 @@ hipError_t launch_append_norm(AppendNormLaunch L, hipStream_t s);
 size_t plan_step_bytes(const ebd_plan_step_params &p);
 size_t plan_step_workspace(const ebd_plan_step_params *p);  // 0: invalid parameters
 hipError_t launch_plan_step(const PlanStepLaunch &L, hipStream_t s);
+hipError_t launch_keep_rows(const KeepRowsLaunch &L, hipStream_t s);
 int64_t gather_paged_groups(const ebd_gather_paged_params &p);
 hipError_t launch_gather_paged(GatherPagedLaunch L, hipStream_t s);
 int64_t attend_paged_groups(const AttendPagedLaunch &L);

@@ -479,4 +479,22 @@ ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *
   return timed_launch("plan_step", s, [&] { return launch_plan_step(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
 }
 
+ebd_status ebd_keep_rows(const ebd_keep_rows_params *p, uint16_t *K, uint16_t *V, uint32_t *status, void *stream) {
+  if (!p || !valid_pages(p->pages) || p->max_kept < 0 || p->reserved != 0) return EBD_ERR_INVALID_ARG;
+  if (!supported_pages(p->pages) || p->pages.num_seqs > kGridMax || p->max_kept > kGridMax) return EBD_ERR_UNSUPPORTED;
+  if (p->pages.num_seqs == 0) return EBD_OK;
+  if (!K || !V || !p->new_off || !p->len || !p->kept || (p->max_kept > 0 && !p->path)) return EBD_ERR_INVALID_ARG;
+  if (!aligned16(K) || !aligned16(V)) return EBD_ERR_INVALID_ARG;
+  const ebd_status ds = device_ok();
+  if (ds != EBD_OK) return ds;
+  KeepRowsLaunch L{};
+  L.p = *p;
+  L.K = K;
+  L.V = V;
+  L.status = status;
+  L.shift = log2_of(p->pages.page_size);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return timed_launch("keep_rows", s, [&] { return launch_keep_rows(L, s); }) == hipSuccess ? EBD_OK : EBD_ERR_HIP;
+}
+
 }  // extern "C"

@@ -7,6 +7,7 @@
     ebd_norm_rope       norms of heads and rotary positions in one pass; ebd_norm_rope_backward: their gradients
     ebd_append_norm     ebd_append_paged for models that normalise queries and keys for each head
     ebd_attend_tree     attention of trees of drafted tokens over the pages
+    ebd_keep_rows       the rows of a tree's accepted path moved together
     ebd_plan_step       page tables, slots, positions and tree masks of a step, from the new token counts
 
 Each call takes a parameter struct (`rope_params`, `append_paged_params`, ...) that a program makes once
@@ -130,6 +131,19 @@ class ebd_attend_tree_params(ctypes.Structure):
     ]
 
 
+class ebd_keep_rows_params(ctypes.Structure):
+    _fields_ = [
+        ("pages", ebd_pages),
+        ("new_off", ctypes.c_void_p),
+        ("len", ctypes.c_void_p),
+        ("path", ctypes.c_void_p),
+        ("kept", ctypes.c_void_p),
+        ("len_out", ctypes.c_void_p),
+        ("max_kept", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 class ebd_norm(ctypes.Structure):
     _fields_ = [
         ("weight", ctypes.c_void_p),
@@ -209,6 +223,8 @@ _lib.ebd_gather_paged.argtypes = [_P] * 7
 _lib.ebd_gather_paged.restype = ctypes.c_int
 _lib.ebd_attend_tree.argtypes = [_P] * 8 + [ctypes.c_size_t, _P]
 _lib.ebd_attend_tree.restype = ctypes.c_int
+_lib.ebd_keep_rows.argtypes = [_P] * 5
+_lib.ebd_keep_rows.restype = ctypes.c_int
 _lib.ebd_norm_rope.argtypes = [_P] * 4
 _lib.ebd_norm_rope.restype = ctypes.c_int
 _lib.ebd_norm_rope_backward.argtypes = [_P] * 6 + [ctypes.c_size_t, _P]
@@ -542,6 +558,24 @@ def attend_tree_params(pgs: ebd_pages, q, y, new_off, len, max_new: int, max_row
     return p
 
 
+def keep_rows_params(pgs: ebd_pages, new_off, len, path, kept, len_out=None) -> ebd_keep_rows_params:
+    """Of sequences new_off [sequences + 1] int64 that hold len [sequences] int32 rows, the new tokens path [sequences,
+    most kept] int32 (the first kept [sequences] int32 of each) are kept; len_out [sequences] int32 (may be len) receives
+    the rows then held."""
+    S = pgs.num_seqs
+    if not isinstance(path, torch.Tensor) or path.dim() != 2:
+        raise ValueError("path must be [sequences, most kept]")
+    p = ebd_keep_rows_params()
+    p.pages, p.max_kept = pgs, path.shape[1]
+    p.new_off, p.len = _table(new_off, torch.int64, (S + 1,), "new_off"), _table(len, _I32, (S,), "len")
+    p.path, p.kept = _table(path, _I32, (S, path.shape[1]), "path"), _table(kept, _I32, (S,), "kept")
+    p.len_out = _table(len_out, _I32, (S,), "len_out")
+    p.seqs = (S,)
+    K, V = pgs.pools
+    return _plan(p, _here(K, V, pgs.keep, new_off, len, path, kept, len_out), (pgs.keep, new_off, len, path, kept, len_out),
+                 K=K, V=V)
+
+
 def gather_paged_params(pgs: ebd_pages, seq_off, max_rows: int) -> ebd_gather_paged_params:
     """Units seq_off [sequences * KV heads + 1] int64, the longest at most max_rows.  The rows that there is room for
     are those of each call's outputs."""
@@ -629,6 +663,13 @@ def ebd_attend_tree(params: ebd_attend_tree_params, q, K, V, y, workspace, lse=N
                                 _out(params, "workspace", workspace, workspace.dtype, None), workspace.nbytes,
                                 _on_stream(params, stream))
     _check("ebd_attend_tree", code)
+
+
+def ebd_keep_rows(params: ebd_keep_rows_params, K, V, status=None, stream=None) -> None:
+    """Move the rows of the accepted paths together (asynchronous)."""
+    code = _lib.ebd_keep_rows(params.at, _arg(params, "K", K), _arg(params, "V", V),
+                              _out(params, "status", status, _I32, params.seqs), _on_stream(params, stream))
+    _check("ebd_keep_rows", code)
 
 
 def ebd_gather_paged(params: ebd_gather_paged_params, K, V, Ku, Vu, status=None, stream=None) -> None:

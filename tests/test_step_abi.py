@@ -205,3 +205,20 @@ def test_tree_refusals():
     assert need > 256 and _tree(max_rows=1 << 20, ws_bytes=need - 1)[0] == NO_WS
     assert _tree(ws=None)[0] == NO_WS and _tree(ws=FAKE + 64)[0] == NO_WS
     assert _tree(num_tokens=0, mask=None)[0] == OK and _tree(pages=_pages(num_seqs=0))[0] == OK
+
+
+def _keep(K=FAKE, V=FAKE, **kw):
+    p = paged.ebd_keep_rows_params()
+    _with(p, pages=_pages(), new_off=FAKE, len=FAKE, path=FAKE, kept=FAKE, len_out=None, max_kept=4)
+    return LIB.ebd_keep_rows(ctypes.byref(_with(p, **kw)), K, V, None, None)
+
+
+def test_keep_refusals():
+    assert LIB.ebd_keep_rows(None, FAKE, FAKE, None, None) == BAD
+    for kw, code in BAD_PAGES:
+        assert _keep(pages=_pages(**kw)) == code, kw
+    for kw in (dict(max_kept=-1), dict(reserved=1), dict(new_off=None), dict(len=None), dict(path=None), dict(kept=None),
+               dict(K=None), dict(V=None), dict(K=FAKE + 8), dict(V=FAKE + 2)):
+        assert _keep(**kw) == BAD, kw
+    assert _keep(pages=_pages(num_seqs=1 << 24)) == UNSUPPORTED and _keep(max_kept=1 << 24) == UNSUPPORTED
+    assert _keep(pages=_pages(num_seqs=0)) == OK
