@@ -70,10 +70,22 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
     for (int b = 0; b < NQ; ++b)
       if (__any(TREE ? tree_past_table(L, sq, 16 * b + c) : past_table(L, sq, 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   }
-  Range R = TREE || p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, 0, token(nrow - 1));
-  if constexpr (TREE) R.every_hi = (int)min((int64_t)R.every_hi, max((int64_t)0, sq.first));
+  Range R;
+  uint64_t word0[NQ];  // of a row's mask: few rows have few tokens
+  if constexpr (TREE) {
+    R = p.window > 0 ? range_of<NQ>(span) : tree_range_of(sq);
+    if (p.window > 0) R.every_hi = (int)min((int64_t)R.every_hi, max((int64_t)0, sq.first));
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) word0[b] = L.mask[(sq.t0 + token(min(16 * b + c, nrow - 1))) * L.mask_words];
+  } else {
+    R = p.qpos ? range_of<NQ>(span) : range_of_tokens(p, sq, 0, token(nrow - 1));
+  }
   // whether this lane's row of a block sees a key inside its span
-  auto masked = [&](int b, int k) { return mask_bits(L, sq, sq.t0 + token(min(16 * b + c, nrow - 1)), k); };
+  auto masked = [&](int b, int k) {
+    return mask_bits(L, sq, k, [&](int i) {
+      return i == 0 ? word0[b] : L.mask[(sq.t0 + token(min(16 * b + c, nrow - 1))) * L.mask_words + i];
+    });
+  };
   const Keys split = split_of(L, R.lo, R.hi, kTileKeys, sp);
   const int k_beg = split.beg, k_end = split.end;  // (below 2^30: no sum below overflows)
 
@@ -183,6 +195,7 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   for (int b = 0; b < NQ; ++b) {
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) asm volatile("" : "+v"(Q[b][kb]));
+    if constexpr (TREE) asm volatile("" : "+v"(word0[b]));
   }
 
   for (; k < k_end; k += stride, stage ^= 1) {

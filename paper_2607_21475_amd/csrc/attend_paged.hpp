@@ -144,15 +144,16 @@ struct Span {
 // Under a mask (TREE) a row of span lo .. hi - 1 sees, of those, the rows held before the step, and the new tokens' rows
 // (from sq.first on) whose bit is set in its token's mask.
 
-// Bits of the rows k .. k + 31: set for held ones, and as token t's mask says for new ones.
-__device__ __forceinline__ uint32_t mask_bits(const AttendPagedLaunch &L, const Seq &q, int64_t t, int k) {
+// Bits of the rows k .. k + 31: set for held ones, and for new ones as word(i) says, the words of a token's mask (0 past
+// its last).
+template <class F>
+__device__ __forceinline__ uint32_t mask_bits(const AttendPagedLaunch &L, const Seq &q, int k, const F &word) {
   const int64_t d = k - q.first;
   if (d + 32 <= 0) return ~0u;
-  const uint64_t *m = L.mask + t * L.mask_words;
-  if (d < 0) return (uint32_t)m[0] << (int)-d | ((1u << (int)-d) - 1u);
+  if (d < 0) return (uint32_t)word(0) << (int)-d | ((1u << (int)-d) - 1u);
   const int i = (int)min(d >> 6, (int64_t)L.mask_words), s = (int)(d & 63);
-  uint64_t w = i < L.mask_words ? m[i] >> s : 0;
-  if (s > 32 && i + 1 < L.mask_words) w |= m[i + 1] << (64 - s);
+  uint64_t w = i < L.mask_words ? word(i) >> s : 0;
+  if (s > 32 && i + 1 < L.mask_words) w |= word(i + 1) << (64 - s);
   return (uint32_t)w;
 }
 
@@ -169,15 +170,16 @@ __device__ __forceinline__ bool sees_any(const AttendPagedLaunch &L, const Seq &
   return false;
 }
 
+// (without branches, so that a position on its way is waited for where it is used)
 __device__ __forceinline__ Span tree_span_of(const AttendPagedLaunch &L, const Seq &q, int row) {
   const ebd_attend_paged_params &p = L.p;
-  const int j = L.by_group.quotient(row);
-  if (j >= q.tokens) return {0, 0};
+  const int j = min(L.by_group.quotient(row), q.tokens - 1);  // (a sequence that is looked at has tokens)
   const int64_t pos = p.qpos ? (int64_t)p.qpos[q.t0 + j] : q.first + j;
-  if (pos < 0) return {0, 0};
   const int64_t lo = p.window > 0 ? min(max((int64_t)0, pos - p.window + 1), max((int64_t)0, q.first)) : 0;
-  return lo < q.seen ? Span{(int)lo, (int)q.seen} : Span{0, 0};
+  const bool sees = (row < q.tokens * p.group) & (pos >= 0) & (lo < q.seen);
+  return Span{sees ? (int)lo : 0, sees ? (int)q.seen : 0};
 }
+
 __device__ __forceinline__ Span span_of(const AttendPagedLaunch &L, const Seq &q, int row) {
   const ebd_attend_paged_params &p = L.p;
   const int j = L.by_group.quotient(row);
@@ -213,6 +215,13 @@ __device__ __forceinline__ bool tree_past_table(const AttendPagedLaunch &L, cons
 struct Range {
   int lo, hi, every_lo, every_hi;
 };
+// What the rows of a block see without a window, whatever their masks and positions: known from the sequence alone, so that
+// the first tiles can be asked for.
+__device__ __forceinline__ Range tree_range_of(const Seq &q) {
+  const int seen = (int)max(q.seen, (int64_t)0);
+  return {0, seen, 0, (int)min((int64_t)seen, max((int64_t)0, q.first))};
+}
+
 template <int N>
 __device__ __forceinline__ Range range_of(const Span (&s)[N]) {
   int lo = INT32_MAX, hi = 0, elo = 0, ehi = INT32_MAX;

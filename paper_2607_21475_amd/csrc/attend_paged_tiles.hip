@@ -17,6 +17,14 @@
 //   64 query rows by eight waves, in four groups of two that take every fourth tile of 32 keys: 33 to 64 rows are
 //   too few to hide the memory with 128-row blocks, and too much work for attend_rows' one wave a SIMD (16 sequences
 //   of up to 6144 rows, 56 query rows: 40 us, attend_rows 58).
+//   Trees (a mask says which new tokens a token sees): a lane reads its row's bits for a tile of new rows from the mask's words,
+//   the first of which wait in LDS; tiles of held rows are as above.  They have a shape more: 128 query rows by eight waves in
+//   two groups of four, tiles of 64 keys, one work-group a CU.  Alone on its CU a work-group of four waves takes 1.9 us a
+//   tile, whatever the depth of its loads (three or four tiles on their way: the same), a chain of products, weights and
+//   products; two groups take two tiles in that time, as two work-groups would, but leave half as many partial sums.  Four
+//   sequences of up to 300 tokens, 4 heads of 7, under a window of 2048: 51 us, with work-groups of four waves 58 (three
+//   splits), 77 (one).  32 sequences of 64 tokens over 16384 rows, 8 heads of 4, by blocks of 256: 606 to 627 us (0.88 to
+//   0.91 PFLOP/s, keys read once at 3.5 TB/s), by 128: 650; from keys that caches hold 520, as far as the power limit goes.
 //   The matrix products bound it: 4 x 128 operations per (query row, key).  So the weights of the first two shapes are
 //   rounded to bf16 (half a step, 2^-8, averaged over a row's keys); a second product with their tails, 16 bits in all,
 //   costs 20 to 40% (8192 tokens over 8192 rows 770 us with it, 566 without, 1024 over 131072 2930 / 2070, 1024 over 1024
@@ -82,11 +90,11 @@ __device__ __forceinline__ float max_halves(float x) {
 
 // RW waves of 32 query rows each, KG groups of them that take every KG'th tile of KEYS keys.  TREE: the new tokens see each
 // other by a mask.
-template <int RW, int KG, int KEYS, bool NT, bool TREE>
+template <int RW, int KG, int KEYS, bool NT, bool TREE, bool TAILS = (KG > 1)>
 __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
   constexpr int kWaves = RW * KG, kRows = 32 * RW;
   constexpr int kSub = KEYS / 32;             // blocks of 32 keys of a tile
-  constexpr bool kTails = KG > 1;             // weights as a bf16 head and a bf16 tail, not a head alone
+  constexpr bool kTails = TAILS;              // weights as a bf16 head and a bf16 tail, not a head alone
   constexpr int kPart = KEYS / RW;            // rows of a tile that a wave loads
   constexpr int kTile = KEYS * kRowBytes;     // bytes of a tile's K, or of its V
   constexpr int kStage = KG * 2 * kTile;
@@ -102,6 +110,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   __shared__ Range ranges[kWaves];
   __shared__ int bad_pages[kWaves];
   __shared__ float2 merged[KG > 1 ? KG : 1][kRows];  // maximum and total weight of a group's rows
+  constexpr int kMaskHeld = 4;
+  __shared__ uint64_t held_words[TREE ? kWaves : 1][32][kMaskHeld];
   const ebd_attend_paged_params &p = L.p;
   const int H = p.pages.kv_heads, G = p.group;
   // heads vary fastest (work-groups go round the XCDs: a head's stay together for 8, 4, 2 heads and
@@ -128,7 +138,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const bool sees = span[0].lo < span[0].hi;
   if (sq.held > sq.seen && __any(TREE ? tree_past_table(L, sq, row) : past_table(L, sq, row)) && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   Range R, all;
-  if (!TREE && !p.qpos) {
+  if (TREE && p.window == 0) {
+    all = tree_range_of(sq);
+    R = 32 * rw < nrow ? all : Range{0, 0, 0, 0};
+  } else if (!TREE && !p.qpos) {
     R = range_of_tokens(p, sq, token(row0 + 32 * rw), token(row0 + 32 * rw + 31));
     all = range_of_tokens(p, sq, token(row0), token(row0 + nrow - 1));
   } else {
@@ -193,8 +206,12 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const uint32_t tiles_at = lds_at(tiles);
   auto tile_of = [&](int stage) { return tiles_at + stage * kStage + kg * 2 * kTile; };  // this group's
   const int own_hi = min(span[0].hi, k_end);
-  // of a lane's row: whether it sees the keys k .. k + 31 inside its span
-  auto masked = [&](int k) { return mask_bits(L, sq, sq.t0 + token(min(row, row0 + nrow - 1)), k); };
+  // of a lane's row: whether it sees the keys k .. k + 31 inside its span; the first words of the wave's masks wait in LDS,
+  // since a load from memory would be waited for together with the tiles on their way
+  const int64_t mask_at = TREE ? (sq.t0 + token(min(row, row0 + nrow - 1))) * L.mask_words : 0;
+  auto masked = [&](int k) {
+    return mask_bits(L, sq, k, [&](int i) { return i < kMaskHeld ? held_words[wave][c][i] : L.mask[mask_at + i]; });
+  };
   uint32_t(*poison)[8] = poisons[wave];
   bool poisoned = false;
   f32x16 S[kSub];
@@ -358,6 +375,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       pg = page_of(k + step + kPart * rw);
     };
     load(k, 0);
+    if constexpr (TREE) {
+#pragma unroll
+      for (int i = half; i < kMaskHeld; i += 2) held_words[wave][c][i] = i < L.mask_words ? L.mask[mask_at + i] : 0;
+    }
     {
       // the wave's query rows come the same way, into the stage that is still free: whole rows, where operand loads
       // would gather 16 bytes from each
@@ -559,6 +580,11 @@ hipError_t launch_tiles(const AttendPagedLaunch &L, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attend_tiles(const AttendPagedLaunch &L, hipStream_t s) {
+  if (L.mask && L.rows == kTileRows && L.pairs) {
+    const dim3 grid((unsigned)attend_paged_groups(L));
+    hipLaunchKernelGGL((attend_tiles_kernel<4, 2, 64, false, true, false>), grid, dim3(512), 0, s, L);
+    return hipGetLastError();
+  }
   return L.mask ? launch_tiles<true>(L, s) : launch_tiles<false>(L, s);
 }
 

@@ -264,6 +264,7 @@ struct AttendPagedLaunch {
   float2 *stats;       // [groups, rows] their maximum and total weight
   const uint64_t *mask;  // [tokens, mask_words] which new tokens a token sees (NULL: all up to it)
   int32_t mask_words;
+  int32_t pairs;       // (with a mask) work-groups of 128 query rows whose eight waves take two tiles at a time
 };
 
 constexpr int kRowsWaves = 4;      // waves of an attend_rows work-group

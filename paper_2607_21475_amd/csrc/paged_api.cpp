@@ -111,12 +111,15 @@ constexpr int64_t kRowsLeast = 128;  // fewest rows of a split: a tile for each 
 constexpr int64_t kTilesLeast = 256;
 constexpr int64_t kStartRows = 320;
 constexpr int64_t kTilesStartRows = 640;
+constexpr double kPairsSpeed = 1.9, kLongSpeed = 1.09;  // of attend_tiles' shapes for trees
 constexpr double kTilesJoin = 250.0;  // (and a row for each 128 query rows' sums, 135 KB written and read)
 constexpr double kRowsJoin = 300.0;
 constexpr int64_t kSplitsMost = 256;
 constexpr int64_t kCacheBytes = (int64_t)64 << 20;
 
-int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start, double join, double join_each) {
+// (speed: keys that a work-group takes in the time of one; total: receives the cost)
+int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start, double join, double join_each,
+               double speed = 1.0, double *total = nullptr) {
   const int64_t most = std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least));
   int64_t best = 1;
   double cost = 0.0;
@@ -125,16 +128,17 @@ int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_
     const int64_t rows = ((span + ns - 1) / ns + 127) / 128 * 128;
     const int64_t groups = units * ((span + rows - 1) / rows);  // (rounded up, the size may leave fewer splits)
     const double rounds = groups <= 2 * slots ? (double)((groups + slots - 1) / slots) : (double)groups / (double)slots + 0.5;
-    const double c = rounds * (double)(rows + start) + (ns > 1 ? join + join_each * (double)groups : 0.0);
+    const double c = rounds * ((double)rows / speed + (double)start) + (ns > 1 ? join + join_each * (double)groups : 0.0);
     if (i == 0 || c < cost) best = ns, cost = c;
   }
+  if (total) *total = cost;
   return best;
 }
 
 // A launch for blocks of `rows` query rows; `sum` query rows in all, the sequences' most `rows_max` each, and each of those
 // that it takes more than `more_than`.
 AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, bool tree, int32_t rows, int64_t rows_max,
-                                    int64_t sum, int64_t more_than = 0) {
+                                    int64_t sum, int64_t more_than = 0, bool pairs = false, double *cost = nullptr) {
   AttendPagedLaunch L{};
   L.p = *p;
   L.rows = rows;
@@ -152,11 +156,21 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, bool tree,
   L.units = L.blocks ? S * aside : counted;
   // the most rows a block of query rows sees, under a window from a tile's border on
   int64_t span = p->max_rows;
-  if (p->window > 0 && !p->qpos) span = std::min<int64_t>(span, (int64_t)p->window + (tree ? p->max_new : rows / p->group) + 1);
+  // (of a tree's tokens, whose positions are theirs to say, the rows that they see if these lie behind the held rows)
+  if (p->window > 0 && (tree || !p->qpos))
+    span = std::min<int64_t>(span, (int64_t)p->window + (tree ? p->max_new : rows / p->group) + 1);
   span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
-  const int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
+  int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
+  // (a tree's blocks all see to their sequence's end: one more than fill a round costs another, so that the ones that are
+  // not full are counted, half a sequence each)
+  if (tree && !L.blocks) full = std::min<int64_t>(L.units, sum / rows + (S + 1) / 2);
   L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
-  if (tiles) {
+  if (tiles && tree) {
+    const double speed = pairs ? kPairsSpeed : rows == kTileRows ? 1.0 : kLongSpeed;
+    L.pairs = pairs;
+    L.nsplit = (int32_t)splits(full * H, span, rows == kTileRows && !pairs ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows,
+                               kTilesJoin, (double)rows / kTileRows, speed, cost);
+  } else if (tiles) {
     L.nsplit = (int32_t)splits(full * H, span, rows == kTileRows ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows,
                                kTilesJoin, (double)rows / kTileRows);
   } else {
@@ -191,11 +205,30 @@ struct AttendPagedPlan {
 // 2048 over 16384 513 / 504, 512 over 4096 61 / 60; not taken: 8192 over 8192 571 / 567, 2048 over 8192 257 / 265, 1500
 // over 6000 167 / 180, 256 over 1024 30 / 35, 160 (a block half empty) over 32768 122 / 130; 8 ragged sequences of up to
 // 256 over up to 16384 320 / 420.
-bool long_blocks(const ebd_attend_paged_params *p, bool tree, int64_t most) {
+bool long_blocks(const ebd_attend_paged_params *p, int64_t most) {
   if (p->pages.num_seqs != 1 || most < kLongRows || (int64_t)p->max_new * 8 > p->max_rows) return false;
-  const AttendPagedLaunch L = attend_paged_part(p, tree, kLongRows, most, std::min<int64_t>(p->num_tokens * p->group, most));
+  const AttendPagedLaunch L = attend_paged_part(p, false, kLongRows, most, std::min<int64_t>(p->num_tokens * p->group, most));
   const int64_t groups = attend_paged_groups(L), rows = (most + kLongRows - 1) / kLongRows * kLongRows;
   return groups <= kCus && 8 * groups >= 7 * kCus && 8 * most >= 7 * rows;
+}
+// The shape of a tree's blocks of 128 query rows or more: two work-groups of 128 rows a CU (A), one of 128 rows by eight waves
+// that takes two tiles at a time (B), or one of 256 rows (C, where these are full).  By the cost of each, in which A's two take
+// a key each in the time of one, B's two keys and C's one and a little (it loads every key for twice as many rows).  All
+// blocks of a tree see to its end, so that short launches are alike and nothing ends early beside a longer one.
+// us of A / B / C with their best splits, 8 KV heads of 4 query heads unless said: one sequence, 64 tokens over 4096 rows
+// 25.7 / 24.1 / 28.1, over 32768 66.7 / 51.5 / 73.4; 128 over 16384 55.9 / 51.7 / 53.4; 16 of 48 over 4096 100 / 82 / -;
+// 8 of 32 over 8192 69 / 60 / -; four of up to 300, 4 heads of 7, under a window of 2048 58.6 / 51.6 / 58.1; 24 of 64 over
+// 4096 155 / 164 / 129; 32 of 64 over 8192 340 / 337 / 310; 64 of 64 over 4096 355 / 355 / 316; 64 of 30 over 2048 118 /
+// 124 / -.
+AttendPagedLaunch tree_part(const ebd_attend_paged_params *p, int64_t rows_max, int64_t sum, int64_t more_than) {
+  double a = 0.0, b = 0.0, c = 0.0;
+  AttendPagedLaunch L = attend_paged_part(p, true, kTileRows, rows_max, sum, more_than, false, &a);
+  const AttendPagedLaunch B = attend_paged_part(p, true, kTileRows, rows_max, sum, more_than, true, &b);
+  if (b < a) L = B, a = b;
+  const int64_t S = p->pages.num_seqs, aside = (rows_max + kLongRows - 1) / kLongRows;
+  if (8 * rows_max < 7 * aside * kLongRows || 8 * sum < 7 * S * aside * kLongRows) return L;
+  const AttendPagedLaunch C = attend_paged_part(p, true, kLongRows, rows_max, sum, more_than, false, &c);
+  return c < a ? C : L;
 }
 AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p, bool tree = false) {
   const int64_t S = p->pages.num_seqs, G = p->group, most = (int64_t)p->max_new * G;
@@ -208,9 +241,11 @@ AttendPagedPlan attend_paged_plan(const ebd_attend_paged_params *p, bool tree = 
     plan.parts = 2;
     plan.part[1] = attend_paged_part(p, tree, small, small, S * small);
     plan.part[1].at_most = small;
-    plan.part[0] = attend_paged_part(p, tree, rows, most, sum, small);
-  } else if (long_blocks(p, tree, most)) {
-    plan.part[0] = attend_paged_part(p, tree, kLongRows, most, sum);
+    plan.part[0] = tree ? tree_part(p, most, sum, small) : attend_paged_part(p, false, rows, most, sum, small);
+  } else if (tree && rows == kTileRows) {
+    plan.part[0] = tree_part(p, most, sum, 0);
+  } else if (long_blocks(p, most)) {
+    plan.part[0] = attend_paged_part(p, false, kLongRows, most, sum);
   } else {
     plan.part[0] = attend_paged_part(p, tree, rows, most, sum);
   }

@@ -93,6 +93,8 @@ CASES = [
     ([6000] * 4, [4] * 4, 8, 4, 64, "heads", 0, "tree", 1, True),
     ([6000] * 4, [8] * 4, 8, 4, 64, "heads", 0, "tree", 1, True),
     ([6000] * 4, [15] * 4, 8, 4, 64, "heads", 0, "tree", 1, True),
+    ([600] * 24, [64] * 24, 8, 4, 64, "heads", 0, "tree", 1, True),   # (blocks of 256 query rows)
+    ([300] * 64, [30] * 64, 8, 4, 16, "tokens", 0, "tree", 1, True),  # (two work-groups of 128 a CU)
 ]
 
 
