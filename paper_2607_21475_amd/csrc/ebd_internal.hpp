@@ -183,7 +183,7 @@ struct NormRopeLaunch {
   ebd_norm_rope_params p;  // amplitude resolved
   const uint16_t *x;
   uint16_t *y;
-  int32_t per, tpb;
+  int32_t shift;  // 2^shift waves a token
 };
 
 struct NormRopeBackwardLaunch {
@@ -203,7 +203,7 @@ struct AppendNormLaunch {
   uint16_t *K, *V, *q_out;
   uint32_t *status;
   int32_t shift;
-  int32_t per, tpb;
+  int32_t waves;  // 2^waves of a token
 };
 
 struct PlanStepLaunch {

@@ -9,6 +9,12 @@
 // Eight lanes take a row, 16 elements each: as the rotation pairs them (rope_device.hpp), so that norm, rotation and
 // gradients stay in registers and a row's sums are three exchanges between neighbouring lanes.  All steps are fp32, and an
 // output is rounded once.  Each row is read and written once: memory bounds large calls, a chain of loads small ones.
+//
+// Forward, a wave takes a token, eight of its rows at a time and the next eight on their way, or (few tokens) a share of its
+// rows: it makes the token's sines itself, a pair a lane, and finds the token's place itself, so that waves never wait for
+// each other, and both cost one wave's instructions whatever the rows.  (A work-group a token, a wave for each eight rows and
+// the sines shared behind a barrier, issues twice the instructions: 8191 tokens of 40 rows 34.4 us, so 33.0; 5.1 TB/s, of 32
+// rows with shared weights 24 us, 5.5 TB/s, the rate of a copy.)
 #include "ebd.h"
 #include "ebd_internal.hpp"
 #include "rope_device.hpp"
@@ -24,9 +30,10 @@ struct Part {
 
 // As split_row, but where halves are no whole chunks, each lane takes neighbouring ones, and the pairs meet in LDS.
 __device__ __forceinline__ Split part_of(const ebd_rotary &R, int l, bool rotated) {
-  Split sp = split_row(R, l, rotated);
-  if (sp.how == kOdd) sp.e0 = 16 * l, sp.e1 = 16 * l + 8;
-  return sp;
+  const bool half = rotated && R.freq && R.layout == EBD_ROPE_HALF, whole = R.rot_dim % 16 == 0;
+  const bool pairs = half && whole && 16 * l < R.rot_dim;
+  const int how = !rotated || !R.freq ? kCopy : !half ? kPairs : !whole ? kOdd : pairs ? kHalf : kCopy;
+  return {how, pairs ? 8 * l : 16 * l, pairs ? R.rot_dim / 2 + 8 * l : 16 * l + 8};
 }
 
 __device__ __forceinline__ void unpack8(const uint4 &v, float (&x)[8]) {
@@ -37,10 +44,14 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float (&x)[8]) {
 __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
-__device__ __forceinline__ Part load_row(const Split &S, const uint16_t *p) {
+struct Raw {
+  uint4 a, b;
+};
+__device__ __forceinline__ Raw load_raw(const Split &S, const uint16_t *p) { return {load16(p + S.e0), load16(p + S.e1)}; }
+__device__ __forceinline__ Part unpack(const Raw &r) {
   Part x;
-  unpack8(load16(p + S.e0), x.a);
-  unpack8(load16(p + S.e1), x.b);
+  unpack8(r.a, x.a);
+  unpack8(r.b, x.b);
   return x;
 }
 __device__ __forceinline__ void store_part(const Split &S, uint16_t *p, const Part &x) {
@@ -91,25 +102,30 @@ __device__ __forceinline__ float normalise(Part &x, float eps) {
   return r * scale;
 }
 
-// The pairs of a lane's part of a row turned; SIGN -1: back.  `row`: the row's place in LDS, of 128 elements, for pairs that
-// lie in different lanes (which are those of one wave).
+// The pairs of a lane's part of a row turned; SIGN -1: back.  t: the part's pairs; cs: all of the token's, for rows whose
+// pairs lie in different lanes (those of one wave): they meet in LDS, at `row`.
 template <bool ODD, int SIGN>
-__device__ __forceinline__ void turn_part(const ebd_rotary &R, const Split &S, Part &x, const float2 *cs, float *row) {
-  auto pair = [&](float &u, float &v, const float2 &t) {
-    const float c = t.x, s = SIGN * t.y, y = u * c - v * s;
-    v = v * c + u * s;
-    u = y;
+__device__ __forceinline__ void turn_part(const ebd_rotary &R, const Split &S, Part &x, const float2 (&t)[8],
+                                          const float2 *cs, float *row) {
+  // (by value: from references the compiler makes addresses)
+  auto pair = [](float u, float v, float2 t) {
+    const float s = SIGN * t.y;
+    return make_float2(u * t.x - v * s, v * t.x + u * s);
   };
   const int n = R.rot_dim / 2;
   if (S.how == kHalf) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pair(x.a[i], x.b[i], cs[S.e0 + i]);
+    for (int i = 0; i < 8; ++i) {
+      const float2 y = pair(x.a[i], x.b[i], t[i]);
+      x.a[i] = y.x, x.b[i] = y.y;
+    }
   } else if (S.how == kPairs) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int u = S.e0 / 2 + i, v = u + 4;
-      if (u < n) pair(x.a[2 * i], x.a[2 * i + 1], cs[u]);
-      if (v < n) pair(x.b[2 * i], x.b[2 * i + 1], cs[v]);
+      const float2 y = pair(x.a[2 * i], x.a[2 * i + 1], t[i]), z = pair(x.b[2 * i], x.b[2 * i + 1], t[i + 4]);
+      x.a[2 * i] = u < n ? y.x : x.a[2 * i], x.a[2 * i + 1] = u < n ? y.y : x.a[2 * i + 1];
+      x.b[2 * i] = v < n ? z.x : x.b[2 * i], x.b[2 * i + 1] = v < n ? z.y : x.b[2 * i + 1];
     }
   }
   if constexpr (ODD) {
@@ -138,37 +154,68 @@ __device__ __forceinline__ void multiply(Part &x, const Part &w) {
 }
 
 constexpr int kOddRow = kHeadDim + 4;  // a row in LDS, padded
+constexpr int kForwardWaves = 4;       // waves of a work-group, which have nothing to do with each other
+typedef __attribute__((address_space(4))) int32_t const_i32;  // read through the scalar cache
+typedef __attribute__((address_space(4))) int64_t const_i64;
 
 }  // namespace
 
+// A wave's token and its share of the token's rows: every `waves`'th block of eight, from `part` on.
+struct Share {
+  int64_t t;
+  int part, waves;
+};
+__device__ __forceinline__ Share share_of(int shift) {
+  const uint32_t w = blockIdx.x * kForwardWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  return {(int64_t)(w >> shift), (int)(w & ((1u << shift) - 1u)), 1 << shift};
+}
+
+// The wave's sines: pair i by lane i, then the eight pairs of a lane's part (8 l .. 8 l + 7 in both layouts).
+__device__ __forceinline__ void make_turns(const ebd_rotary &R, int64_t pos, float2 *cs, float2 (&t)[8]) {
+  const int lane = threadIdx.x & 63;
+  if (lane < R.rot_dim / 2) cs[lane] = turn(R, lane, pos);
+  wave_sync();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = cs[8 * (lane & 7) + i];  // (those past the last pair are not used)
+}
+
 template <bool ODD>
-__global__ __launch_bounds__(8 * kRopeRows) void norm_rope_kernel(NormRopeLaunch L) {
-  __shared__ float2 cs[4][kHeadDim / 2];
-  __shared__ float rows[ODD ? kRopeRows : 1][kOddRow];
+__global__ __launch_bounds__(64 * kForwardWaves) void norm_rope_kernel(NormRopeLaunch L) {
+  __shared__ float2 cs[kForwardWaves][kHeadDim / 2];
+  __shared__ float rows[ODD ? 8 * kForwardWaves : 1][kOddRow];
   const ebd_norm_rope_params &p = L.p;
-  const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per, l = i % 8, n = p.rot.rot_dim / 2;
-  const int64_t t = token_group(blockIdx.x, blockIdx.z) * L.tpb + slot;
-  const int h = blockIdx.y * kRopeRows + i / 8;
-  const bool live = t < p.num_tokens && h < p.num_heads;
+  const Share w = share_of(L.shift);
+  if (w.t >= p.num_tokens) return;
+  const int wave = threadIdx.x >> 6, l = threadIdx.x & 7, r0 = (threadIdx.x >> 3) & 7;
   const Split sp = part_of(p.rot, l, true);
-  Part x = {}, w = {};
-  if (live) {
-    x = load_row(sp, L.x + t * p.x.token_stride + h * p.x.head_stride);
-    w = load_weights(sp, p.norm.weight + h * p.norm.head_stride);
+  const uint16_t *x0 = L.x + w.t * p.x.token_stride;
+  uint16_t *y0 = L.y + w.t * p.y.token_stride;
+  float *odd = rows[ODD ? threadIdx.x >> 3 : 0];
+  int h = 8 * w.part + r0;
+  Raw x = {}, next = {};
+  Part g = {};
+  if (h < p.num_heads) {
+    x = load_raw(sp, x0 + h * p.x.head_stride);
+    g = load_weights(sp, p.norm.weight + h * p.norm.head_stride);
   }
-  if (t < p.num_tokens && p.rot.freq && i < n) cs[slot][i] = turn(p.rot, i, p.pos[t]);
-  __syncthreads();
-  if (!live) return;
-  normalise(x, p.norm.eps);
-  multiply(x, w);
-  turn_part<ODD, 1>(p.rot, sp, x, cs[slot], rows[ODD ? threadIdx.x / 8 : 0]);
-  store_part(sp, L.y + t * p.y.token_stride + h * p.y.head_stride, x);
+  float2 t[8] = {};
+  if (p.rot.freq) make_turns(p.rot, ((const const_i32 *)p.pos)[w.t], cs[wave], t);
+  for (; h - r0 < p.num_heads; h += 8 * w.waves, x = next) {
+    const int after = h + 8 * w.waves;
+    if (after < p.num_heads) next = load_raw(sp, x0 + after * p.x.head_stride);
+    Part v = unpack(x);
+    normalise(v, p.norm.eps);
+    multiply(v, g);
+    if (p.norm.head_stride && after < p.num_heads) g = load_weights(sp, p.norm.weight + after * p.norm.head_stride);
+    turn_part<ODD, 1>(p.rot, sp, v, t, cs[wave], odd);
+    if (h < p.num_heads) store_part(sp, y0 + h * p.y.head_stride, v);
+  }
 }
 
 constexpr int kBackwardRows = 64;  // (128 of them leave too few registers)
 
 // A work-group takes every gridDim.x'th group of tokens; a thread's head stays the same, so that its share of dw waits in
-// registers.  Shared weights: the work-group's rows are added up (within a wave, then through LDS) and leave one row of
+// registers; the next group's rows are on their way meanwhile.  Shared weights: the work-group's rows are added up (within a wave, then through LDS) and leave one row of
 // sums; weights of each head's own: each token slot leaves a row for every head.
 template <bool ODD, bool SHARED>
 __global__ __launch_bounds__(8 * kBackwardRows) void norm_rope_backward_kernel(NormRopeBackwardLaunch L) {
@@ -182,19 +229,27 @@ __global__ __launch_bounds__(8 * kBackwardRows) void norm_rope_backward_kernel(N
   Part w = {}, dw = {};
   if (h < p.num_heads) w = load_weights(sp, p.norm.weight + h * p.norm.head_stride);
   int par = 0;
+  Raw x0 = {}, d0 = {};  // the rows of the token after this one's, on their way
+  auto ask = [&](int64_t g) {
+    const int64_t t = g * L.tpb + slot;
+    if (t >= p.num_tokens || h >= p.num_heads) return;
+    x0 = load_raw(sp, L.x + t * p.x.token_stride + h * p.x.head_stride);
+    d0 = load_raw(sp, L.dy + t * p.dy.token_stride + h * p.dy.head_stride);
+  };
+  ask(blockIdx.x);
   for (int64_t g = blockIdx.x; g * L.tpb < p.num_tokens; g += gridDim.x, par ^= 1) {
     const int64_t t = g * L.tpb + slot;
     const bool live = t < p.num_tokens && h < p.num_heads;
-    Part x = {}, d = {};
-    if (live) {
-      x = load_row(sp, L.x + t * p.x.token_stride + h * p.x.head_stride);
-      d = load_row(sp, L.dy + t * p.dy.token_stride + h * p.dy.head_stride);
-    }
+    Part x = unpack(x0), d = unpack(d0);
+    if ((g + gridDim.x) * L.tpb < p.num_tokens) ask(g + gridDim.x);
     if (t < p.num_tokens && p.rot.freq && i < n) cs[par][slot][i] = turn(p.rot, i, p.pos[t]);
     __syncthreads();  // (the other half is written by the next group's tokens, which every wave reaches after this one's)
     if (live) {
       const float r = normalise(x, p.norm.eps);
-      turn_part<ODD, -1>(p.rot, sp, d, cs[par][slot], rows[ODD ? threadIdx.x / 8 : 0]);
+      float2 tt[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) tt[k] = cs[par][slot][8 * l + k];
+      turn_part<ODD, -1>(p.rot, sp, d, tt, cs[par][slot], rows[ODD ? threadIdx.x / 8 : 0]);
       float m = 0.0f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -269,68 +324,110 @@ __global__ __launch_bounds__(1024) void norm_rope_join_kernel(NormRopeBackwardLa
   L.dweight[(int64_t)h * kHeadDim + threadIdx.x] = (float)all;
 }
 
-// Rows of a token in order: its keys, its queries, its values.
+// Blocks of eight rows of a token in order: of its keys, its queries, its values.  A block holds rows of one kind, so that
+// the kind, its pointers and strides are the wave's, not the lanes' (blocks of neighbouring rows whatever their kind: 8192
+// tokens, 8 KV heads of 4 query heads, 53 us, so 41; a barrier and a wave
+// for each block 54).
 template <bool ODD>
-__global__ __launch_bounds__(8 * kRopeRows) void append_norm_kernel(AppendNormLaunch L) {
-  __shared__ float2 cs[4][kHeadDim / 2];
-  __shared__ float rows[ODD ? kRopeRows : 1][kOddRow];
+__global__ __launch_bounds__(64 * kForwardWaves) void append_norm_kernel(AppendNormLaunch L) {
+  __shared__ float2 cs[kForwardWaves][kHeadDim / 2];
+  __shared__ float rows[ODD ? 8 * kForwardWaves : 1][kOddRow];
   const ebd_append_paged_params &p = L.p.append;
-  const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per, l = i % 8, n = p.rot.rot_dim / 2;
-  const int64_t t = token_group(blockIdx.x, blockIdx.z) * L.tpb + slot;
-  const int row = blockIdx.y * kRopeRows + i / 8;
-  const int kv = p.pages.kv_heads, S = p.pages.num_seqs;
-  const bool isk = row < kv, isq = !isk && row < kv + p.q_heads;
-  const bool here = t < p.num_tokens && row < 2 * kv + p.q_heads;
-  const int h = isk ? row : (isq ? row - kv : row - kv - p.q_heads);
-  const Split sp = part_of(p.rot, l, isk || isq);
-  const ebd_rows &in = isq ? p.q_rows : (isk ? p.k_rows : p.v_rows);
-  const ebd_norm &norm = isq ? L.p.q_norm : L.p.k_norm;
-  const bool normed = (isk || isq) && norm.weight;
-  Part x = {}, w = {};
-  if (here) {  // asked for before the token's place is known
-    x = load_row(sp, (isq ? L.q : (isk ? L.k_new : L.v_new)) + t * in.token_stride + h * in.head_stride);
-    if (normed) w = load_weights(sp, norm.weight + h * norm.head_stride);
-  }
-  // the wave's token: its place
-  bool live = here;
-  int64_t base = -1;
+  const Share w = share_of(L.waves);
+  if (w.t >= p.num_tokens) return;
+  const int wave = threadIdx.x >> 6, l = threadIdx.x & 7, r0 = (threadIdx.x >> 3) & 7;
+  const int kv = p.pages.kv_heads, nk = (kv + 7) / 8, nq = (p.q_heads + 7) / 8, blocks = 2 * nk + nq;
+  float *odd = rows[ODD ? threadIdx.x >> 3 : 0];
+  const Split turned = part_of(p.rot, l, true), copied = {kCopy, 16 * l, 16 * l + 8};
+  enum { kKey, kQuery, kValue };
+  auto kind_of = [&](int b) { return b < nk ? kKey : b < nk + nq ? kQuery : kValue; };
+  auto head_of = [&](int b) { return 8 * (b < nk ? b : b < nk + nq ? b - nk : b - nk - nq) + r0; };
+  auto load = [&](int b) -> Raw {
+    const int kind = kind_of(b), h = head_of(b);
+    const ebd_rows &in = kind == kKey ? p.k_rows : kind == kQuery ? p.q_rows : p.v_rows;
+    const uint16_t *x = (kind == kKey ? L.k_new : kind == kQuery ? L.q : L.v_new) + w.t * in.token_stride;
+    if (h >= (kind == kQuery ? p.q_heads : kv)) return {};
+    return load_raw(kind == kValue ? copied : turned, x + h * in.head_stride);
+  };
+  auto weights = [&](int b) -> Part {  // (asked for with the rows: behind them, a wait would be one for the next rows, too)
+    const int kind = kind_of(b), h = head_of(b);
+    const ebd_norm &norm = kind == kKey ? L.p.k_norm : L.p.q_norm;
+    if (kind == kValue || !norm.weight || h >= (kind == kQuery ? p.q_heads : kv)) return {};
+    return load_weights(turned, norm.weight + h * norm.head_stride);
+  };
+  Raw x = {}, next = {};
+  Part g = {}, next_g = {};
+  int b = w.part;
+  if (b < blocks) x = load(b), g = weights(b);  // asked for before the token's place is known
+  int64_t base = -1, pos = 0;
   if (L.p.slots) {
-    const int64_t at = t < p.num_tokens ? L.p.slots[t] : -1;
-    live &= at >= 0 && (at >> L.shift) < p.pages.num_pages;
-    if (t < p.num_tokens && p.rot.freq && i < n) cs[slot][i] = turn(p.rot, i, p.pos[t]);
+    const int64_t at = ((const const_i64 *)L.p.slots)[w.t];
+    if (at < 0 || (at >> L.shift) >= p.pages.num_pages) return;
     base = (at >> L.shift) * p.pages.page_stride + (at & (p.pages.page_size - 1)) * p.pages.row_stride;
-    if (!live) base = -1;
   } else {
-    const int s = t < p.num_tokens ? find_seq(p.new_off, S, t) : -1;
-    live &= s >= 0;
-    if (s >= 0) {
-      const int64_t r = (int64_t)p.len[s] - p.new_off[s + 1] + t;
-      if (p.rot.freq && i < n) cs[slot][i] = turn(p.rot, i, p.pos ? p.pos[t] : r);
-      base = page_row(p.pages, L.shift, s, r);
-      if (base < 0 && i == 0 && blockIdx.y == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+    const int s = __builtin_amdgcn_readfirstlane(find_seq(p.new_off, p.pages.num_seqs, w.t));
+    if (s < 0) return;
+    pos = (int64_t)((const const_i32 *)p.len)[s] - ((const const_i64 *)p.new_off)[s + 1] + w.t;
+    const int64_t e = pos >> L.shift;  // (as page_row, by scalar loads)
+    const int pg = pos >= 0 && e < p.pages.max_pages
+                       ? ((const const_i32 *)p.pages.page_table)[(int64_t)s * p.pages.max_pages + e] : -1;
+    if ((uint32_t)pg < (uint32_t)p.pages.num_pages)
+      base = pg * p.pages.page_stride + (pos & (p.pages.page_size - 1)) * p.pages.row_stride;
+    else if (w.part == 0 && (threadIdx.x & 63) == 0 && L.status)
+      atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  }
+  float2 t[8] = {};
+  if (p.rot.freq) make_turns(p.rot, p.pos ? (int64_t)((const const_i32 *)p.pos)[w.t] : pos, cs[wave], t);
+  for (; b < blocks; b += w.waves, x = next, g = next_g) {
+    if (b + w.waves < blocks) next = load(b + w.waves), next_g = weights(b + w.waves);
+    const int kind = kind_of(b), h = head_of(b);
+    if (kind != kQuery && base < 0) continue;
+    const bool here = h < (kind == kQuery ? p.q_heads : kv);
+    if (kind == kValue) {
+      uint16_t *y = L.V + base + h * p.pages.head_stride;
+      if (here) store16(y + copied.e0, x.a), store16(y + copied.e1, x.b);
+      continue;
     }
+    const ebd_norm &norm = kind == kKey ? L.p.k_norm : L.p.q_norm;
+    Part v = unpack(x);
+    if (norm.weight) {
+      normalise(v, norm.eps);
+      multiply(v, g);
+    }
+    turn_part<ODD, 1>(p.rot, turned, v, t, cs[wave], odd);
+    if (here)
+      store_part(turned, kind == kKey ? L.K + base + h * p.pages.head_stride
+                                      : L.q_out + w.t * p.q_out_rows.token_stride + h * p.q_out_rows.head_stride, v);
   }
-  __syncthreads();
-  if (!live || (!isq && base < 0)) return;
-  uint16_t *y = isq ? L.q_out + t * p.q_out_rows.token_stride + h * p.q_out_rows.head_stride
-                    : (isk ? L.K : L.V) + base + h * p.pages.head_stride;
-  if (normed) {
-    normalise(x, norm.eps);
-    multiply(x, w);
-  }
-  turn_part<ODD, 1>(p.rot, sp, x, cs[slot], rows[ODD ? threadIdx.x / 8 : 0]);
-  store_part(sp, y, x);
 }
 
 namespace {
 bool odd(const ebd_rotary &R) { return R.freq && R.layout == EBD_ROPE_HALF && R.rot_dim % 16; }
+// us with the join, by 256 / 512 / 768 / 1024 work-groups: 8191 tokens of 40 rows, weights of their own 72.5 / 55.2 / 65.7 /
+// 76.2 (more partial sums; without the rows on their way 60 by 512), of 32 with shared ones 68.2 / 46.0 / 43.1 / 43.3, 2048
+// of 32 22.0 / 18.1 / 18.0 / 19.1
 constexpr int64_t kBackwardGroups = 512;
 constexpr int64_t kBackwardChain = 256;  // most token groups of a work-group: as many fp32 additions in a row
 }  // namespace
 
+// Waves of a token (their logarithm): one where the tokens are enough to fill the chip, else as many as there are blocks of
+// eight rows, or as fill it.
+// us by one wave a token below / at / above the line: norms of 8191 tokens of 32 rows 23.6 / 24.8, 2048 of 32 - / 7.6 / 8.0;
+// appends, whose waves each find the token's place, of 8192 tokens of 48 rows 41.8 / 41.4 / 40.3, of 2000 of 36 rows
+// 12.0 / 13.4 / 18.3.
+constexpr int64_t kNormFill = 4096, kAppendFill = 2048;
+int32_t forward_shift(int64_t tokens, int64_t rows, int64_t fill) {
+  int32_t s = 0;
+  while ((tokens << s) < fill && (8 << s) < rows) ++s;
+  return s;
+}
+dim3 forward_grid(int64_t tokens, int32_t shift) {
+  return dim3((unsigned)(((tokens << shift) + kForwardWaves - 1) / kForwardWaves));
+}
+
 hipError_t launch_norm_rope(NormRopeLaunch L, hipStream_t s) {
-  cut_tokens(L.p.num_heads, &L.per, &L.tpb);
-  const dim3 grid = rope_grid(L.p.num_tokens, L.p.num_heads, L.tpb), block(L.per * L.tpb);
+  L.shift = forward_shift(L.p.num_tokens, L.p.num_heads, kNormFill);
+  const dim3 grid = forward_grid(L.p.num_tokens, L.shift), block(64 * kForwardWaves);
   if (odd(L.p.rot)) hipLaunchKernelGGL(norm_rope_kernel<true>, grid, block, 0, s, L);
   else hipLaunchKernelGGL(norm_rope_kernel<false>, grid, block, 0, s, L);
   return hipGetLastError();
@@ -369,9 +466,8 @@ hipError_t launch_norm_rope_join(const NormRopeBackwardLaunch &L, hipStream_t s)
 
 hipError_t launch_append_norm(AppendNormLaunch L, hipStream_t s) {
   const ebd_append_paged_params &p = L.p.append;
-  const int64_t rows = 2 * (int64_t)p.pages.kv_heads + p.q_heads;
-  cut_tokens(rows, &L.per, &L.tpb);
-  const dim3 grid = rope_grid(p.num_tokens, rows, L.tpb), block(L.per * L.tpb);
+  L.waves = forward_shift(p.num_tokens, 8 * (2 * ((p.pages.kv_heads + 7) / 8) + (int64_t)(p.q_heads + 7) / 8), kAppendFill);
+  const dim3 grid = forward_grid(p.num_tokens, L.waves), block(64 * kForwardWaves);
   if (odd(p.rot)) hipLaunchKernelGGL(append_norm_kernel<true>, grid, block, 0, s, L);
   else hipLaunchKernelGGL(append_norm_kernel<false>, grid, block, 0, s, L);
   return hipGetLastError();
