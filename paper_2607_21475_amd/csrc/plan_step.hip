@@ -5,9 +5,10 @@
 // pages of ended sequences go behind the ring's last.  Then token j's slot is its row's page times P and the row's place in
 // it, its position first + j, or first + its depth in a tree, whose mask is its own bit and its parent's mask.
 //
-// Three launches, each of which needs all that the one before it found: plan_count (a wave per sequence: what it needs
-// and gives back), plan_fill (a wave per sequence: sums over the sequences before it, its entries), plan_tokens (a thread per
-// token) or plan_trees (a work-group per sequence, its parents in LDS, where each token walks up to its root).
+// Few sequences: one launch (plan_one).  Others: three, each of which needs all that the one before it found: plan_count (a
+// wave per sequence: what it needs and gives back), plan_fill (a wave per sequence: sums over the sequences before it, its
+// entries), plan_tokens (a thread per token) or plan_trees (a work-group per sequence, its parents in LDS, where each token
+// walks up to its root).  Latency bounds all of it: 512 sequences and 66 thousand tokens, 1.1 MB read and written, 18.6 us.
 #include "ebd.h"
 #include "ebd_internal.hpp"
 #include "paged_device.hpp"
@@ -70,12 +71,83 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t x) {
   return x;
 }
 
+// f(entry, its page, whether there is such an entry) for the entries e0 .. e1 - 1 of a sequence, in order, 64 at a time by a
+// wave's lanes, 512 of them in flight (512 sequences, of which 20 with 2049 entries have ended: 29.4 us in all one by one, 18.6
+// so).
+template <class F>
+__device__ __forceinline__ void scan(const int32_t *row, int e0, int e1, const F &f) {
+  constexpr int kFlight = 8;
+  const int lane = threadIdx.x & 63;
+  for (int base = e0; base < e1; base += 64 * kFlight) {
+    int pg[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const int e = base + 64 * k + lane;
+      pg[k] = -1;
+      if (e < e1) pg[k] = row[e];
+    }
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      if (base + 64 * k < e1) f(base + 64 * k + lane, pg[k], base + 64 * k + lane < e1);
+  }
+}
+
 // Slot of row `row` of sequence s, or -1.
 __device__ __forceinline__ int64_t slot_of(const ebd_plan_step_params &p, int shift, int s, int row) {
   const int e = row >> shift;
   if (e >= p.max_pages) return -1;
   const int pg = p.page_table[(int64_t)s * p.max_pages + e];
   return in_pool(p, pg) ? ((int64_t)pg << shift) + (row & (p.page_size - 1)) : -1;
+}
+
+// A wave fills sequence s's entries: holes from the ring's `take`'th page on, or (n < 0: ended) its pages to the ring, from
+// the `back`'th place behind its last; whether a hole is left.
+__device__ __forceinline__ bool fill(const ebd_plan_step_params &p, const FreePages &f, int s, int n, int first, int shift,
+                                     int64_t take, int64_t back) {
+  const uint64_t below = (1ull << (threadIdx.x & 63)) - 1;
+  int32_t *row = p.page_table + (int64_t)s * p.max_pages;
+  if (n < 0) {
+    scan(row, 0, p.max_pages, [&](int e, int pg, bool here) {
+      const uint64_t has = __ballot(here && in_pool(p, pg));
+      const int64_t at = f.count + back + __popcll(has & below);
+      if (here && in_pool(p, pg) && at < p.num_pages) p.free_pages[ring_at(p, f.head, at)] = pg;
+      if (here && pg != -1) row[e] = -1;
+      back += __popcll(has);
+    });
+    return false;
+  }
+  bool none = false;
+  if (n > 0) {
+    scan(row, first >> shift, min(((first + n - 1) >> shift) + 1, p.max_pages), [&](int e, int pg, bool here) {
+      const bool hole = here && !in_pool(p, pg);
+      const uint64_t holes = __ballot(hole);
+      const int64_t at = take + __popcll(holes & below);
+      if (hole && at < f.count) row[e] = p.free_pages[ring_at(p, f.head, at)];
+      none |= hole && at >= f.count;
+      take += __popcll(holes);
+    });
+  }
+  return __any(none);
+}
+
+// The state behind the step.
+__device__ __forceinline__ void finish(const ebd_plan_step_params &p, const FreePages &f, int64_t take, int64_t back) {
+  const int64_t taken = min(take, (int64_t)f.count);
+  p.free_state[0] = ring_at(p, f.head, taken);
+  p.free_state[1] = (int)min(f.count - taken + back, (int64_t)p.num_pages);
+}
+
+// Position and mask of token j of a tree, whose parents are in LDS; its depth.
+__device__ __forceinline__ int walk(const int32_t *parent, int j, uint64_t *mask, int W) {
+  // words from the last down to the one a bit falls into are finished: parents come before their children
+  int w = W - 1, depth = 0;
+  uint64_t bits = 0;
+  for (int i = j; i >= 0; i = parent[i], ++depth) {
+    for (; w > i >> 6; --w, bits = 0) mask[w] = bits;
+    bits |= 1ull << (i & 63);
+  }
+  for (; w >= 0; --w, bits = 0) mask[w] = bits;
+  return depth - 1;
 }
 
 }  // namespace
@@ -92,7 +164,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanStepLaunch
   const int32_t *row = p.page_table + (int64_t)s * p.max_pages;
   const int e0 = q.n < 0 ? 0 : q.e0, e1 = q.n < 0 ? p.max_pages : q.e1;
   int found = 0;  // entries without a page, or (ended) with one
-  for (int e = e0 + lane; e < e1; e += 64) found += in_pool(p, row[e]) == (q.n < 0);
+  scan(row, e0, e1, [&](int, int pg, bool here) { found += here && in_pool(p, pg) == (q.n < 0); });
   found = wave_sum(found);
   if (lane == 0) {
     L.info[s] = make_int4(q.n, q.first, q.n < 0 ? 0 : found, q.n < 0 ? found : 0);
@@ -122,7 +194,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_fill_kernel(PlanStepLaunch 
   }
   if (s >= p.num_seqs) return;
   const int4 me = L.info[s];
-  const int2 f = *L.state;
+  const FreePages f = {L.state->x, L.state->y};
   const int n = max(me.x, 0);
   if (lane == 0) {
     p.new_off[s] = t;
@@ -131,37 +203,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_fill_kernel(PlanStepLaunch 
     if (beyond && L.status) atomicOr(&L.status[s], EBD_ST_BAD_LAYOUT);
     if (s == p.num_seqs - 1) {
       p.new_off[s + 1] = t + n;
-      const int64_t taken = min(take + me.z, (int64_t)f.y);
-      p.free_state[0] = ring_at(p, f.x, taken);
-      p.free_state[1] = (int)min(f.y - taken + back + me.w, (int64_t)p.num_pages);
+      finish(p, f, take + me.z, back + me.w);
     }
   }
-  int32_t *row = p.page_table + (int64_t)s * p.max_pages;
-  if (me.x < 0) {
-    for (int base = 0; base < p.max_pages; base += 64) {
-      const int e = base + lane;
-      const int pg = e < p.max_pages ? row[e] : -1;
-      const uint64_t has = __ballot(in_pool(p, pg));
-      const int64_t at = f.y + back + __popcll(has & ((1ull << lane) - 1));
-      if (in_pool(p, pg) && at < p.num_pages) p.free_pages[ring_at(p, f.x, at)] = pg;
-      if (e < p.max_pages && pg != -1) row[e] = -1;
-      back += __popcll(has);
-    }
-    return;
-  }
-  if (me.z == 0) return;
-  const int e0 = me.y >> L.shift, e1 = min(((me.y + n - 1) >> L.shift) + 1, p.max_pages);
-  bool none = false;
-  for (int base = e0; base < e1; base += 64) {
-    const int e = base + lane;
-    const bool hole = e < e1 && !in_pool(p, row[e]);
-    const uint64_t holes = __ballot(hole);
-    const int64_t at = take + __popcll(holes & ((1ull << lane) - 1));
-    if (hole && at < f.y) row[e] = p.free_pages[ring_at(p, f.x, at)];
-    none |= hole && at >= f.y;
-    take += __popcll(holes);
-  }
-  if (__any(none) && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  const bool none = fill(p, f, s, me.x, me.y, L.shift, take, back);
+  if (none && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
 }
 
 __global__ __launch_bounds__(kPlanThreads) void plan_tokens_kernel(PlanStepLaunch L) {
@@ -214,19 +260,130 @@ __global__ __launch_bounds__(kPlanThreads) void plan_trees_kernel(PlanStepLaunch
     uint64_t *mask = p.mask + (t0 + j) * W;
     int depth = 0;
     if (j < in) {
-      // words from the last down to the one a bit falls into are finished: parents come before their children
-      int w = W - 1;
-      uint64_t bits = 0;
-      for (int i = j; i >= 0; i = parent[i], ++depth) {
-        for (; w > i >> 6; --w, bits = 0) mask[w] = bits;
-        bits |= 1ull << (i & 63);
-      }
-      for (; w >= 0; --w, bits = 0) mask[w] = bits;
+      depth = walk(parent, j, mask, W);
     } else {
       for (int w = 0; w < W; ++w) mask[w] = 0;
     }
-    if (p.pos) p.pos[t0 + j] = j < in ? first + depth - 1 : -1;
+    if (p.pos) p.pos[t0 + j] = j < in ? first + depth : -1;
     if (p.slots) p.slots[t0 + j] = slot_of(p, L.shift, s, first + j);
+  }
+}
+
+// All of it by one work-group, for up to 64 sequences, of which 16 lanes each take the entries, and two tokens a thread.
+// us by one launch / by three: 64 sequences of one token 4.9 / 9.4, 64 trees of 30 5.7 / 9.4.  A version for up to 1024
+// sequences in turns and 4096 tokens was no faster where this one does not serve: 256 of one token 10.5 / 9.8, 128 trees of 15
+// 10.6 / 9.5, one of 4000 11.4 / 9.5, and tables of many entries, which a wave each gives back when their sequences end, 64
+// of 8200 entries 163 / 39.
+constexpr int kOneThreads = 1024;
+constexpr int kOneSeqs = kOneThreads / 16;
+constexpr int kOneTokens = 2;
+constexpr int64_t kOneEntries = (int64_t)1 << 17;
+__global__ __launch_bounds__(kOneThreads) void plan_one_kernel(PlanStepLaunch L) {
+  __shared__ int new_of[kOneSeqs], first_of[kOneSeqs], take_of[kOneSeqs], back_of[kOneSeqs];
+  __shared__ int64_t off[kOneSeqs + 1];
+  __shared__ int32_t parent[kOneThreads * kOneTokens];
+  const ebd_plan_step_params &p = L.p;
+  const int S = p.num_seqs, me = threadIdx.x, lane = me & 63, wave = me >> 6, s = me >> 4;
+  int32_t up[kOneTokens];  // asked for first, used last
+#pragma unroll
+  for (int k = 0; k < kOneTokens; ++k) {
+    const int t = me + k * kOneThreads;
+    up[k] = -1;
+    if (p.parent && t < p.num_tokens) up[k] = p.parent[t];
+  }
+  const FreePages f = free_pages(p, p.free_state[0], p.free_state[1]);
+  // 16 lanes' sequence: what it needs; a wave for what an ended one gives back
+  Request q = {0, 0, 0, 0, 0};
+  if (s < S) q = request(p, L.shift, p.count[s], p.len[s]);
+  int32_t *row = p.page_table + (int64_t)s * p.max_pages;
+  int found = 0;
+  for (int e = q.e0 + (lane & 15); e < q.e1; e += 16) found += !in_pool(p, row[e]);
+#pragma unroll
+  for (int o = 8; o; o >>= 1) found += __shfl_xor(found, o);
+  if ((lane & 15) == 0) new_of[s] = q.n, first_of[s] = q.first, take_of[s] = found, back_of[s] = 0;
+  const uint64_t ended = __ballot((lane & 15) == 0 && q.n < 0);
+  for (uint64_t rest = ended; rest; rest &= rest - 1) {
+    const int e = 4 * wave + (__builtin_ctzll(rest) >> 4);
+    int held = 0;
+    scan(p.page_table + (int64_t)e * p.max_pages, 0, p.max_pages, [&](int, int pg, bool here) { held += here && in_pool(p, pg); });
+    held = wave_sum(held);
+    if (lane == 0) back_of[e] = held;
+  }
+  __syncthreads();
+  if (wave == 0) {  // the sums over the sequences before each (counts pass 32 bits, pages do not)
+    int64_t upto = max(new_of[lane], 0);
+    int take = take_of[lane], back = back_of[lane];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(upto, o);
+      const int y = __shfl_up(take, o), z = __shfl_up(back, o);
+      if (lane >= o) upto += x, take += y, back += z;
+    }
+    off[lane + 1] = upto;
+    if (lane == 0) off[0] = 0, p.new_off[0] = 0;
+    if (lane < S) p.new_off[lane + 1] = upto;
+    if (lane == S - 1) finish(p, f, take, back);
+    take_of[lane] = take - take_of[lane], back_of[lane] = back - back_of[lane];
+  }
+  __syncthreads();
+  if ((lane & 15) == 0 && s < S) {
+    if (q.n != 0) p.len[s] = q.n < 0 ? 0 : q.first + q.n;
+    if (off[s + 1] > p.num_tokens && q.n > 0 && (p.slots || p.pos || p.mask)) q.status |= EBD_ST_BAD_LAYOUT;
+    if (q.status && L.status) atomicOr(&L.status[s], q.status);
+  }
+  bool none = false;
+  int take = take_of[s];
+  for (int base = q.e0; base < q.e1; base += 16) {
+    const int e = base + (lane & 15);
+    const bool hole = e < q.e1 && !in_pool(p, row[e]);
+    const uint32_t holes = (uint32_t)(__ballot(hole) >> (lane & 48)) & 0xffffu;
+    const int at = take + __popc(holes & ((1u << (lane & 15)) - 1u));
+    if (hole && at < f.count) row[e] = p.free_pages[ring_at(p, f.head, at)];
+    none |= hole && at >= f.count;
+    take += __popc(holes);
+  }
+  if (none && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  for (uint64_t rest = ended; rest; rest &= rest - 1) {
+    const int e = 4 * wave + (__builtin_ctzll(rest) >> 4);
+    fill(p, f, e, -1, 0, L.shift, 0, back_of[e]);
+  }
+  __syncthreads();  // the entries are written
+  int seq[kOneTokens];
+#pragma unroll
+  for (int k = 0; k < kOneTokens; ++k) {
+    const int t = me + k * kOneThreads;
+    int lo = 0, hi = S;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid + 1] <= t) lo = mid + 1;
+      else hi = mid;
+    }
+    seq[k] = t < p.num_tokens ? lo : S;
+    if (p.mask && seq[k] < S) {
+      const int j = t - (int)off[lo];
+      const bool bad = j >= 64 * p.mask_words || up[k] < -1 || up[k] >= j;
+      if (bad && L.status) atomicOr(&L.status[lo], EBD_ST_BAD_LAYOUT);
+      parent[t] = bad ? -1 : up[k];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kOneTokens; ++k) {
+    const int t = me + k * kOneThreads, u = seq[k];
+    if (t >= p.num_tokens) break;
+    const int t0 = u < S ? (int)off[u] : 0, j = t - t0, at = u < S ? first_of[u] + j : -1;
+    int pos = at;
+    if (p.mask) {
+      uint64_t *mask = p.mask + (int64_t)t * p.mask_words;
+      if (u < S && j < 64 * p.mask_words) {
+        pos = first_of[u] + walk(parent + t0, j, mask, p.mask_words);
+      } else {
+        pos = -1;
+        for (int w = 0; w < p.mask_words; ++w) mask[w] = 0;
+      }
+    }
+    if (p.pos) p.pos[t] = pos;
+    if (p.slots) p.slots[t] = u < S ? slot_of(p, L.shift, u, at) : -1;
   }
 }
 
@@ -234,6 +391,10 @@ size_t plan_step_bytes(const ebd_plan_step_params &p) { return 256 + (size_t)p.n
 
 hipError_t launch_plan_step(const PlanStepLaunch &L, hipStream_t s) {
   const ebd_plan_step_params &p = L.p;
+  if (p.num_seqs <= kOneSeqs && p.num_tokens <= kOneThreads * kOneTokens && (int64_t)p.num_seqs * p.max_pages <= kOneEntries) {
+    hipLaunchKernelGGL(plan_one_kernel, dim3(1), dim3(kOneThreads), 0, s, L);
+    return hipGetLastError();
+  }
   const dim3 block(kPlanThreads), seqs((unsigned)((p.num_seqs + kPlanWaves - 1) / kPlanWaves));
   hipLaunchKernelGGL(plan_count_kernel, seqs, block, 0, s, L);
   hipLaunchKernelGGL(plan_fill_kernel, seqs, block, 0, s, L);
