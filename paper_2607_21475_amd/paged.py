@@ -26,7 +26,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from . import EBD_WS_ATTEND_PAGED, HEAD_DIM, _check, _lib, _ptr, ebd_workspace_size, workspace
+from . import EBD_WS_ATTEND_PAGED, EBD_WS_ATTEND_TREE, EBD_WS_PLAN_STEP, HEAD_DIM, _check, _lib, _ptr, ebd_workspace_size, workspace
 
 EBD_ROPE_HALF = 0
 EBD_ROPE_PAIRS = 1
@@ -771,12 +771,15 @@ def rope_frequencies(rot_dim: int = HEAD_DIM, base: float = 10000.0, scaling: st
 @dataclass
 class PagedCache:
     """The pools of one layer and what its sequences hold: K, V [pages, KV heads, rows per page, 128] bf16, page_table
-    [sequences, pages per sequence] int32, len [sequences] int32 (all on the device, the caller's to update)."""
+    [sequences, pages per sequence] int32, len [sequences] int32 (all on the device, the caller's to update).  A pool whose
+    pages `plan` deals out has its free ones in the ring free_pages [pages] int32, free_state [2] int32."""
 
     K: torch.Tensor
     V: torch.Tensor
     page_table: torch.Tensor
     len: torch.Tensor
+    free_pages: Optional[torch.Tensor] = None
+    free_state: Optional[torch.Tensor] = None
 
     @classmethod
     def allocate(cls, lengths: Sequence[int], kv_heads: int, page_size: int = 64, spare: int = 0, device="cuda"):
@@ -792,16 +795,55 @@ class PagedCache:
         return cls(torch.empty(shape, dtype=_BF, device=device), torch.empty(shape, dtype=_BF, device=device),
                    table.to(device), torch.zeros(len(used), dtype=torch.int32, device=device))
 
+    @classmethod
+    def pool(cls, num_seqs: int, num_pages: int, kv_heads: int, page_size: int = 64, max_pages: Optional[int] = None,
+             device="cuda"):
+        """A pool of free pages and `num_seqs` sequences without rows, of up to max_pages pages each (default: all)."""
+        shape = (num_pages, kv_heads, page_size, HEAD_DIM)
+        table = torch.full((num_seqs, num_pages if max_pages is None else max_pages), -1, dtype=torch.int32, device=device)
+        return cls(torch.empty(shape, dtype=_BF, device=device), torch.empty(shape, dtype=_BF, device=device), table,
+                   torch.zeros(num_seqs, dtype=torch.int32, device=device),
+                   torch.arange(num_pages, dtype=torch.int32, device=device),
+                   torch.tensor([0, num_pages], dtype=torch.int32, device=device))
+
     @property
     def pages(self) -> ebd_pages:
         return pages(self.K, self.V, self.page_table)
 
-    def append(self, k_new, v_new, new_off, rot: Optional[ebd_rotary] = None, pos=None, q=None, status=None):
-        """Append tokens (self.len counts them already); returns the rotated queries (zeros for padding tokens), or None
-        without q."""
+    def plan(self, count, num_tokens: int, parent=None, mask_words: Optional[int] = None, ws: Optional[torch.Tensor] = None,
+             status=None):
+        """Pages for the new tokens count [sequences] int32 (negative: the sequence has ended) of a step of at most
+        num_tokens tokens, and len with them: {"new_off", "slots" [num_tokens] int64, "pos" [num_tokens] int32, "ws"}, and
+        with the trees parent [num_tokens] int32 "mask" [num_tokens, mask_words] int64 (by default of as many words as
+        num_tokens tokens need, up to 64)."""
+        if self.free_pages is None or self.free_state is None:
+            raise ValueError("the cache has no ring of free pages")
+        dev, T = self.K.device, int(num_tokens)
+        new = {"new_off": torch.empty(self.len.numel() + 1, dtype=torch.int64, device=dev),
+               "slots": torch.empty(T, dtype=torch.int64, device=dev), "pos": torch.empty(T, dtype=_I32, device=dev)}
+        if parent is not None:
+            words = max(1, min(64, -(-T // 64))) if mask_words is None else int(mask_words)
+            new["mask"] = torch.empty((T, words), dtype=torch.int64, device=dev)
+        p = plan_step_params(count, self.len, self.page_table, self.K.shape[2], self.free_pages, self.free_state,
+                             new["new_off"], slots=new["slots"], pos=new["pos"], parent=parent, mask=new.get("mask"))
+        need = ebd_workspace_size(EBD_WS_PLAN_STEP, p)
+        new["ws"] = workspace(need, dev) if ws is None or ws.numel() < need else ws
+        ebd_plan_step(p, new["ws"], status=status)
+        return new
+
+    def append(self, k_new, v_new, new_off, rot: Optional[ebd_rotary] = None, pos=None, q=None, status=None,
+               k_norm: Optional[ebd_norm] = None, q_norm: Optional[ebd_norm] = None, slots=None):
+        """Append tokens (self.len counts them already), normalised by k_norm and q_norm, at their slots if given (of
+        `plan`; a rotation then needs pos); returns the queries as the attention takes them (zeros for padding tokens), or
+        None without q."""
         q_out = None if q is None else torch.zeros(q.shape, dtype=_BF, device=q.device)
-        p = append_paged_params(self.pages, k_new, v_new, new_off, self.len, rot, pos=pos, q=q, q_out=q_out)
-        ebd_append_paged(p, k_new, v_new, self.K, self.V, q, q_out, status=status)
+        if k_norm is None and q_norm is None and slots is None:
+            p = append_paged_params(self.pages, k_new, v_new, new_off, self.len, rot, pos=pos, q=q, q_out=q_out)
+            ebd_append_paged(p, k_new, v_new, self.K, self.V, q, q_out, status=status)
+        else:
+            p = append_norm_params(self.pages, k_new, v_new, new_off, self.len, k_norm, q_norm, rot, pos=pos, q=q,
+                                   q_out=q_out, slots=slots)
+            ebd_append_norm(p, k_new, v_new, self.K, self.V, q, q_out, status=status)
         return q_out
 
     def attend(self, q, new_off, max_new: int, max_rows: int, qpos=None, window: int = 0, scale: float = 0.0,
@@ -817,6 +859,25 @@ class PagedCache:
             ws = workspace(need, q.device)
         ebd_attend_paged(p, q, self.K, self.V, y, ws, lse=lse, status=status)
         return {"y": y, "lse": lse, "ws": ws}
+
+    def attend_tree(self, q, new_off, max_new: int, max_rows: int, mask, qpos=None, window: int = 0, scale: float = 0.0,
+                    ws: Optional[torch.Tensor] = None, status=None):
+        """Attention of trees of new tokens, as `attend`; mask and qpos as `plan` makes them."""
+        y = torch.zeros(q.shape, dtype=_BF, device=q.device)
+        lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device)
+        p = attend_tree_params(self.pages, q, y, new_off, self.len, max_new, max_rows, mask, qpos=qpos, window=window,
+                               scale=scale)
+        need = ebd_workspace_size(EBD_WS_ATTEND_TREE, p)
+        if ws is None or ws.numel() < need:
+            ws = workspace(need, q.device)
+        ebd_attend_tree(p, q, self.K, self.V, y, ws, lse=lse, status=status)
+        return {"y": y, "lse": lse, "ws": ws}
+
+    def keep(self, new_off, path, kept, status=None):
+        """Keep the accepted paths path [sequences, most kept] int32 of kept [sequences] int32 tokens; len then counts
+        these alone."""
+        p = keep_rows_params(self.pages, new_off, self.len, path, kept, len_out=self.len)
+        ebd_keep_rows(p, self.K, self.V, status=status)
 
     def gather(self, lengths: Sequence[int], status=None):
         """The first lengths[s] rows of every sequence as units: (K [rows, 128], V, seq_off), as cache.evict takes them
