@@ -609,8 +609,8 @@ ebd_status ebd_append_norm(const ebd_append_norm_params *p, const uint16_t *k_ne
  *                follows its sequence's new token 64 w + i or is it; 0 for padding.  mask_words 1 .. 64; a token whose index
  *                does not fit gets an empty mask and position -1.
  *   num_tokens   room in slots, pos, parent and mask; new_off goes on past it, but nothing else is written there.
- *   status       [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when new rows are left without a page (the ring is empty,
- *                the table too short); EBD_ST_BAD_LAYOUT when new tokens have no room in num_tokens or in the mask, a parent
+ *   status       [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when new rows are left without a page (the ring is empty
+ *                or holds no page of the pool, the table is too short); EBD_ST_BAD_LAYOUT when new tokens have no room in num_tokens or in the mask, a parent
  *                is out of place (taken for -1), or the sequence would hold more than 2^30 rows (it gets none, and keeps
  *                what it has; a negative len counts as 0).
  * Pages that several sequences share must not be given back by ending one of them.  At most 65536 sequences, 2^24 - 1 tokens.

@@ -122,8 +122,9 @@ __device__ __forceinline__ bool fill(const ebd_plan_step_params &p, const FreePa
       const bool hole = here && !in_pool(p, pg);
       const uint64_t holes = __ballot(hole);
       const int64_t at = take + __popcll(holes & below);
-      if (hole && at < f.count) row[e] = p.free_pages[ring_at(p, f.head, at)];
-      none |= hole && at >= f.count;
+      const int got = hole && at < f.count ? p.free_pages[ring_at(p, f.head, at)] : -1;
+      if (hole && at < f.count) row[e] = got;
+      none |= hole && !in_pool(p, got);
       take += __popcll(holes);
     });
   }
@@ -269,21 +270,23 @@ __global__ __launch_bounds__(kPlanThreads) void plan_trees_kernel(PlanStepLaunch
   }
 }
 
-// All of it by one work-group, for up to 64 sequences, of which 16 lanes each take the entries, and two tokens a thread.
-// us by one launch / by three: 64 sequences of one token 4.9 / 9.4, 64 trees of 30 5.7 / 9.4.  A version for up to 1024
-// sequences in turns and 4096 tokens was no faster where this one does not serve: 256 of one token 10.5 / 9.8, 128 trees of 15
-// 10.6 / 9.5, one of 4000 11.4 / 9.5, and tables of many entries, which a wave each gives back when their sequences end, 64
-// of 8200 entries 163 / 39.
+// All of it by one work-group, for up to 128 sequences, of which eight lanes each take the entries, and four tokens a thread.
+// us by one launch / by three: 64 sequences of one token 5.0 / 9.7, 64 trees of 30 6.4 / 9.5, 128 trees of 15 7.2 / 9.6, of 30
+// 9.2 / 9.6, 16 of 130 8.2 / 9.5.  Not taken: one sequence of 4000 tokens in pages of 16, whose 250 entries eight lanes would
+// take, 14.6 / 10.0; 256 sequences of one token, by a version that takes sequences in turns, 10.5 / 9.8; tables of many
+// entries, which a wave each gives back when their sequences end, 64 of 8200 163 / 39.
 constexpr int kOneThreads = 1024;
-constexpr int kOneSeqs = kOneThreads / 16;
-constexpr int kOneTokens = 2;
-constexpr int64_t kOneEntries = (int64_t)1 << 17;
+constexpr int kOneLanes = 8;
+constexpr int kOneSeqs = kOneThreads / kOneLanes;
+constexpr int kOneTokens = 4;
+constexpr int64_t kOneEntries = (int64_t)1 << 17;  // of all sequences' tables
+constexpr int64_t kOnePages = 128;                // of a sequence's new rows
 __global__ __launch_bounds__(kOneThreads) void plan_one_kernel(PlanStepLaunch L) {
   __shared__ int new_of[kOneSeqs], first_of[kOneSeqs], take_of[kOneSeqs], back_of[kOneSeqs];
   __shared__ int64_t off[kOneSeqs + 1];
   __shared__ int32_t parent[kOneThreads * kOneTokens];
   const ebd_plan_step_params &p = L.p;
-  const int S = p.num_seqs, me = threadIdx.x, lane = me & 63, wave = me >> 6, s = me >> 4;
+  const int S = p.num_seqs, me = threadIdx.x, lane = me & 63, wave = me >> 6, s = me / kOneLanes, own = lane % kOneLanes;
   int32_t up[kOneTokens];  // asked for first, used last
 #pragma unroll
   for (int k = 0; k < kOneTokens; ++k) {
@@ -292,18 +295,18 @@ __global__ __launch_bounds__(kOneThreads) void plan_one_kernel(PlanStepLaunch L)
     if (p.parent && t < p.num_tokens) up[k] = p.parent[t];
   }
   const FreePages f = free_pages(p, p.free_state[0], p.free_state[1]);
-  // 16 lanes' sequence: what it needs; a wave for what an ended one gives back
+  // eight lanes' sequence: what it needs; a wave for what an ended one gives back
   Request q = {0, 0, 0, 0, 0};
   if (s < S) q = request(p, L.shift, p.count[s], p.len[s]);
   int32_t *row = p.page_table + (int64_t)s * p.max_pages;
   int found = 0;
-  for (int e = q.e0 + (lane & 15); e < q.e1; e += 16) found += !in_pool(p, row[e]);
+  for (int e = q.e0 + own; e < q.e1; e += kOneLanes) found += !in_pool(p, row[e]);
 #pragma unroll
-  for (int o = 8; o; o >>= 1) found += __shfl_xor(found, o);
-  if ((lane & 15) == 0) new_of[s] = q.n, first_of[s] = q.first, take_of[s] = found, back_of[s] = 0;
-  const uint64_t ended = __ballot((lane & 15) == 0 && q.n < 0);
+  for (int o = kOneLanes / 2; o; o >>= 1) found += __shfl_xor(found, o);
+  if (own == 0) new_of[s] = q.n, first_of[s] = q.first, take_of[s] = found, back_of[s] = 0;
+  const uint64_t ended = __ballot(own == 0 && q.n < 0);
   for (uint64_t rest = ended; rest; rest &= rest - 1) {
-    const int e = 4 * wave + (__builtin_ctzll(rest) >> 4);
+    const int e = (64 * wave + __builtin_ctzll(rest)) / kOneLanes;
     int held = 0;
     scan(p.page_table + (int64_t)e * p.max_pages, 0, p.max_pages, [&](int, int pg, bool here) { held += here && in_pool(p, pg); });
     held = wave_sum(held);
@@ -311,40 +314,48 @@ __global__ __launch_bounds__(kOneThreads) void plan_one_kernel(PlanStepLaunch L)
   }
   __syncthreads();
   if (wave == 0) {  // the sums over the sequences before each (counts pass 32 bits, pages do not)
-    int64_t upto = max(new_of[lane], 0);
-    int take = take_of[lane], back = back_of[lane];
+    static_assert(kOneSeqs == 128, "two sequences a lane");
+    const int a = 2 * lane, b = a + 1, n0 = max(new_of[a], 0), t0 = take_of[a], b0 = back_of[a];
+    int64_t upto = (int64_t)n0 + max(new_of[b], 0);
+    int take = t0 + take_of[b], back = b0 + back_of[b];
+    const int64_t n2 = upto;
+    const int t2 = take, b2 = back;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int64_t x = __shfl_up(upto, o);
       const int y = __shfl_up(take, o), z = __shfl_up(back, o);
       if (lane >= o) upto += x, take += y, back += z;
     }
-    off[lane + 1] = upto;
     if (lane == 0) off[0] = 0, p.new_off[0] = 0;
-    if (lane < S) p.new_off[lane + 1] = upto;
-    if (lane == S - 1) finish(p, f, take, back);
-    take_of[lane] = take - take_of[lane], back_of[lane] = back - back_of[lane];
+    if (lane == 63) finish(p, f, take, back);  // (sequences that are not there take and give nothing)
+    const int64_t before = upto - n2;
+    off[a + 1] = before + n0, off[b + 1] = upto;
+    if (a < S) p.new_off[a + 1] = before + n0;
+    if (b < S) p.new_off[b + 1] = upto;
+    take_of[a] = take - t2, take_of[b] = take - t2 + t0;
+    back_of[a] = back - b2, back_of[b] = back - b2 + b0;
   }
   __syncthreads();
-  if ((lane & 15) == 0 && s < S) {
+  if (own == 0 && s < S) {
     if (q.n != 0) p.len[s] = q.n < 0 ? 0 : q.first + q.n;
     if (off[s + 1] > p.num_tokens && q.n > 0 && (p.slots || p.pos || p.mask)) q.status |= EBD_ST_BAD_LAYOUT;
     if (q.status && L.status) atomicOr(&L.status[s], q.status);
   }
   bool none = false;
   int take = take_of[s];
-  for (int base = q.e0; base < q.e1; base += 16) {
-    const int e = base + (lane & 15);
+  for (int base = q.e0; base < q.e1; base += kOneLanes) {
+    const int e = base + own;
     const bool hole = e < q.e1 && !in_pool(p, row[e]);
-    const uint32_t holes = (uint32_t)(__ballot(hole) >> (lane & 48)) & 0xffffu;
-    const int at = take + __popc(holes & ((1u << (lane & 15)) - 1u));
-    if (hole && at < f.count) row[e] = p.free_pages[ring_at(p, f.head, at)];
-    none |= hole && at >= f.count;
+    const uint32_t holes = (uint32_t)(__ballot(hole) >> (lane - own)) & ((1u << kOneLanes) - 1u);
+    const int at = take + __popc(holes & ((1u << own) - 1u));
+    const int got = hole && at < f.count ? p.free_pages[ring_at(p, f.head, at)] : -1;
+    if (hole && at < f.count) row[e] = got;
+    none |= hole && !in_pool(p, got);
     take += __popc(holes);
   }
   if (none && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   for (uint64_t rest = ended; rest; rest &= rest - 1) {
-    const int e = 4 * wave + (__builtin_ctzll(rest) >> 4);
+    const int e = (64 * wave + __builtin_ctzll(rest)) / kOneLanes;
     fill(p, f, e, -1, 0, L.shift, 0, back_of[e]);
   }
   __syncthreads();  // the entries are written
@@ -391,7 +402,8 @@ size_t plan_step_bytes(const ebd_plan_step_params &p) { return 256 + (size_t)p.n
 
 hipError_t launch_plan_step(const PlanStepLaunch &L, hipStream_t s) {
   const ebd_plan_step_params &p = L.p;
-  if (p.num_seqs <= kOneSeqs && p.num_tokens <= kOneThreads * kOneTokens && (int64_t)p.num_seqs * p.max_pages <= kOneEntries) {
+  if (p.num_seqs <= kOneSeqs && p.num_tokens <= kOneThreads * kOneTokens &&
+      p.num_tokens <= kOnePages * p.page_size && (int64_t)p.num_seqs * p.max_pages <= kOneEntries) {
     hipLaunchKernelGGL(plan_one_kernel, dim3(1), dim3(kOneThreads), 0, s, L);
     return hipGetLastError();
   }

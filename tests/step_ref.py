@@ -107,7 +107,7 @@ def plan(count, lens, table, page, ring, state, room, parent=None, words=0):
                     continue
                 if taken < free:
                     table[s][e] = ring[(head + taken) % N]
-                else:
+                if not known(table[s][e]):
                     status[s] |= BAD_PAGE
                 taken += 1
             lens[s] = first + n

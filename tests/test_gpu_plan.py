@@ -186,3 +186,16 @@ def test_plan_in_a_graph(seqs, new, tree):
         graph.replay()
         want = step.plan(count, before[0], before[1], 16, before[2], before[3], room, parent, 1)
         _check(t, want)
+
+
+@pytest.mark.parametrize("seqs", [4, 300])
+def test_plan_from_a_ring_of_bad_pages(seqs):
+    """Numbers outside the pool among the free pages: taken in their turn, and flagged."""
+    rng = random.Random(seqs)
+    lens, count = [rng.randint(0, 40) for _ in range(seqs)], [rng.randint(0, 50) for _ in range(seqs)]
+    table, ring, state = _server(rng, lens, 16, 7, 4 * seqs)
+    for i in range(0, state[1], 3):
+        ring[(state[0] + i) % len(ring)] = rng.choice([-1, len(ring), 2 ** 31 - 1])
+    want = step.plan(count, lens, table, 16, ring, state, 50 * seqs)
+    assert 0 < sum(x > 0 for x in want["status"])
+    _check(_run(count, lens, table, 16, ring, state, 50 * seqs)[0], want)
