@@ -102,49 +102,76 @@ __device__ __forceinline__ float normalise(Part &x, float eps) {
   return r * scale;
 }
 
-// The pairs of a lane's part of a row turned; SIGN -1: back.  t: the part's pairs; cs: all of the token's, for rows whose
-// pairs lie in different lanes (those of one wave): they meet in LDS, at `row`.
-template <bool ODD, int SIGN>
-__device__ __forceinline__ void turn_part(const ebd_rotary &R, const Split &S, Part &x, const float2 (&t)[8],
-                                          const float2 *cs, float *row) {
-  // (by value: from references the compiler makes addresses)
-  auto pair = [](float u, float v, float2 t) {
-    const float s = SIGN * t.y;
-    return make_float2(u * t.x - v * s, v * t.x + u * s);
-  };
-  const int n = R.rot_dim / 2;
-  if (S.how == kHalf) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 y = pair(x.a[i], x.b[i], t[i]);
-      x.a[i] = y.x, x.b[i] = y.y;
-    }
-  } else if (S.how == kPairs) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int u = S.e0 / 2 + i, v = u + 4;
-      const float2 y = pair(x.a[2 * i], x.a[2 * i + 1], t[i]), z = pair(x.b[2 * i], x.b[2 * i + 1], t[i + 4]);
-      x.a[2 * i] = u < n ? y.x : x.a[2 * i], x.a[2 * i + 1] = u < n ? y.y : x.a[2 * i + 1];
-      x.b[2 * i] = v < n ? z.x : x.b[2 * i], x.b[2 * i + 1] = v < n ? z.y : x.b[2 * i + 1];
-    }
-  }
+// The sines that a lane's part of a row is turned by: its eight pairs, or (ODD) those of each of its sixteen elements.
+template <bool ODD>
+struct Turns {
+  float2 t[8];
+};
+template <>
+struct Turns<true> {
+  float2 t[16];
+};
+
+// ... from cs, the token's (those past the last pair are not used).
+template <bool ODD>
+__device__ __forceinline__ Turns<ODD> turns_of(const ebd_rotary &R, const Split &S, const float2 *cs) {
+  Turns<ODD> T;
   if constexpr (ODD) {
-    if (S.how == kOdd) {
+    const int n = R.rot_dim / 2;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) row[S.e0 + i] = x.a[i], row[S.e1 + i] = x.b[i];
+    for (int i = 0; i < 16; ++i) {
+      const int e = i < 8 ? S.e0 + i : S.e1 + i - 8;
+      const float2 t = cs[e < n ? e : max(0, min(e - n, kHeadDim / 2 - 1))];
+      T.t[i] = make_float2(t.x, e < n ? -t.y : t.y);
+    }
+  } else {
+    const int l = threadIdx.x & 7;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) T.t[i] = cs[8 * l + i];
+  }
+  return T;
+}
+
+// A part of a row turned; SIGN -1: back.  row: a place in LDS for it where its pairs lie in different lanes (ODD).
+template <bool ODD, int SIGN>
+__device__ __forceinline__ void turn_part(const ebd_rotary &R, const Split &S, Part &x, const Turns<ODD> &T, float *row) {
+  const int n = R.rot_dim / 2;
+  if constexpr (ODD) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      *reinterpret_cast<f32x4 *>(row + S.e0 + i) = f32x4{x.a[i], x.a[i + 1], x.a[i + 2], x.a[i + 3]};
+      *reinterpret_cast<f32x4 *>(row + S.e1 + i) = f32x4{x.b[i], x.b[i + 1], x.b[i + 2], x.b[i + 3]};
     }
     wave_sync();
-    if (S.how == kOdd) {
-      auto one = [&](float &u, int e) {
-        if (e >= 2 * n) return;
-        const float2 t = cs[e < n ? e : e - n];
-        const float v = row[e < n ? e + n : e - n], s = SIGN * t.y;
-        u = u * t.x + (e < n ? -v : v) * s;
-      };
+    auto one = [&](float u, int e, float2 t) {
+      const float v = row[e < n ? e + n : max(0, e - n)];
+      const float y = u * t.x + v * (SIGN * t.y);
+      return e < 2 * n ? y : u;
+    };
 #pragma unroll
-      for (int i = 0; i < 8; ++i) one(x.a[i], S.e0 + i), one(x.b[i], S.e1 + i);
-    }
+    for (int i = 0; i < 8; ++i) x.a[i] = one(x.a[i], S.e0 + i, T.t[i]), x.b[i] = one(x.b[i], S.e1 + i, T.t[8 + i]);
     wave_sync();  // (before the next row is written)
+  } else {
+    // (by value: from references the compiler makes addresses)
+    auto pair = [](float u, float v, float2 t) {
+      const float s = SIGN * t.y;
+      return make_float2(u * t.x - v * s, v * t.x + u * s);
+    };
+    if (S.how == kHalf) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 y = pair(x.a[i], x.b[i], T.t[i]);
+        x.a[i] = y.x, x.b[i] = y.y;
+      }
+    } else if (S.how == kPairs) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int u = S.e0 / 2 + i, v = u + 4;
+        const float2 y = pair(x.a[2 * i], x.a[2 * i + 1], T.t[i]), z = pair(x.b[2 * i], x.b[2 * i + 1], T.t[i + 4]);
+        x.a[2 * i] = u < n ? y.x : x.a[2 * i], x.a[2 * i + 1] = u < n ? y.y : x.a[2 * i + 1];
+        x.b[2 * i] = v < n ? z.x : x.b[2 * i], x.b[2 * i + 1] = v < n ? z.y : x.b[2 * i + 1];
+      }
+    }
   }
 }
 
@@ -170,13 +197,11 @@ __device__ __forceinline__ Share share_of(int shift) {
   return {(int64_t)(w >> shift), (int)(w & ((1u << shift) - 1u)), 1 << shift};
 }
 
-// The wave's sines: pair i by lane i, then the eight pairs of a lane's part (8 l .. 8 l + 7 in both layouts).
-__device__ __forceinline__ void make_turns(const ebd_rotary &R, int64_t pos, float2 *cs, float2 (&t)[8]) {
+// The wave's sines, pair i by lane i.
+__device__ __forceinline__ void make_turns(const ebd_rotary &R, int64_t pos, float2 *cs) {
   const int lane = threadIdx.x & 63;
   if (lane < R.rot_dim / 2) cs[lane] = turn(R, lane, pos);
   wave_sync();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) t[i] = cs[8 * (lane & 7) + i];  // (those past the last pair are not used)
 }
 
 template <bool ODD>
@@ -198,8 +223,11 @@ __global__ __launch_bounds__(64 * kForwardWaves) void norm_rope_kernel(NormRopeL
     x = load_raw(sp, x0 + h * p.x.head_stride);
     g = load_weights(sp, p.norm.weight + h * p.norm.head_stride);
   }
-  float2 t[8] = {};
-  if (p.rot.freq) make_turns(p.rot, ((const const_i32 *)p.pos)[w.t], cs[wave], t);
+  Turns<ODD> turns = {};
+  if (p.rot.freq) {
+    make_turns(p.rot, ((const const_i32 *)p.pos)[w.t], cs[wave]);
+    turns = turns_of<ODD>(p.rot, sp, cs[wave]);
+  }
   for (; h - r0 < p.num_heads; h += 8 * w.waves, x = next) {
     const int after = h + 8 * w.waves;
     if (after < p.num_heads) next = load_raw(sp, x0 + after * p.x.head_stride);
@@ -207,7 +235,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) void norm_rope_kernel(NormRopeL
     normalise(v, p.norm.eps);
     multiply(v, g);
     if (p.norm.head_stride && after < p.num_heads) g = load_weights(sp, p.norm.weight + after * p.norm.head_stride);
-    turn_part<ODD, 1>(p.rot, sp, v, t, cs[wave], odd);
+    turn_part<ODD, 1>(p.rot, sp, v, turns, odd);
     if (h < p.num_heads) store_part(sp, y0 + h * p.y.head_stride, v);
   }
 }
@@ -216,52 +244,64 @@ constexpr int kBackwardRows = 64;  // (128 of them leave too few registers)
 
 // A work-group takes every gridDim.x'th group of tokens; a thread's head stays the same, so that its share of dw waits in
 // registers; the next group's rows are on their way meanwhile.  Shared weights: the work-group's rows are added up (within a wave, then through LDS) and leave one row of
-// sums; weights of each head's own: each token slot leaves a row for every head.
+// sums; weights of each head's own: the token slots'
+// rows are added up, and leave one for every head.
 template <bool ODD, bool SHARED>
 __global__ __launch_bounds__(8 * kBackwardRows) void norm_rope_backward_kernel(NormRopeBackwardLaunch L) {
   __shared__ float2 cs[2][4][kHeadDim / 2];
   __shared__ float rows[ODD ? kBackwardRows : 1][kOddRow];
-  __shared__ float sums[SHARED ? kBackwardRows / 8 : 1][kHeadDim];
+  __shared__ float sums[SHARED ? kBackwardRows / 8 : 32][kHeadDim];
   const ebd_norm_rope_backward_params &p = L.p;
   const int slot = token_slot(L.per), i = threadIdx.x - slot * L.per, l = i % 8, n = p.rot.rot_dim / 2;
   const int h = blockIdx.y * kBackwardRows + i / 8;
   const Split sp = part_of(p.rot, l, true);
   Part w = {}, dw = {};
   if (h < p.num_heads) w = load_weights(sp, p.norm.weight + h * p.norm.head_stride);
-  int par = 0;
-  Raw x0 = {}, d0 = {};  // the rows of the token after this one's, on their way
-  auto ask = [&](int64_t g) {
+  // The rows of the token after this one's, and its position, are on their way meanwhile.  Nothing else is loaded in the
+  // loop, since a wait for it would be one for these; past the last token or head, that one's are asked for, and not used
+  // (conditions would cost more).  Two sets of registers in turn, without copies at the loop's end, were no faster: they
+  // leave a wave less on a SIMD.
+  struct Token {
+    Raw x, d;
+    int pos;
+  };
+  const bool turns = p.rot.freq && i < n;
+  const double freq = turns ? p.rot.freq[i] : 0.0;
+  const int row = min(h, p.num_heads - 1);
+  const uint16_t *xs = L.x + row * p.x.head_stride, *ds = L.dy + row * p.dy.head_stride;
+  auto ask = [&](int64_t g, Token &to) {
+    const int64_t t = min(g * L.tpb + slot, (int64_t)p.num_tokens - 1);
+    to.x = load_raw(sp, xs + t * p.x.token_stride);
+    to.d = load_raw(sp, ds + t * p.dy.token_stride);
+    to.pos = *(turns ? p.pos + t : reinterpret_cast<const int32_t *>(p.norm.weight));
+  };
+  auto take = [&](int64_t g, int par, const Token &now) {
+    if (turns) cs[par][slot][i] = turn_by(p.rot, freq, now.pos);
+    __syncthreads();  // (the other half is written by the next group's tokens, which every wave reaches after this one's)
     const int64_t t = g * L.tpb + slot;
     if (t >= p.num_tokens || h >= p.num_heads) return;
-    x0 = load_raw(sp, L.x + t * p.x.token_stride + h * p.x.head_stride);
-    d0 = load_raw(sp, L.dy + t * p.dy.token_stride + h * p.dy.head_stride);
-  };
-  ask(blockIdx.x);
-  for (int64_t g = blockIdx.x; g * L.tpb < p.num_tokens; g += gridDim.x, par ^= 1) {
-    const int64_t t = g * L.tpb + slot;
-    const bool live = t < p.num_tokens && h < p.num_heads;
-    Part x = unpack(x0), d = unpack(d0);
-    if ((g + gridDim.x) * L.tpb < p.num_tokens) ask(g + gridDim.x);
-    if (t < p.num_tokens && p.rot.freq && i < n) cs[par][slot][i] = turn(p.rot, i, p.pos[t]);
-    __syncthreads();  // (the other half is written by the next group's tokens, which every wave reaches after this one's)
-    if (live) {
-      const float r = normalise(x, p.norm.eps);
-      float2 tt[8];
+    Part x = unpack(now.x), d = unpack(now.d);
+    const float r = normalise(x, p.norm.eps);
+    turn_part<ODD, -1>(p.rot, sp, d, turns_of<ODD>(p.rot, sp, cs[par][slot]), rows[ODD ? threadIdx.x / 8 : 0]);
+    float m = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) tt[k] = cs[par][slot][8 * l + k];
-      turn_part<ODD, -1>(p.rot, sp, d, tt, cs[par][slot], rows[ODD ? threadIdx.x / 8 : 0]);
-      float m = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        dw.a[k] += d.a[k] * x.a[k], dw.b[k] += d.b[k] * x.b[k];
-        d.a[k] *= w.a[k], d.b[k] *= w.b[k];
-        m += d.a[k] * x.a[k] + d.b[k] * x.b[k];
-      }
-      m = sum8(m) * (1.0f / kHeadDim);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) d.a[k] = r * (d.a[k] - x.a[k] * m), d.b[k] = r * (d.b[k] - x.b[k] * m);
-      store_part(sp, L.dx + t * p.dx.token_stride + h * p.dx.head_stride, d);
+    for (int k = 0; k < 8; ++k) {
+      dw.a[k] += d.a[k] * x.a[k], dw.b[k] += d.b[k] * x.b[k];
+      d.a[k] *= w.a[k], d.b[k] *= w.b[k];
+      m += d.a[k] * x.a[k] + d.b[k] * x.b[k];
     }
+    m = sum8(m) * (1.0f / kHeadDim);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) d.a[k] = r * (d.a[k] - x.a[k] * m), d.b[k] = r * (d.b[k] - x.b[k] * m);
+    store_part(sp, L.dx + t * p.dx.token_stride + h * p.dx.head_stride, d);
+  };
+  Token next;
+  ask(blockIdx.x, next);
+  int par = 0;
+  for (int64_t g = blockIdx.x; g * L.tpb < p.num_tokens; g += gridDim.x, par ^= 1) {
+    const Token now = next;
+    ask(g + gridDim.x, next);
+    take(g, par, now);
   }
   if constexpr (SHARED) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -281,28 +321,42 @@ __global__ __launch_bounds__(8 * kBackwardRows) void norm_rope_backward_kernel(N
       for (int v = 0; v < waves; ++v) s += sums[v][e];
       L.part[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kHeadDim + e] = s;
     }
-  } else if (h < p.num_heads) {
-    float *out = L.part + (((int64_t)blockIdx.x * L.tpb + slot) * p.num_heads + h) * kHeadDim;
+  } else {
+    // (token slots of a work-group have up to 16 rows each, 32 in all)
+    if (L.tpb > 1) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) out[sp.e0 + k] = dw.a[k], out[sp.e1 + k] = dw.b[k];
+      for (int k = 0; k < 8; ++k) sums[threadIdx.x / 8][sp.e0 + k] = dw.a[k], sums[threadIdx.x / 8][sp.e1 + k] = dw.b[k];
+      __syncthreads();
+      for (int t = 1; slot == 0 && t < L.tpb; ++t) {
+        const float *other = sums[(threadIdx.x + t * L.per) / 8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dw.a[k] += other[sp.e0 + k], dw.b[k] += other[sp.e1 + k];
+      }
+    }
+    if (slot == 0 && h < p.num_heads) {
+      float *out = L.part + ((int64_t)blockIdx.x * p.num_heads + h) * kHeadDim;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) out[sp.e0 + k] = dw.a[k], out[sp.e1 + k] = dw.b[k];
+    }
   }
 }
 
-// dw of a head: its rows of sums, added in a fixed order in 64 bits: 32 lanes take four elements each of every 32nd row,
-// then the 32 sums meet (512 rows of 40 heads: 20.9 us with a thread an element and 8 of the rows at a time, 5.6 so).
+// A quarter of a head's dw: its rows of sums, added in a fixed order in 64 bits.  Eight lanes take four elements each of
+// every 128th row, and the 128 sums meet (512 rows of 40 heads: 20.9 us by a thread an element and eight rows at a time, 5.6
+// by whole rows, 32 at a time, 4.9 so; of few heads the work-groups are what lacks).
 __global__ __launch_bounds__(1024) void norm_rope_join_kernel(NormRopeBackwardLaunch L) {
-  constexpr int kFlight = 8;
-  __shared__ double sums[16][kHeadDim];
-  const int e = threadIdx.x % 32 * 4, g = threadIdx.x / 32, h = blockIdx.x;
-  const float *part = L.part + (int64_t)h * kHeadDim + e;
-  const int64_t step = (int64_t)gridDim.x * kHeadDim;
+  constexpr int kFlight = 4;
+  __shared__ double sums[16][32];
+  const int quarter = blockIdx.x & 3, h = blockIdx.x >> 2, e = threadIdx.x % 8 * 4, g = threadIdx.x / 8;
+  const float *part = L.part + (int64_t)h * kHeadDim + 32 * quarter + e;
+  const int64_t step = (int64_t)(gridDim.x / 4) * kHeadDim;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int i = g; i < L.parts; i += 32 * kFlight) {
+  for (int i = g; i < L.parts; i += 128 * kFlight) {
     f32x4 v[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       v[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (i + 32 * k < L.parts) v[k] = *reinterpret_cast<const f32x4 *>(part + (i + 32 * k) * step);
+      if (i + 128 * k < L.parts) v[k] = *reinterpret_cast<const f32x4 *>(part + (i + 128 * k) * step);
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
@@ -311,17 +365,20 @@ __global__ __launch_bounds__(1024) void norm_rope_join_kernel(NormRopeBackwardLa
     }
   }
 #pragma unroll
-  for (int c = 0; c < 4; ++c) s[c] += __shfl_xor(s[c], 32);
-  if (threadIdx.x % 64 < 32) {
+  for (int c = 0; c < 4; ++c) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) sums[g / 2][e + c] = s[c];
+    for (int o = 8; o < 64; o <<= 1) s[c] += __shfl_xor(s[c], o);
+  }
+  if (threadIdx.x % 64 < 8) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sums[threadIdx.x / 64][e + c] = s[c];
   }
   __syncthreads();
-  if (threadIdx.x >= kHeadDim) return;
+  if (threadIdx.x >= 32) return;
   double all = 0.0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) all += sums[i][threadIdx.x];
-  L.dweight[(int64_t)h * kHeadDim + threadIdx.x] = (float)all;
+  L.dweight[(int64_t)h * kHeadDim + 32 * quarter + threadIdx.x] = (float)all;
 }
 
 // Blocks of eight rows of a token in order: of its keys, its queries, its values.  A block holds rows of one kind, so that
@@ -376,8 +433,11 @@ __global__ __launch_bounds__(64 * kForwardWaves) void append_norm_kernel(AppendN
     else if (w.part == 0 && (threadIdx.x & 63) == 0 && L.status)
       atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   }
-  float2 t[8] = {};
-  if (p.rot.freq) make_turns(p.rot, p.pos ? (int64_t)((const const_i32 *)p.pos)[w.t] : pos, cs[wave], t);
+  Turns<ODD> turns = {};
+  if (p.rot.freq) {
+    make_turns(p.rot, p.pos ? (int64_t)((const const_i32 *)p.pos)[w.t] : pos, cs[wave]);
+    turns = turns_of<ODD>(p.rot, turned, cs[wave]);
+  }
   for (; b < blocks; b += w.waves, x = next, g = next_g) {
     if (b + w.waves < blocks) next = load(b + w.waves), next_g = weights(b + w.waves);
     const int kind = kind_of(b), h = head_of(b);
@@ -394,7 +454,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) void append_norm_kernel(AppendN
       normalise(v, norm.eps);
       multiply(v, g);
     }
-    turn_part<ODD, 1>(p.rot, turned, v, t, cs[wave], odd);
+    turn_part<ODD, 1>(p.rot, turned, v, turns, odd);
     if (here)
       store_part(turned, kind == kKey ? L.K + base + h * p.pages.head_stride
                                       : L.q_out + w.t * p.q_out_rows.token_stride + h * p.q_out_rows.head_stride, v);
@@ -403,10 +463,11 @@ __global__ __launch_bounds__(64 * kForwardWaves) void append_norm_kernel(AppendN
 
 namespace {
 bool odd(const ebd_rotary &R) { return R.freq && R.layout == EBD_ROPE_HALF && R.rot_dim % 16; }
-// us with the join, by 256 / 512 / 768 / 1024 work-groups: 8191 tokens of 40 rows, weights of their own 72.5 / 55.2 / 65.7 /
-// 76.2 (more partial sums; without the rows on their way 60 by 512), of 32 with shared ones 68.2 / 46.0 / 43.1 / 43.3, 2048
-// of 32 22.0 / 18.1 / 18.0 / 19.1
-constexpr int64_t kBackwardGroups = 512;
+// Work-groups of more than four waves: one a CU, since a wave that shares its SIMD with another of its group keeps the others
+// waiting at the barrier.  us with the join, by 128 / 256 / 384 / 512 / 768 work-groups: 8191 tokens of 40 rows, weights of
+// their own (five waves) 85 / 51 / 65 / 57 / 62, 1000 of 40 18.9 / 15.8 / 20.5 / 21.3 / 25.6, 8191 of 32 with shared ones (four
+// waves) 79 / 46 / 42 / 38 / 39, 4212 of 7 with their own 18.3 / 13.8 / 12.7 / 12.0 / 12.9.
+constexpr int64_t kBackwardGroups = 512, kBackwardWide = 256;
 constexpr int64_t kBackwardChain = 256;  // most token groups of a work-group: as many fp32 additions in a row
 }  // namespace
 
@@ -438,9 +499,9 @@ NormRopeBackwardLaunch norm_rope_backward_plan(const ebd_norm_rope_backward_para
   L.p = p;
   cut_tokens(p.num_heads, &L.per, &L.tpb, kBackwardRows);
   const int64_t groups = ((int64_t)p.num_tokens + L.tpb - 1) / L.tpb, blocks = (p.num_heads + kBackwardRows - 1) / kBackwardRows;
-  L.groups = (int32_t)std::min<int64_t>(groups, std::max<int64_t>(std::max<int64_t>(1, kBackwardGroups / blocks),
-                                                                  (groups + kBackwardChain - 1) / kBackwardChain));
-  L.parts = p.norm.head_stride ? L.groups * L.tpb : (int32_t)(L.groups * blocks);
+  const int64_t fill = std::max<int64_t>(1, (L.per > 256 ? kBackwardWide : kBackwardGroups) / blocks);
+  L.groups = (int32_t)std::min<int64_t>(groups, std::max<int64_t>(fill, (groups + kBackwardChain - 1) / kBackwardChain));
+  L.parts = p.norm.head_stride ? L.groups : (int32_t)(L.groups * blocks);
   return L;
 }
 
@@ -460,7 +521,7 @@ hipError_t launch_norm_rope_backward(const NormRopeBackwardLaunch &L, hipStream_
 
 hipError_t launch_norm_rope_join(const NormRopeBackwardLaunch &L, hipStream_t s) {
   const unsigned heads = L.p.norm.head_stride ? L.p.num_heads : 1;
-  hipLaunchKernelGGL(norm_rope_join_kernel, dim3(heads), dim3(1024), 0, s, L);
+  hipLaunchKernelGGL(norm_rope_join_kernel, dim3(4 * heads), dim3(1024), 0, s, L);
   return hipGetLastError();
 }
 

@@ -12,14 +12,15 @@ namespace ebd {
 
 constexpr int kRopeRows = 128;  // most rows of a work-group: 8 lanes each
 
-// cos and sin (times the amplitude) of pair `i` at position `pos`.
-__device__ __forceinline__ float2 turn(const ebd_rotary &R, int i, int64_t pos) {
-  const double t = (double)pos * R.freq[i] * 0.15915494309189535;  // 1 / 2 pi
+// cos and sin (times the amplitude) of the pair of frequency `freq` at position `pos`.
+__device__ __forceinline__ float2 turn_by(const ebd_rotary &R, double freq, int64_t pos) {
+  const double t = (double)pos * freq * 0.15915494309189535;  // 1 / 2 pi
   float s, c;
   sincospif(2.0f * (float)(t - rint(t)), &s, &c);
   if (R.flags & EBD_ROPE_INVERSE) s = -s;
   return make_float2(R.amplitude * c, R.amplitude * s);
 }
+__device__ __forceinline__ float2 turn(const ebd_rotary &R, int i, int64_t pos) { return turn_by(R, R.freq[i], pos); }
 
 // How the eight lanes of a row split it: lane l's two 16-byte chunks (elements), and whether the second
 // elements of the first chunk's pairs are the second chunk (halves), which needs rot_dim / 2 to be whole
