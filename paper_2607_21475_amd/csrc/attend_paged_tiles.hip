@@ -23,8 +23,8 @@
 //   tile, whatever the depth of its loads (three or four tiles on their way: the same), a chain of products, weights and
 //   products; two groups take two tiles in that time, as two work-groups would, but leave half as many partial sums.  Four
 //   sequences of up to 300 tokens, 4 heads of 7, under a window of 2048: 51 us, with work-groups of four waves 58 (three
-//   splits), 77 (one).  32 sequences of 64 tokens over 16384 rows, 8 heads of 4, by blocks of 256: 606 to 627 us (0.88 to
-//   0.91 PFLOP/s, keys read once at 3.5 TB/s), by 128: 650; from keys that caches hold 520, as far as the power limit goes.
+//   splits), 77 (one).  32 sequences of 64 tokens over 16384 rows, 8 heads of 4, by blocks of 256: 596 to 627 us (0.88 to
+//   0.92 PFLOP/s, keys read once at 3.5 TB/s), by 128: 650; from keys that caches hold 520, as far as the power limit goes.
 //   The matrix products bound it: 4 x 128 operations per (query row, key).  So the weights of the first two shapes are
 //   rounded to bf16 (half a step, 2^-8, averaged over a row's keys); a second product with their tails, 16 bits in all,
 //   costs 20 to 40% (8192 tokens over 8192 rows 770 us with it, 566 without, 1024 over 131072 2930 / 2070, 1024 over 1024
@@ -309,6 +309,20 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     const uint32_t bad = bad_of(k);
     if (!partial(k, bad)) return;
     bool any = false;
+    // (all tiles of new rows come here; most hold nothing that a weight of zero would not hide, and are only looked at: 22
+    // sequences of 304 tokens over 3 rows 64.5 us noting always, 55.5 so, four of up to 300 under a window 54.5 / 52)
+    if constexpr (TREE) {
+#pragma unroll
+      for (int i = 0; i < kPart / 4; ++i) {
+        const u32x4 v = lds_read<u32x4>(tile_of(stage) + kTile + (kPart * rw + (lane >> 4) + 4 * i) * kRowBytes + (lane & 15) * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= not_finite(v[e]) | not_finite(v[e] << 16);
+      }
+      any = __any(any);
+      if (lane == 0) noted[stage][kg][rw] = any;
+      if (!any) return;
+      any = false;
+    }
 #pragma unroll
     for (int i = 0; i < kPart / 4; ++i) {
       const int r = kPart * rw + (lane >> 4) + 4 * i;
@@ -354,7 +368,10 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
     if (!partial(k, bad) || !__any(lane < RW && noted[stage][kg][lane & (RW - 1)])) return;
     start_notes();
 #pragma unroll 1
-    for (int r = 0; r < KEYS; ++r) keep_note(k + r, lane < 16 ? notes[stage][kg][r][lane] : 0u);
+    for (int r = 0; r < KEYS; ++r) {
+      if (TREE && !noted[stage][kg][r / kPart]) continue;  // (that wave wrote none)
+      keep_note(k + r, lane < 16 ? notes[stage][kg][r][lane] : 0u);
+    }
     wave_sync();
   };
   auto mine = [&](int k) { return k < min(R.hi, k_end) && k + KEYS > R.lo; };  // whether this wave's rows see the tile
