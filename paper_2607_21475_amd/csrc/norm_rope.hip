@@ -243,9 +243,9 @@ __global__ __launch_bounds__(64 * kForwardWaves) void norm_rope_kernel(NormRopeL
 constexpr int kBackwardRows = 64;  // (128 of them leave too few registers)
 
 // A work-group takes every gridDim.x'th group of tokens; a thread's head stays the same, so that its share of dw waits in
-// registers; the next group's rows are on their way meanwhile.  Shared weights: the work-group's rows are added up (within a wave, then through LDS) and leave one row of
-// sums; weights of each head's own: the token slots'
-// rows are added up, and leave one for every head.
+// registers; the next group's rows are on their way meanwhile.  Shared weights: the work-group's rows are added up (within a
+// wave, then through LDS) and leave one row of sums; weights of each head's own: the token slots' rows are added up, and leave
+// one for every head.
 template <bool ODD, bool SHARED>
 __global__ __launch_bounds__(8 * kBackwardRows) void norm_rope_backward_kernel(NormRopeBackwardLaunch L) {
   __shared__ float2 cs[2][4][kHeadDim / 2];
@@ -497,8 +497,9 @@ hipError_t launch_norm_rope(NormRopeLaunch L, hipStream_t s) {
 NormRopeBackwardLaunch norm_rope_backward_plan(const ebd_norm_rope_backward_params &p) {
   NormRopeBackwardLaunch L{};
   L.p = p;
-  cut_tokens(p.num_heads, &L.per, &L.tpb, kBackwardRows);
-  const int64_t groups = ((int64_t)p.num_tokens + L.tpb - 1) / L.tpb, blocks = (p.num_heads + kBackwardRows - 1) / kBackwardRows;
+  const int32_t heads = std::max(p.num_heads, 1);  // (without heads the sums of shared weights are written, as zeros)
+  cut_tokens(heads, &L.per, &L.tpb, kBackwardRows);
+  const int64_t groups = ((int64_t)p.num_tokens + L.tpb - 1) / L.tpb, blocks = (heads + kBackwardRows - 1) / kBackwardRows;
   const int64_t fill = std::max<int64_t>(1, (L.per > 256 ? kBackwardWide : kBackwardGroups) / blocks);
   L.groups = (int32_t)std::min<int64_t>(groups, std::max<int64_t>(fill, (groups + kBackwardChain - 1) / kBackwardChain));
   L.parts = p.norm.head_stride ? L.groups : (int32_t)(L.groups * blocks);

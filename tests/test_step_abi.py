@@ -222,3 +222,12 @@ def test_keep_refusals():
         assert _keep(**kw) == BAD, kw
     assert _keep(pages=_pages(num_seqs=1 << 24)) == UNSUPPORTED and _keep(max_kept=1 << 24) == UNSUPPORTED
     assert _keep(pages=_pages(num_seqs=0)) == OK
+
+
+def test_sizes_of_calls_without_tokens_heads_or_sequences():
+    """Workspace sizes are numbers whatever is zero (a division by any of these would end the process)."""
+    for heads in (0, 1, 200):
+        for tokens in (0, 1, 100000):
+            for stride in (0, 128):
+                code, size = _backward(num_heads=heads, num_tokens=tokens, norm=_norm(head_stride=stride), ws=None)
+                assert size >= 256 and code in ((OK,) if not heads and stride else (NO_WS,))
