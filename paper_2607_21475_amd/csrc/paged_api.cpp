@@ -163,7 +163,7 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, bool tree,
   int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
   // (a tree's blocks all see to their sequence's end: one more than fill a round costs another, so that the ones that are
   // not full are counted, half a sequence each)
-  if (tree && !L.blocks) full = std::min<int64_t>(L.units, sum / rows + (S + 1) / 2);
+  if (tree && !L.blocks) full = std::max<int64_t>(1, std::min<int64_t>(L.units, sum / rows + (S + 1) / 2));
   L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
   if (tiles && tree) {
     const double speed = pairs ? kPairsSpeed : rows == kTileRows ? 1.0 : kLongSpeed;

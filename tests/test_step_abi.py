@@ -231,3 +231,11 @@ def test_sizes_of_calls_without_tokens_heads_or_sequences():
             for stride in (0, 128):
                 code, size = _backward(num_heads=heads, num_tokens=tokens, norm=_norm(head_stride=stride), ws=None)
                 assert size >= 256 and code in ((OK,) if not heads and stride else (NO_WS,))
+    for seqs in (0, 1, 5, 3000):
+        for tokens in (0, 1, 100, 40000):
+            for new in (0, 1, 8, 64, 500):
+                for window in (0, 7):
+                    kw = dict(pages=_pages(num_seqs=seqs), num_tokens=tokens, max_new=new, window=window, max_rows=5000)
+                    p = _tree_params(words=8, **kw)
+                    assert LIB.ebd_workspace_size(ebd.EBD_WS_ATTEND_TREE, ctypes.byref(p)) >= 256, (seqs, tokens, new)
+                    assert LIB.ebd_workspace_size(ebd.EBD_WS_ATTEND_PAGED, ctypes.byref(p.attend)) >= 256
