@@ -499,8 +499,8 @@ ebd_status ebd_append_norm(const ebd_append_norm_params *n, const uint16_t *k_ne
 ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *workspace, size_t ws_bytes, void *stream) {
   if (!valid_plan_step(p)) return EBD_ERR_INVALID_ARG;
   if (!supported_plan_step(p)) return EBD_ERR_UNSUPPORTED;
-  if (p->num_seqs == 0) return EBD_OK;
-  if (!p->count || !p->len || !p->page_table || !p->free_pages || !p->free_state || !p->new_off) return EBD_ERR_INVALID_ARG;
+  if (p->num_seqs > 0 && (!p->count || !p->len || !p->page_table)) return EBD_ERR_INVALID_ARG;
+  if (!p->free_pages || !p->free_state || !p->new_off) return EBD_ERR_INVALID_ARG;
   if (!workspace || ws_bytes < plan_bytes(*p) || ((uintptr_t)workspace & 255)) return EBD_ERR_WORKSPACE;
   const ebd_status ds = device_ok();
   if (ds != EBD_OK) return ds;

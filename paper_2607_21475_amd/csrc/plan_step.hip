@@ -177,6 +177,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_fill_kernel(PlanStepLaunch 
   __shared__ int64_t sums[kPlanWaves][3];
   const ebd_plan_step_params &p = L.p;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, s0 = blockIdx.x * kPlanWaves, s = s0 + wave;
+  if (p.num_seqs == 0 && threadIdx.x == 0) p.new_off[0] = 0;
   // tokens, pages taken and pages given back by the sequences before this one
   int64_t t = 0, take = 0, back = 0;
   for (int i = threadIdx.x; i < s0; i += kPlanThreads) {
@@ -407,7 +408,7 @@ hipError_t launch_plan_step(const PlanStepLaunch &L, hipStream_t s) {
     hipLaunchKernelGGL(plan_one_kernel, dim3(1), dim3(kOneThreads), 0, s, L);
     return hipGetLastError();
   }
-  const dim3 block(kPlanThreads), seqs((unsigned)((p.num_seqs + kPlanWaves - 1) / kPlanWaves));
+  const dim3 block(kPlanThreads), seqs((unsigned)std::max(1, (p.num_seqs + kPlanWaves - 1) / kPlanWaves));
   hipLaunchKernelGGL(plan_count_kernel, seqs, block, 0, s, L);
   hipLaunchKernelGGL(plan_fill_kernel, seqs, block, 0, s, L);
   if (p.num_tokens > 0 && p.parent) {

@@ -33,7 +33,7 @@ def _run(count, lens, table, page, ring, state, room, parent=None, words=0, want
 
     dev = dict(device="cuda")
     t = {"count": torch.tensor(count, dtype=I32, **dev), "len": torch.tensor(lens, dtype=I32, **dev),
-         "table": torch.tensor(table, dtype=I32, **dev).view(len(lens), -1), "ring": torch.tensor(ring, dtype=I32, **dev),
+         "table": torch.tensor(table, dtype=I32, **dev).view(len(lens), -1 if lens else 4), "ring": torch.tensor(ring, dtype=I32, **dev),
          "state": torch.tensor(state, dtype=I32, **dev), "new_off": torch.full((len(lens) + 1,), 7, **dev)}
     t["slots"] = torch.full((room,), 7, **dev) if want_slots else None
     t["pos"] = torch.full((room,), 7, dtype=I32, **dev) if want_pos else None
@@ -199,3 +199,13 @@ def test_plan_from_a_ring_of_bad_pages(seqs):
     want = step.plan(count, lens, table, 16, ring, state, 50 * seqs)
     assert 0 < sum(x > 0 for x in want["status"])
     _check(_run(count, lens, table, 16, ring, state, 50 * seqs)[0], want)
+
+
+@pytest.mark.parametrize("room", [3, 5000])
+def test_plan_without_sequences(room):
+    """Every token is padding then: nothing may be left of what slots, positions and masks held."""
+    for parent, words in ((None, 0), ([], 2)):
+        t = _run([], [], torch.zeros((0, 4), dtype=I32).tolist(), 16, [3, 4, 5], [1, 2], room, parent, words)[0]
+        assert t["new_off"].tolist() == [0] and t["state"].tolist() == [1, 2] and t["ring"].tolist() == [3, 4, 5]
+        assert bool((t["slots"] == -1).all()) and bool((t["pos"] == -1).all())
+        assert words == 0 or bool((t["mask"] == 0).all())

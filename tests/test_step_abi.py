@@ -154,7 +154,7 @@ def test_plan_refusals():
         assert _plan(**kw) == (UNSUPPORTED, 0), kw
     need = _plan()[1]
     assert _plan(ws=None)[0] == NO_WS and _plan(ws=FAKE + 8)[0] == NO_WS and _plan(ws_bytes=need - 1)[0] == NO_WS
-    assert _plan(num_seqs=0)[0] == OK
+    assert _plan(num_seqs=0, new_off=None)[0] == BAD  # (its one entry is written, and every token is padding)
 
 
 def test_plans_of_the_binding():
