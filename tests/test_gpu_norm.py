@@ -186,6 +186,29 @@ def test_norm_long_sums():
     ref.check(_backward(x, dy, torch.empty_like(x), ebd.head_norm(w, EPS), None, None, w.shape), dw, tw, "dw")
 
 
+@pytest.mark.parametrize("tokens,heads,own", [(3000001, 1, False), (300001, 2, True)])
+def test_norm_many_tokens(tokens, heads, own):
+    """Work-groups of hundreds of tokens each, and a launch of millions of waves' shares."""
+    import paper_2607_21475_amd as ebd
+
+    g = _gen(10)
+    x, dy = ref.spaced((tokens, heads, 128), g, False), ref.spaced((tokens, heads, 128), g, False)
+    w, f = _weights(g, heads, own), step.frequencies(128)
+    pos = torch.arange(tokens, device="cuda", dtype=torch.int32)
+    norm, r = ebd.head_norm(w, EPS), ebd.rotary(f)
+    y, gx = torch.empty_like(x), torch.empty_like(x)
+    ebd.ebd_norm_rope(ebd.norm_rope_params(x, y, norm, r, pos), x, y)
+    gw = _backward(x, dy, gx, norm, r, pos, w.shape)
+    dw = tw = 0.0
+    for a in range(0, tokens, 200000):
+        b = slice(a, min(a + 200000, tokens))
+        ref.check(y[b], *step.norm_rope(x[b], w, EPS, pos[b], f), "y")
+        (dx, tx), (p, tp) = step.norm_rope_gradients(x[b], w, EPS, dy[b], pos[b], f)
+        ref.check(gx[b], dx, tx, "dx")
+        dw, tw = dw + p, tw + tp
+    ref.check(gw, dw, tw, "dw")
+
+
 # ---- append ------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("lens,news,kv,heads,page,order,rot,layout,fused,given,own,which", [

@@ -65,7 +65,7 @@ CASES = [
     (1, 3, 4096, 32, 140, True, 64, 0, 0), (5, 40, 7, 16, 20, True, 2, 1, 0.2), (64, 4000, 1, 16, 70, False, 0, 0, 0),
     (63, 900, 66, 64, 200, True, 2, 9, 0.1), (300, 200, 3, 16, 400, False, 0, 40, 0), (257, 70, 61, 16, 1500, True, 1, 17, 0),
     (1000, 64, 5, 16, 900, True, 1, 100, 0), (700, 300, 1, 128, 800, False, 0, 0, 0.05), (40, 9000, 700, 16, 2100, False, 0, 5, 0),
-    (4100, 20, 2, 16, 5000, False, 0, 50, 0), (33, 2, 300, 16, 900, True, 5, 0, 0),
+    (4100, 20, 2, 16, 5000, False, 0, 50, 0), (65536, 3, 1, 16, 9000, False, 0, 300, 0), (33, 2, 300, 16, 900, True, 5, 0, 0),
 ]
 
 

@@ -319,3 +319,40 @@ def test_tree_in_a_graph_and_on_two_streams():
             ebd.ebd_attend_tree(p, q, c.K, c.V, o, w)
     torch.cuda.synchronize()
     assert all(torch.equal(o, y) for o, _, _ in outs)
+
+
+@pytest.mark.parametrize("held,news,kv,G,window", [
+    ([70, 9, 300], [5, 0, 3], 2, 4, 0), ([500, 20], [3, 1], 1, 40, 0), ([64, 0, 17, 900], [0, 4, 0, 90], 1, 33, 50),
+    ([3, 2000], [1, 40], 2, 17, 0), ([0] * 40, [s % 3 for s in range(40)], 2, 4, 0), ([10] * 3, [0, 0, 0], 2, 4, 0),
+])
+def test_tree_many_heads_and_sequences_without_tokens(held, news, kv, G, window):
+    rng = random.Random(sum(held) + G)
+    lens = [h + m for h, m in zip(held, news)]
+    c = ref.Cache(lens, kv, 16, _gen(G))
+    words = max(1, -(-max(news) // 64))
+    mask, pos = [], []
+    for h, m in zip(held, news):
+        a, d = step.masks_of(step.tree(m, rng), words)
+        mask += a
+        pos += [h + x for x in d]
+    if not mask:  # padding tokens alone
+        q, y, lse, st = _none(c, news, G)
+        assert bool((y == 7).all()) and bool((lse == 7).all()) and not bool(st.any())
+        return
+    q, y, lse, st = _call(c, news, G, mask, pos, window=window, pad=1)
+    assert not bool(st.any())
+    _check(c, news, G, mask, pos, q, y, lse, window, few=6)
+
+
+def _none(c, news, G):
+    import paper_2607_21475_amd as ebd
+
+    q = ref.spaced((2, c.kv * G, 128), _gen(1), False)
+    y, lse = torch.full_like(q, 7.0), torch.full((2, c.kv * G), 7.0, device="cuda")
+    off = torch.zeros(len(news) + 1, dtype=torch.int64, device="cuda")
+    st = torch.zeros(len(news), dtype=torch.int32, device="cuda")
+    p = ebd.attend_tree_params(ebd.pages(c.K, c.V, c.table), q, y, off, c.len, 4, max(c.lens),
+                               torch.full((2, 1), -1, dtype=torch.int64, device="cuda"))
+    ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_TREE, p))
+    ebd.ebd_attend_tree(p, q, c.K, c.V, y, ws, lse=lse, status=st)
+    return q, y, lse, st
