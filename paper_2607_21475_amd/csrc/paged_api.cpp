@@ -111,15 +111,18 @@ constexpr int64_t kRowsLeast = 128;  // fewest rows of a split: a tile for each 
 constexpr int64_t kTilesLeast = 256;
 constexpr int64_t kStartRows = 320;
 constexpr int64_t kTilesStartRows = 640;
-constexpr double kPairsSpeed = 1.9, kLongSpeed = 1.09;  // of attend_tiles' shapes for trees
+constexpr double kPairsSpeed = 1.8, kLongSpeed = 1.09;  // of attend_tiles' shapes for trees
+constexpr int64_t kRaggedStartRows = 400;
 constexpr double kTilesJoin = 250.0;  // (and a row for each 128 query rows' sums, 135 KB written and read)
 constexpr double kRowsJoin = 300.0;
 constexpr int64_t kSplitsMost = 256;
 constexpr int64_t kCacheBytes = (int64_t)64 << 20;
 
-// (speed: keys that a work-group takes in the time of one; total: receives the cost)
+// (speed: keys that a work-group takes in the time of one; ragged: the sequences are taken to have from the most rows down
+// to none, so that a launch of more than a round takes half of the most on average and ends half of a work-group of the
+// longest behind that; total: receives the cost)
 int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_t start, double join, double join_each,
-               double speed = 1.0, double *total = nullptr) {
+               double speed = 1.0, bool ragged = false, double *total = nullptr) {
   const int64_t most = std::min<int64_t>(kSplitsMost, std::max<int64_t>(1, span / least));
   int64_t best = 1;
   double cost = 0.0;
@@ -127,8 +130,13 @@ int64_t splits(int64_t units, int64_t span, int64_t slots, int64_t least, int64_
     const int64_t ns = std::min(most, i < 8 ? i + 1 : std::max<int64_t>(1, (i - 7) * slots / units));
     const int64_t rows = ((span + ns - 1) / ns + 127) / 128 * 128;
     const int64_t groups = units * ((span + rows - 1) / rows);  // (rounded up, the size may leave fewer splits)
-    const double rounds = groups <= 2 * slots ? (double)((groups + slots - 1) / slots) : (double)groups / (double)slots + 0.5;
-    const double c = rounds * ((double)rows / speed + (double)start) + (ns > 1 ? join + join_each * (double)groups : 0.0);
+    const double fill = (double)groups / (double)slots, longest = (double)rows / speed + (double)start;
+    double c = longest;
+    if (ragged && groups > slots)
+      c = fill * (0.5 * (double)rows / speed + (double)start) + 0.5 * longest;
+    else if (!ragged)
+      c = longest * (groups <= 2 * slots ? (double)((groups + slots - 1) / slots) : fill + 0.5);
+    if (ns > 1) c += join + join_each * (double)groups;
     if (i == 0 || c < cost) best = ns, cost = c;
   }
   if (total) *total = cost;
@@ -161,15 +169,25 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, bool tree,
     span = std::min<int64_t>(span, (int64_t)p->window + (tree ? p->max_new : rows / p->group) + 1);
   span = std::max<int64_t>(span, 1) + (p->window > 0 ? 63 : 0);
   int64_t full = std::max<int64_t>(1, L.blocks ? L.units : sum / rows);  // blocks that have work to do
+  // Trees whose tokens are far fewer than their sequences could have differ, and so, most likely, do the rows they lie
+  // over.  us as if all were alike / so, 8 KV heads of 4 query heads, up to the most tokens over up to the most rows: 6 of
+  // 100 over 8192 120 / 84, 8 of 60 over 16384 146 / 119, 24 of 48 over 16384 402 / 270, 20 of 96 over 16384 474 / 332, 4 of
+  // 120 over 16384 126 / 93; over rows that are all alike: 24 of 48 467 / 343, 16 of 64 over 16384 293 / 313, 24 of 64
+  // over 4096 134 / 152, 20 of 60 over 8192 204 / 242.
+  const bool ragged = tree && tiles && S > 1 && 4 * sum < 3 * S * rows_max;
   // (a tree's blocks all see to their sequence's end: one more than fill a round costs another, so that the ones that are
   // not full are counted, half a sequence each)
-  if (tree && !L.blocks) full = std::max<int64_t>(1, std::min<int64_t>(L.units, sum / rows + (S + 1) / 2));
+  if (tree && (ragged || !L.blocks)) {
+    const int64_t taken = std::min<int64_t>(S, sum / std::max<int64_t>(p->group, more_than + 1));
+    full = std::max<int64_t>(1, std::min<int64_t>(L.units, sum / rows + (taken + 1) / 2));
+  }
   L.least = (int32_t)(tiles ? kTilesLeast : kRowsLeast);
   if (tiles && tree) {
     const double speed = pairs ? kPairsSpeed : rows == kTileRows ? 1.0 : kLongSpeed;
     L.pairs = pairs;
-    L.nsplit = (int32_t)splits(full * H, span, rows == kTileRows && !pairs ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows,
-                               kTilesJoin, (double)rows / kTileRows, speed, cost);
+    L.nsplit = (int32_t)splits(full * H, span, rows == kTileRows && !pairs ? 2 * kCus : kCus, kTilesLeast,
+                               ragged ? kRaggedStartRows : kTilesStartRows, kTilesJoin, (double)rows / kTileRows, speed,
+                               ragged, cost);
   } else if (tiles) {
     L.nsplit = (int32_t)splits(full * H, span, rows == kTileRows ? 2 * kCus : kCus, kTilesLeast, kTilesStartRows,
                                kTilesJoin, (double)rows / kTileRows);
@@ -212,21 +230,22 @@ bool long_blocks(const ebd_attend_paged_params *p, int64_t most) {
   return groups <= kCus && 8 * groups >= 7 * kCus && 8 * most >= 7 * rows;
 }
 // The shape of a tree's blocks of 128 query rows or more: two work-groups of 128 rows a CU (A), one of 128 rows by eight waves
-// that takes two tiles at a time (B), or one of 256 rows (C, where these are full).  By the cost of each, in which A's two take
+// that takes two tiles at a time (B), or one of 256 rows (C, unless a sequence's last has work for half of it only).  By the cost of each, in which A's two take
 // a key each in the time of one, B's two keys and C's one and a little (it loads every key for twice as many rows).  All
 // blocks of a tree see to its end, so that short launches are alike and nothing ends early beside a longer one.
 // us of A / B / C with their best splits, 8 KV heads of 4 query heads unless said: one sequence, 64 tokens over 4096 rows
 // 25.7 / 24.1 / 28.1, over 32768 66.7 / 51.5 / 73.4; 128 over 16384 55.9 / 51.7 / 53.4; 16 of 48 over 4096 100 / 82 / -;
 // 8 of 32 over 8192 69 / 60 / -; four of up to 300, 4 heads of 7, under a window of 2048 58.6 / 51.6 / 58.1; 24 of 64 over
 // 4096 155 / 164 / 129; 32 of 64 over 8192 340 / 337 / 310; 64 of 64 over 4096 355 / 355 / 316; 64 of 30 over 2048 118 /
-// 124 / -.
+// 124 / -.  Blocks of 256 that are not full, where two of 128 are not either: 32 of 40 over 16384 605 / 582 / 487, 10 of 40 over
+// 32768 368 / 400 / 332, 5 of 48 over 8192 62 / 60 / 59, 40 of 100 over 8192 748 / 728 / 712.
 AttendPagedLaunch tree_part(const ebd_attend_paged_params *p, int64_t rows_max, int64_t sum, int64_t more_than) {
   double a = 0.0, b = 0.0, c = 0.0;
   AttendPagedLaunch L = attend_paged_part(p, true, kTileRows, rows_max, sum, more_than, false, &a);
   const AttendPagedLaunch B = attend_paged_part(p, true, kTileRows, rows_max, sum, more_than, true, &b);
   if (b < a) L = B, a = b;
-  const int64_t S = p->pages.num_seqs, aside = (rows_max + kLongRows - 1) / kLongRows;
-  if (8 * rows_max < 7 * aside * kLongRows || 8 * sum < 7 * S * aside * kLongRows) return L;
+  const int64_t tiles = (rows_max + kTileRows - 1) / kTileRows, aside = (rows_max + kLongRows - 1) / kLongRows;
+  if (8 * tiles * kTileRows < 7 * aside * kLongRows) return L;
   const AttendPagedLaunch C = attend_paged_part(p, true, kLongRows, rows_max, sum, more_than, false, &c);
   return c < a ? C : L;
 }

@@ -356,3 +356,31 @@ def _none(c, news, G):
     ws = ebd.workspace(ebd.ebd_workspace_size(ebd.EBD_WS_ATTEND_TREE, p))
     ebd.ebd_attend_tree(p, q, c.K, c.V, y, ws, lse=lse, status=st)
     return q, y, lse, st
+
+
+@pytest.mark.parametrize("seqs,new,least,context,kv,G,window", [
+    (24, 40, 40, 600, 8, 4, 0),     # blocks of 256 query rows, 160 of them taken
+    (12, 64, 0, 3000, 8, 4, 0),     # token counts down to none, over 0 to 3000 rows
+    (6, 100, 1, 2500, 4, 4, 0),
+    (20, 55, 0, 700, 2, 7, 90),
+    (40, 70, 1, 300, 4, 2, 0),
+    (3, 200, 1, 5000, 1, 4, 2000),
+])
+def test_tree_batches_of_different_lengths(seqs, new, least, context, kv, G, window):
+    rng = random.Random(seqs + new)
+    held = [context] + [rng.randrange(context) for _ in range(seqs - 2)] + [0]
+    news = [new] + [rng.randint(least, new) for _ in range(seqs - 2)] + [least]
+    if least < new:
+        news[1:seqs - 1] = [m * m // new for m in news[1:seqs - 1]]  # few tokens for most
+    lens = [h + m for h, m in zip(held, news)]
+    c = ref.Cache(lens, kv, 16, _gen(seqs), fill=math.nan)
+    words = -(-new // 64)
+    mask, pos = [], []
+    for h, m in zip(held, news):
+        a, d = step.masks_of(step.tree(m, rng), words)
+        mask += a
+        pos += [h + x for x in d]
+    q, y, lse, st = _call(c, news, G, mask, pos, window=window, pad=3)
+    assert not bool(st.any())
+    assert bool((y[sum(news):] == 7).all()) and bool((lse[sum(news):] == 7).all())
+    _check(c, news, G, mask, pos, q, y, lse, window, few=3 if seqs * kv > 100 else 6)
