@@ -648,7 +648,9 @@ ebd_status ebd_plan_step(const ebd_plan_step_params *p, uint32_t *status, void *
  *   mask_words  1 .. 64.
  *   attend.qpos positions of the tokens, or NULL; a token with a negative position sees nothing, whatever its mask.  The window
  *               does not apply to new tokens, which the mask alone chooses.
- * Everything else is as for ebd_attend_paged (outputs, bounds, status, rounding of weights, values that are not finite).
+ * Everything else is as for ebd_attend_paged (outputs, bounds, status, rounding of weights, values that are not finite), but
+ * that weights of 8 bits, from 65 query rows of a sequence on, are divided by the sum of what they were rounded to: y may be
+ * off by 2^-8 of the weighted mean of |v - y|, beside its own rounding.
  * workspace: ebd_workspace_size(EBD_WS_ATTEND_TREE, p) bytes, 256-byte aligned.
  */
 typedef struct ebd_attend_tree_params {

@@ -28,7 +28,10 @@
 //   The matrix products bound it: 4 x 128 operations per (query row, key).  So the weights of the first two shapes are
 //   rounded to bf16 (half a step, 2^-8, averaged over a row's keys); a second product with their tails, 16 bits in all,
 //   costs 20 to 40% (8192 tokens over 8192 rows 770 us with it, 566 without, 1024 over 131072 2930 / 2070, 1024 over 1024
-//   38.7 / 32.0).  The third shape is bound by memory and has it (the call above with its join 42.0 / 40.9).  1024 tokens, 32
+//   38.7 / 32.0).  Each key's rounding is its own, and few keys rule many rows, so that trees divide by the sum of the rounded
+//   weights (dot products of their pairs with ones; lse keeps the exact sum): y is then off by 2^-8 of the weighted mean of |v - y|,
+//   not of |v|, nothing where one key rules or values are alike.  Costs 1 to 4%, a second product 25 to 45% (the trees above 634 us,
+//   621 without, 891 with tails; the four sequences 53, 51, 72).  The third shape is bound by memory and has it (the call above with its join 42.0 / 40.9).  1024 tokens, 32
 //   heads, over 131072 rows: 1.95 to 2.06 ms, 1.06 to 1.12 PFLOP/s; the matrix cores are busy 54% of the
 //   cycles, of which the power limit leaves about 2.0 to 2.1 GHz (a large product runs at 1.34 PFLOP/s there).
 #include "attend_paged.hpp"
@@ -38,6 +41,7 @@ namespace ebd {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLazy = 8.0f;
 
@@ -94,6 +98,7 @@ template <int RW, int KG, int KEYS, bool NT, bool TREE, bool TAILS = (KG > 1)>
 __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPagedLaunch L) {
   constexpr int kWaves = RW * KG, kRows = 32 * RW;
   constexpr int kSub = KEYS / 32;             // blocks of 32 keys of a tile
+  constexpr bool kRounded = TREE && !TAILS;   // the sums are divided by the rounded weights' total
   constexpr bool kTails = TAILS;              // weights as a bf16 head and a bf16 tail, not a head alone
   constexpr int kPart = KEYS / RW;            // rows of a tile that a wave loads
   constexpr int kTile = KEYS * kRowBytes;     // bytes of a tile's K, or of its V
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   f32x16 O[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) O[d] = f32x16{};
-  float m = -INFINITY, z = 0.0f;
+  float m = -INFINITY, z = 0.0f, zr = 0.0f;  // zr: of the weights as they are rounded (kRounded)
   const float sc2 = L.scale * kLog2e;
 
   const uint32_t tiles_at = lds_at(tiles);
@@ -274,6 +279,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       const float a = mn == -INFINITY ? 1.0f : fast_exp2(m - mn);
       m = mn;
       z *= a;
+      if constexpr (kRounded) zr *= a;
 #pragma unroll
       for (int d = 0; d < 4; ++d) O[d] *= a;
     }
@@ -291,6 +297,17 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
       }
     }
     z += (part_z[0] + part_z[1]) + (part_z[2] + part_z[3]);
+    if constexpr (kRounded) {
+      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+      float part_r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int b = 0; b < 2 * kSub; ++b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          part_r[i] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{W[b][2 * i], W[b][2 * i + 1]}, ones, part_r[i], false);
+      }
+      zr += (part_r[0] + part_r[1]) + (part_r[2] + part_r[3]);
+    }
   };
   auto bad_of = [&](int k) {
     uint32_t bad = 0;
@@ -481,6 +498,12 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
         }
         wave_sync();
       }
+    }
+    if constexpr (kRounded) {
+      // as if the rounded weights had the exact ones' total, by which the rest divides (the key at the maximum weighs about 1)
+      const float exact = add_xor32(z), rounded = add_xor32(zr), a = rounded != 0.0f ? exact / rounded : 1.0f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) O[d] *= a;
     }
     // (a NaN weight makes the row's total NaN, and with it what is noted)
     if (poisoned) {
