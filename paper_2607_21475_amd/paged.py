@@ -370,7 +370,8 @@ def rope_params(x, y, pos, rot: ebd_rotary) -> ebd_rope_params:
 
 
 def head_norm(weight, eps: float = 1e-6) -> ebd_norm:
-    """Norms of heads: weights [128] of all heads, or [heads, 128] of each one's own (fp32)."""
+    """Norms of heads: weights [128] of all heads, or [heads, 128] of each one's own (fp32; one row expanded over the heads
+    serves forward calls only)."""
     if not isinstance(weight, torch.Tensor):
         raise TypeError("weight must be a torch.Tensor")
     if weight.dtype != torch.float32:
@@ -424,6 +425,9 @@ def norm_rope_params(x, y, norm: ebd_norm, rot: Optional[ebd_rotary] = None, pos
 def norm_rope_backward_params(x, dy, dx, norm: ebd_norm, rot: Optional[ebd_rotary] = None,
                               pos=None) -> ebd_norm_rope_backward_params:
     """Gradients of norm_rope_params' call with the same norm, rot and pos: dy -> dx (may be dy or x)."""
+    if isinstance(norm, ebd_norm) and norm.keep.dim() == 2 and norm.head_stride == 0:
+        # (the heads' gradients would be added up in the first row, and the others left as they were)
+        raise ValueError("norm has one row of weights, expanded over the heads: give head_norm that row")
     (tokens, heads, _), _ = _layout(x, "x")
     _layout(dy, "dy", heads, tokens)
     _layout(dx, "dx", heads, tokens)
