@@ -776,7 +776,9 @@ def rope_frequencies(rot_dim: int = HEAD_DIM, base: float = 10000.0, scaling: st
 class PagedCache:
     """The pools of one layer and what its sequences hold: K, V [pages, KV heads, rows per page, 128] bf16, page_table
     [sequences, pages per sequence] int32, len [sequences] int32 (all on the device, the caller's to update).  A pool whose
-    pages `plan` deals out has its free ones in the ring free_pages [pages] int32, free_state [2] int32."""
+    pages `plan` deals out has its free ones in the ring free_pages [pages] int32, free_state [2] int32.  The layers of a model
+    are caches with pools of their own that share page_table and len: one of them plans a step, and the last one's `keep`
+    updates len."""
 
     K: torch.Tensor
     V: torch.Tensor
@@ -877,10 +879,11 @@ class PagedCache:
         ebd_attend_tree(p, q, self.K, self.V, y, ws, lse=lse, status=status)
         return {"y": y, "lse": lse, "ws": ws}
 
-    def keep(self, new_off, path, kept, status=None):
+    def keep(self, new_off, path, kept, status=None, update_len: bool = True):
         """Keep the accepted paths path [sequences, most kept] int32 of kept [sequences] int32 tokens; len then counts
-        these alone."""
-        p = keep_rows_params(self.pages, new_off, self.len, path, kept, len_out=self.len)
+        these alone.  Layers whose caches share len (and the table, of one plan) find their rows by it: all but the last one's
+        call need update_len False, which leaves it as it is."""
+        p = keep_rows_params(self.pages, new_off, self.len, path, kept, len_out=self.len if update_len else None)
         ebd_keep_rows(p, self.K, self.V, status=status)
 
     def gather(self, lengths: Sequence[int], status=None):
