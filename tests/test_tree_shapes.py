@@ -20,3 +20,7 @@ def test_batches_have_their_shapes(planner, name):
     for pad in (0, 2):
         (rows, pairs, nsplit), *others = planner(tree_shapes.params(news, held, kv, G, window, pad=pad))
         assert not others and (rows, pairs) == shape and (nsplit > 1) == split, (rows, pairs, nsplit)
+    new, rows = tree_shapes.bounds(name)
+    for kw in (dict(max_new=new), dict(max_rows=rows)):
+        (rows, pairs, nsplit), *others = planner(tree_shapes.params(news, held, kv, G, window, **kw))
+        assert not others and (rows, pairs) == shape and (nsplit > 1) == split, (kw, rows, pairs, nsplit)

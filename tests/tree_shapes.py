@@ -72,3 +72,9 @@ BATCHES = {
     "long_window": ([70, 69, 70], [300, 37, 90], 64, 2, 45, (256, False), False),
     "long_splits": ([130, 128, 130], [3000, 2900, 3000], 16, 1, 0, (256, False), True),
 }
+
+
+def bounds(name):
+    """(max_new, max_rows) a little below a batch's truth, by which it keeps its shape."""
+    news, held, *_ = BATCHES[name]
+    return max(news) - 1, max(h + m for h, m in zip(held, news)) - 3
