@@ -574,7 +574,9 @@ ebd_status ebd_norm_rope_backward(const ebd_norm_rope_backward_params *p, const 
  *   slots  [num_tokens] device int64 or NULL.  Given (by ebd_plan_step), token t goes to slot slots[t] % page_size of page
  *          slots[t] / page_size, and append.new_off, append.len and the page table are not read (they may be NULL);
  *          append.pos is then needed where there is a rotation, and nothing is written, the query included, for a token
- *          whose slot lies outside the pool (-1: padding); status is not written.  No two tokens may have one slot.
+ *          whose slot lies outside the pool (-1: padding, or a new row that got no page, which ebd_plan_step flags: what an
+ *          attention makes of such a token's q_out, which holds what it held, is not its output); status is not written.  No
+ *          two tokens may have one slot.
  *          NULL: as ebd_append_paged.
  */
 typedef struct ebd_append_norm_params {
@@ -610,10 +612,11 @@ ebd_status ebd_append_norm(const ebd_append_norm_params *p, const uint16_t *k_ne
  *                does not fit gets an empty mask and position -1.
  *   num_tokens   room in slots, pos, parent and mask; new_off goes on past it, but nothing else is written there.
  *   status       [num_seqs] uint32 or NULL, or-ed: EBD_ST_BAD_PAGE when new rows are left without a page (the ring is empty
- *                or holds no page of the pool, the table is too short); EBD_ST_BAD_LAYOUT when new tokens have no room in num_tokens or in the mask, a parent
- *                is out of place (taken for -1), or the sequence would hold more than 2^30 rows (it gets none, and keeps
- *                what it has; a negative len counts as 0).
+ *                or holds no page of the pool, the table is too short); EBD_ST_BAD_LAYOUT when new tokens have no room in
+ *                num_tokens or in the mask, a parent is out of place (taken for -1), or the sequence would hold more than
+ *                2^30 rows (it gets none, and keeps what it has; a negative len counts as 0).
  * Pages that several sequences share must not be given back by ending one of them.  At most 65536 sequences, 2^24 - 1 tokens.
+ * The time of a tree grows with the sum of its tokens' depths: chains of thousands of tokens take milliseconds.
  * workspace: ebd_workspace_size(EBD_WS_PLAN_STEP, p) bytes, 256-byte aligned; nothing in it is kept.
  */
 typedef struct ebd_plan_step_params {
@@ -692,18 +695,16 @@ ebd_status ebd_keep_rows(const ebd_keep_rows_params *p, uint16_t *K, uint16_t *V
 #define EBD_WS_ATTEND 1
 #define EBD_WS_SCORES 2
 #define EBD_WS_ATTEND_PAGED 3
+#define EBD_WS_ATTEND_TREE 4
 #define EBD_WS_NORM_ROPE_BACKWARD 5
 #define EBD_WS_PLAN_STEP 6
-#define EBD_WS_ATTEND_TREE 4
 
 /*
  * Workspace bytes needed by ebd_evict (which = EBD_WS_EVICT, params = ebd_evict_params*),
  * ebd_attend_certify (EBD_WS_ATTEND, ebd_attend_params*), ebd_scores (EBD_WS_SCORES,
- * ebd_scores_params*) or ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*),
- * ebd_norm_rope_backward (EBD_WS_NORM_ROPE_BACKWARD,
- * ebd_norm_rope_backward_params*),
- * ebd_plan_step (EBD_WS_PLAN_STEP, ebd_plan_step_params*),
- * ebd_attend_tree (EBD_WS_ATTEND_TREE, ebd_attend_tree_params*).
+ * ebd_scores_params*), ebd_attend_paged (EBD_WS_ATTEND_PAGED, ebd_attend_paged_params*), ebd_attend_tree
+ * (EBD_WS_ATTEND_TREE, ebd_attend_tree_params*), ebd_norm_rope_backward (EBD_WS_NORM_ROPE_BACKWARD,
+ * ebd_norm_rope_backward_params*) or ebd_plan_step (EBD_WS_PLAN_STEP, ebd_plan_step_params*).
  * Depends only on the host fields of the params.  Returns 0 on invalid arguments.
  */
 size_t ebd_workspace_size(int32_t which, const void *params);
@@ -720,15 +721,11 @@ const char *ebd_version(void);
  * ebd_timing_read() waits for the recorded events, and adds the elapsed times of kernel `name`
  * ("evict_select", "evict_copy", "attend_split", "attend_finalize", "append_certain",
  * "scores_stats", "scores_accum", "block_contrib", "cert_step", "rope", "append_paged",
- * "attend_paged", "attend_paged_join", "gather_paged",
- * "norm_rope", "norm_rope_backward", "norm_rope_join",
- * "append_norm",
- * "plan_step",
- * "attend_tree", "attend_tree_join",
- * "keep_rows") to *total_ms and its launch count to
- * *launches; it then clears that kernel's record.  The switch is an atomic flag and the records
- * are guarded by a lock, so both calls may come from any host thread; while timing is off no
- * event is created and launches take no lock.
+ * "attend_paged", "attend_paged_join", "gather_paged", "norm_rope", "norm_rope_backward",
+ * "norm_rope_join", "append_norm", "plan_step", "attend_tree", "attend_tree_join", "keep_rows")
+ * to *total_ms and its launch count to *launches; it then clears that kernel's record.  The switch is
+ * an atomic flag and the records are guarded by a lock, so both calls may come from any host
+ * thread; while timing is off no event is created and launches take no lock.
  */
 ebd_status ebd_timing_enable(int32_t enable);
 ebd_status ebd_timing_read(const char *name, double *total_ms, int64_t *launches);

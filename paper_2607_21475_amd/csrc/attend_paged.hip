@@ -20,6 +20,9 @@
 //   the second product costs nothing beside it.  A decode step of 32 sequences of 16384 rows, 8 KV heads of 4 query
 //   heads: 317 us, 6.8 TB/s, its keys and values read exactly once; of one of 4096 rows, 8 heads: 6.3 us and the join
 //   3.5, a chain of loads (lengths, pages, the tile) of half a microsecond each.
+//   Under a mask the same shapes serve trees of up to 32 query rows, us with the mask / in order: 8 KV heads of 4 query heads, 32
+//   sequences of 4 tokens over 16384 rows 327 / 324, of 8 336 / 329 (6.4 TB/s), 64 of 4 over 4096 171 / 167, of 8 183 / 178, one
+//   of 8 over 4096 15.7 / 14.4 (of 4, one block of 16 rows, 12.2 / 11.5).
 // attend_join: the splits of each row, combined in order.
 #include "attend_paged.hpp"
 
@@ -68,7 +71,8 @@ __global__ __launch_bounds__(256, 1) void attend_rows_kernel(AttendPagedLaunch L
   if (sq.held > sq.seen && L.status && sp == 0 && wave == 0) {
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
-      if (__any(TREE ? tree_past_table(L, sq, 16 * b + c) : past_table(L, sq, 16 * b + c)) && lane == 0) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+      if (__any(TREE ? tree_past_table(L, sq, 16 * b + c) : past_table(L, sq, 16 * b + c)) && lane == 0)
+        atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   }
   Range R;
   uint64_t word0[NQ];  // of a row's mask: few rows have few tokens

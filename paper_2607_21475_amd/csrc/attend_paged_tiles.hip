@@ -22,11 +22,11 @@
 //   two groups of four, tiles of 64 keys, one work-group a CU.  Alone on its CU a work-group of four waves takes 1.9 us a
 //   tile, whatever the depth of its loads (three or four tiles on their way: the same), a chain of products, weights and
 //   products; two groups take two tiles in that time, as two work-groups would, but leave half as many partial sums.  Four
-//   sequences of up to 300 tokens, 4 heads of 7, under a window of 2048: 51 us, with work-groups of four waves 58 (three
-//   splits), 77 (one).  32 sequences of 64 tokens over 16384 rows, 8 heads of 4, by blocks of 256: 596 to 627 us (0.88 to
-//   0.92 PFLOP/s, keys read once at 3.5 TB/s), by 128: 650; from keys that caches hold 520, as far as the power limit goes.
+//   sequences of up to 300 tokens, 4 heads of 7, under a window of 2048: 51 to 53 us, with work-groups of four waves 58 (three
+//   splits).  32 sequences of 64 tokens over 16384 rows, 8 heads of 4, by blocks of 256: 605 to 650 us (0.85 to 0.91 PFLOP/s,
+//   keys read once at 3.4 to 3.6 TB/s), by 128: 687; from keys that caches hold 502, as far as the power limit goes.
 //   The matrix products bound it: 4 x 128 operations per (query row, key).  So the weights of the first two shapes are
-//   rounded to bf16 (half a step, 2^-8, averaged over a row's keys); a second product with their tails, 16 bits in all,
+//   rounded to bf16 (half a step, 2^-8, which averages out where many keys share a row); a second product with their tails, 16 bits in all,
 //   costs 20 to 40% (8192 tokens over 8192 rows 770 us with it, 566 without, 1024 over 131072 2930 / 2070, 1024 over 1024
 //   38.7 / 32.0).  Each key's rounding is its own, and few keys rule many rows, so that trees divide by the sum of the rounded
 //   weights (dot products of their pairs with ones; lse keeps the exact sum): y is then off by 2^-8 of the weighted mean of |v - y|,
@@ -141,7 +141,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void attend_tiles_kernel(AttendPag
   const int row = row0 + 32 * rw + c;
   Span span[1] = {TREE ? tree_span_of(L, sq, row) : span_of(L, sq, row)};
   const bool sees = span[0].lo < span[0].hi;
-  if (sq.held > sq.seen && __any(TREE ? tree_past_table(L, sq, row) : past_table(L, sq, row)) && lane == 0 && L.status) atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
+  if (sq.held > sq.seen && __any(TREE ? tree_past_table(L, sq, row) : past_table(L, sq, row)) && lane == 0 && L.status)
+    atomicOr(&L.status[s], EBD_ST_BAD_PAGE);
   Range R, all;
   if (TREE && p.window == 0) {
     all = tree_range_of(sq);

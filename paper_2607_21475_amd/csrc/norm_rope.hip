@@ -14,7 +14,9 @@
 // rows: it makes the token's sines itself, a pair a lane, and finds the token's place itself, so that waves never wait for
 // each other, and both cost one wave's instructions whatever the rows.  (A work-group a token, a wave for each eight rows and
 // the sines shared behind a barrier, issues twice the instructions: 8191 tokens of 40 rows 34.4 us, so 33.0; 5.1 TB/s, of 32
-// rows with shared weights 24 us, 5.5 TB/s, the rate of a copy.)
+// rows with shared weights 24 us, 5.5 TB/s, the rate of a copy.)  Halves that are no whole chunks (kOdd) meet in LDS: 8191
+// tokens of 32 rows, 34 or 126 of 128 elements rotated, 35 us forward and 54 backward with the join, by whole chunks 27 and 44;
+// an append of 8192 tokens, 8 KV heads of 4 query heads, 48 and 40.
 #include "ebd.h"
 #include "ebd_internal.hpp"
 #include "rope_device.hpp"

@@ -173,7 +173,8 @@ AttendPagedLaunch attend_paged_part(const ebd_attend_paged_params *p, bool tree,
   // over.  us as if all were alike / so, 8 KV heads of 4 query heads, up to the most tokens over up to the most rows: 6 of
   // 100 over 8192 120 / 84, 8 of 60 over 16384 146 / 119, 24 of 48 over 16384 402 / 270, 20 of 96 over 16384 474 / 332, 4 of
   // 120 over 16384 126 / 93; over rows that are all alike: 24 of 48 467 / 343, 16 of 64 over 16384 293 / 313, 24 of 64
-  // over 4096 134 / 152, 20 of 60 over 8192 204 / 242.
+  // over 4096 134 / 152, 20 of 60 over 8192 204 / 242.  (All before the sums' division by the rounded weights, which adds 1 to
+  // 4% to either.)  Equal trees over rows that differ show nothing to the host, and are cut as if all were alike.
   const bool ragged = tree && tiles && S > 1 && 4 * sum < 3 * S * rows_max;
   // (a tree's blocks all see to their sequence's end: one more than fill a round costs another, so that the ones that are
   // not full are counted, half a sequence each)
@@ -234,11 +235,11 @@ bool long_blocks(const ebd_attend_paged_params *p, int64_t most) {
 // a key each in the time of one, B's two keys and C's one and a little (it loads every key for twice as many rows).  All
 // blocks of a tree see to its end, so that short launches are alike and nothing ends early beside a longer one.
 // us of A / B / C with their best splits, 8 KV heads of 4 query heads unless said: one sequence, 64 tokens over 4096 rows
-// 25.7 / 24.1 / 28.1, over 32768 66.7 / 51.5 / 73.4; 128 over 16384 55.9 / 51.7 / 53.4; 16 of 48 over 4096 100 / 82 / -;
-// 8 of 32 over 8192 69 / 60 / -; four of up to 300, 4 heads of 7, under a window of 2048 58.6 / 51.6 / 58.1; 24 of 64 over
-// 4096 155 / 164 / 129; 32 of 64 over 8192 340 / 337 / 310; 64 of 64 over 4096 355 / 355 / 316; 64 of 30 over 2048 118 /
-// 124 / -.  Blocks of 256 that are not full, where two of 128 are not either: 32 of 40 over 16384 605 / 582 / 487, 10 of 40 over
-// 32768 368 / 400 / 332, 5 of 48 over 8192 62 / 60 / 59, 40 of 100 over 8192 748 / 728 / 712.
+// 25.4 / 24.3 / 28.2, over 32768 69 / 54 / 76; 128 over 16384 57.5 / 53.4 / 54.3; 16 of 48 over 4096 101 / 79 / 93; 8 of 32 over
+// 8192 71 / 63 / 68; four of up to 300, 4 heads of 7, under a window of 2048 58 / 51 / 57; 24 of 64 over 4096 172 / 168 / 139; 32
+// of 64 over 8192 351 / 350 / 312; 64 of 64 over 4096 374 / 376 / 321; 64 of 30 over 2048 124 / 125 / 127.  Blocks of 256 that
+// are not full, where two of 128 are not either: 32 of 40 over 16384 637 / 597 / 524, 10 of 40 over 32768 400 / 407 / 342, 5 of
+// 48 over 8192 64 / 61 / 60, 40 of 100 over 8192 794 / 756 / 742.
 AttendPagedLaunch tree_part(const ebd_attend_paged_params *p, int64_t rows_max, int64_t sum, int64_t more_than) {
   double a = 0.0, b = 0.0, c = 0.0;
   AttendPagedLaunch L = attend_paged_part(p, true, kTileRows, rows_max, sum, more_than, false, &a);

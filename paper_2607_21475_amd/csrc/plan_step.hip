@@ -8,7 +8,11 @@
 // Few sequences: one launch (plan_one).  Others: three, each of which needs all that the one before it found: plan_count (a
 // wave per sequence: what it needs and gives back), plan_fill (a wave per sequence: sums over the sequences before it, its
 // entries), plan_tokens (a thread per token) or plan_trees (a work-group per sequence, its parents in LDS, where each token
-// walks up to its root).  Latency bounds all of it: 512 sequences and 66 thousand tokens, 1.1 MB read and written, 18.6 us.
+// walks up to its root).  Latency bounds a step of some hundred sequences and shallow trees: 512 sequences and 66 thousand
+// tokens, 1.1 MB read and written, 6.3 + 9.6 + 4.1 us.  Two parts grow faster than the step.  Each work-group of plan_fill adds
+// up all sequences before its own: 512 sequences of one token 9 us, 4096 13, 16384 69, 65536 764.  And a walk is as long as its
+// token is deep, so that chains are quadratic: of 4096 tokens 1200 us in one launch and 3150 in three (as random trees 155 and
+// 164), two of 512 beside 62 trees of 30 58 (14).
 #include "ebd.h"
 #include "ebd_internal.hpp"
 #include "paged_device.hpp"
@@ -72,8 +76,8 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t x) {
 }
 
 // f(entry, its page, whether there is such an entry) for the entries e0 .. e1 - 1 of a sequence, in order, 64 at a time by a
-// wave's lanes, 512 of them in flight (512 sequences, of which 20 with 2049 entries have ended: 29.4 us in all one by one, 18.6
-// so).
+// wave's lanes, 512 of them in flight (512 sequences, of which 20 with 2049 entries have ended, with the copy that puts the tables
+// back, 3 us: 34.1 in all one by one, 22.8 so).
 template <class F>
 __device__ __forceinline__ void scan(const int32_t *row, int e0, int e1, const F &f) {
   constexpr int kFlight = 8;
